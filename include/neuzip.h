@@ -340,6 +340,106 @@ int neuzip_linear_batch_scratch(const neuzip_blob *const *weights, const uint64_
  * (14.6 for rows of 27776). */
 uint64_t neuzip_linear_scratch_bytes(const uint64_t *out_features, uint32_t count, uint64_t in_features, uint32_t tokens);
 
+/*
+ * neuzip_embedding -- the rows of a compressed embedding table that a call's tokens name, scaled, straight from the blob: the
+ * chunks they lie in are decoded, and nothing else.  (Sec. 2.2's compressed forward pass for the layer that is a lookup.)
+ *     out[i] <- bf16(scale * W_hat[token[i]])
+ *
+ *   table      blob of a row-major rows x features bf16 matrix (any mantissa_bits, with or without block-wise normalisation;
+ *              other element types -> EUNSUPPORTED).  features must be a multiple of 8, rows * features = neuzip_elems(table).
+ *   d_tokens   count row numbers, 64-bit integers.  A number outside 0 .. rows - 1 names no row (padding): its output is zeros.
+ *   scale      the product is formed in binary32 and rounded once, to nearest even; with scale = 1 every word leaves as it is.
+ *   d_out      count x features bf16 words, row-major, 16-byte aligned; overwritten.
+ * count = 0 is a call that does nothing.  Never allocates, never synchronises; a malformed stream is reported by neuzip_check
+ * where a row ends with its chunk.  More than 2^31 - 1 pieces of rows (a row has one, two, or one more than the chunks that it is long) -> EUNSUPPORTED.
+ */
+int neuzip_embedding(const neuzip_blob *table, uint64_t rows, uint64_t features, const int64_t *d_tokens, uint64_t count, float scale,
+                     void *d_out, void *hip_stream);
+
+/*
+ * neuzip_embedding_grad -- the gradient of such a table: every row of it, as neuzip_update takes it.
+ *     grad[r] <- bf16(scale * sum of grad_out[i] over the i with token[i] = r)
+ *
+ *   d_tokens, count, scale   as the lookup had them; a token that names no row takes no part.
+ *   d_grad_out  count x features bf16 words, 16-byte aligned.
+ *   rows, features   as above, rows * features below 2^32.
+ *   d_grad      rows x features bf16 words, 16-byte aligned; overwritten, rows without tokens by zeros.
+ *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_embedding_grad_scratch_bytes(), 16-byte aligned, in use until
+ *               the call's work has run (NULL where that is 0).
+ * The sums are held in binary32 and formed in an order that depends on the tokens alone, so that a call's result is the same every
+ * time; scaled and rounded once.  Never allocates, never synchronises.
+ */
+int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d_grad_out, uint64_t rows, uint64_t features, float scale,
+                          void *d_grad, void *d_scratch, uint64_t scratch_bytes, void *hip_stream);
+uint64_t neuzip_embedding_grad_scratch_bytes(uint64_t count, uint64_t rows, uint64_t features);
+
+/* The activation of a gated feed-forward block: g / (1 + exp(-g)), or 0.5 g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))). */
+enum { NEUZIP_SILU = 0, NEUZIP_GELU_TANH = 1 };
+
+/*
+ * neuzip_gated_linear -- the first half of a gated feed-forward block straight from its two compressed weights, for a decoding
+ * batch:   h <- bf16(act(W_hat_gate x) * (W_hat_up x))
+ *
+ *   gate, up    blobs of out_features x in_features matrices, with the rules of neuzip_linear_batch.
+ *   d_x, tokens, in_features   as for neuzip_linear.
+ *   d_h         tokens x out_features bf16 words, row-major; overwritten.
+ *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_gated_linear_scratch_bytes(), 16-byte aligned, in use until
+ *               the call's work has run.
+ * The two sums, the activation and the product are binary32; h is rounded once.  Never allocates, never synchronises.
+ */
+int neuzip_gated_linear(const neuzip_blob *gate, const neuzip_blob *up, uint64_t out_features, uint64_t in_features, const void *d_x,
+                        uint32_t tokens, int activation, void *d_h, void *d_scratch, uint64_t scratch_bytes, void *hip_stream);
+uint64_t neuzip_gated_linear_scratch_bytes(uint64_t out_features, uint64_t in_features, uint32_t tokens);
+
+/*
+ * neuzip_gated_forward / neuzip_gated_backward -- the same on weights that have been decompressed into temporary space (Alg. 1:
+ * a training batch, or a prompt), with its backward pass.
+ *     g <- x W_gate^T,  u <- x W_up^T,  h <- bf16(act(g) * u)
+ *     dg <- dh * u * act'(g),  du <- dh * act(g);   dx <- dg W_gate + du W_up,  dW_gate <- dg^T x,  dW_up <- du^T x
+ *
+ *   d_x               tokens x in_features bf16 words, row-major, like all matrices here.
+ *   d_gate_weight, d_up_weight   out_features x in_features bf16 words.
+ *   in_features, out_features    multiples of 8, at most 2^22; tokens below 2^31, also 0.
+ *   d_h               tokens x out_features bf16 words; overwritten.
+ *   d_gate, d_up      NULL, or room for g and u (bf16, as d_h), which the backward pass takes; both or neither.
+ *   d_grad_h          tokens x out_features bf16 words.
+ *   d_grad_x          tokens x in_features bf16 words, or NULL: not wanted.
+ *   d_grad_gate_weight, d_grad_up_weight   out_features x in_features bf16 words each, as neuzip_update takes them; or both NULL: not
+ *                     wanted.  (No tokens: zeros.)
+ *   d_scratch         device buffer of scratch_bytes bytes, at least neuzip_gated_backward_scratch_bytes(), in use until the call's
+ *                     work has run.
+ * All pointers are aligned to 16 bytes.  Products are exact, sums binary32; h, g, u and the three gradients are rounded once, to nearest
+ * even, and so are dg and du, which the matrix cores take as bf16.  Results do not change from run to run.  Never allocates, never
+ * synchronises.
+ */
+int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, uint64_t tokens, uint64_t out_features,
+                         uint64_t in_features, int activation, void *d_h, void *d_gate, void *d_up, void *hip_stream);
+int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, const void *d_gate, const void *d_up,
+                          const void *d_grad_h, uint64_t tokens, uint64_t out_features, uint64_t in_features, int activation,
+                          void *d_grad_x, void *d_grad_gate_weight, void *d_grad_up_weight, void *d_scratch, uint64_t scratch_bytes,
+                          void *hip_stream);
+uint64_t neuzip_gated_backward_scratch_bytes(uint64_t tokens, uint64_t out_features, uint64_t in_features);
+
+/*
+ * neuzip_linear_adapters -- neuzip_linear with the low-rank adapter of each token's request beside it (fine-tuned variants of one
+ * compressed model, served together):
+ *     y[t] <- W_hat x[t] + b + scale[a] * B[a] (A[a] x[t]),   a = id[t]
+ *
+ *   weight, out_features, in_features, d_x, tokens, d_bias, d_y   as for neuzip_linear; tokens at most 65535 (else EUNSUPPORTED).
+ *   d_a, d_b    adapters x rank x in_features and adapters x out_features x rank bf16 words, 16-byte aligned.  rank: a multiple of 8,
+ *               at most 512 (a smaller one is filled up with zeros).
+ *   d_scales    `adapters` floats, or NULL: 1.
+ *   d_ids       the adapter of each token, 32-bit integers; outside 0 .. adapters - 1: the token has none.
+ *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_linear_adapters_scratch_bytes(), 16-byte aligned, in use until
+ *               the call's work has run.
+ * The low products A x and all sums are binary32.  Never allocates, never synchronises.
+ */
+int neuzip_linear_adapters(const neuzip_blob *weight, uint64_t out_features, uint64_t in_features, const void *d_x, uint32_t tokens,
+                           const float *d_bias, const void *d_a, const void *d_b, uint32_t rank, uint32_t adapters,
+                           const float *d_scales, const int32_t *d_ids, float *d_y, void *d_scratch, uint64_t scratch_bytes,
+                           void *hip_stream);
+uint64_t neuzip_linear_adapters_scratch_bytes(uint64_t out_features, uint64_t in_features, uint32_t tokens, uint32_t rank);
+
 /* Releases the blob and its device memory.  NULL is a no-op. */
 void neuzip_free(neuzip_blob *blob);
 

@@ -6,6 +6,7 @@ name.  If the library has not been built it is built once with hipcc; if that
 is impossible the import fails loudly -- there is no CPU fallback.
 """
 import ctypes
+import math
 import os
 
 import numpy as np
@@ -15,6 +16,7 @@ from . import build as _build
 
 BF16, F32, F16 = 0, 1, 2
 OK, EINVAL, ENOMEM, EHIP, ECORRUPT, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
+SILU, GELU_TANH = 0, 1
 
 
 class NeuzipError(RuntimeError):
@@ -92,6 +94,22 @@ def _load():
     lib.neuzip_release_workspace.restype = i32
     lib.neuzip_set_workspace_limit.argtypes = [u64]
     lib.neuzip_set_workspace_limit.restype = i32
+    f32 = ctypes.c_float
+    lib.neuzip_embedding.argtypes = [vp, u64, u64, vp, u64, f32, vp, vp]
+    lib.neuzip_embedding_grad.argtypes = [vp, u64, vp, u64, u64, f32, vp, vp, u64, vp]
+    lib.neuzip_embedding_grad_scratch_bytes.argtypes = [u64, u64, u64]
+    lib.neuzip_gated_linear.argtypes = [vp, vp, u64, u64, vp, u32, i32, vp, vp, u64, vp]
+    lib.neuzip_gated_linear_scratch_bytes.argtypes = [u64, u64, u32]
+    lib.neuzip_gated_forward.argtypes = [vp, vp, vp, u64, u64, u64, i32, vp, vp, vp, vp]
+    lib.neuzip_gated_backward.argtypes = [vp, vp, vp, vp, vp, vp, u64, u64, u64, i32, vp, vp, vp, vp, u64, vp]
+    lib.neuzip_gated_backward_scratch_bytes.argtypes = [u64, u64, u64]
+    lib.neuzip_linear_adapters.argtypes = [vp, u64, u64, vp, u32, vp, vp, vp, u32, u32, vp, vp, vp, vp, u64, vp]
+    lib.neuzip_linear_adapters_scratch_bytes.argtypes = [u64, u64, u32, u32]
+    for name in ("neuzip_embedding", "neuzip_embedding_grad", "neuzip_gated_linear", "neuzip_gated_forward", "neuzip_gated_backward",
+                 "neuzip_linear_adapters"):
+        getattr(lib, name).restype = i32
+    for name in ("neuzip_embedding_grad", "neuzip_gated_linear", "neuzip_gated_backward", "neuzip_linear_adapters"):
+        getattr(lib, name + "_scratch_bytes").restype = u64
     lib.neuzip_strerror.argtypes = [i32]
     lib.neuzip_strerror.restype = ctypes.c_char_p
     lib.neuzip_last_hip_error.argtypes = []
@@ -105,6 +123,9 @@ _lib = _load()
 EXPORTED = ["neuzip_compress", "neuzip_compress_noalloc", "neuzip_compress_blockwise", "neuzip_compress_batch", "neuzip_compress_guarded",
             "neuzip_recompress", "neuzip_update", "neuzip_guard", "neuzip_linear", "neuzip_linear_batch",
             "neuzip_linear_batch_scratch", "neuzip_linear_scratch_bytes",
+            "neuzip_embedding", "neuzip_embedding_grad", "neuzip_embedding_grad_scratch_bytes",
+            "neuzip_gated_linear", "neuzip_gated_linear_scratch_bytes", "neuzip_gated_forward", "neuzip_gated_backward",
+            "neuzip_gated_backward_scratch_bytes", "neuzip_linear_adapters", "neuzip_linear_adapters_scratch_bytes",
             "neuzip_block_size", "neuzip_decompress", "neuzip_decompress_sequence", "neuzip_decompress_batch", "neuzip_free",
             "neuzip_compressed_bytes", "neuzip_device_bytes", "neuzip_elems", "neuzip_mantissa_bits", "neuzip_dtype",
             "neuzip_export", "neuzip_import", "neuzip_histogram", "neuzip_frequencies", "neuzip_check", "neuzip_stream_probe",
@@ -447,6 +468,195 @@ def neuzip_linear_batch(weights, out_features, in_features: int, x: torch.Tensor
     tokens = _check_linear(weights, out_features, in_features, x, biases, ys)
     _linear_call(weights, out_features, in_features, x, tokens, biases, ys, stream, "neuzip_linear_batch")
     return ys
+
+
+def _pointer(t):
+    return ctypes.c_void_p(t.data_ptr() if t is not None else None)
+
+
+def _expect(t, dtype, shape, what):
+    """t, a contiguous CUDA tensor of that type and of as many elements as the shape has (its own shape is the caller's affair)."""
+    if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype):
+        raise TypeError(f"expected a contiguous {dtype} CUDA tensor: {what}")
+    if t.numel() != math.prod(shape):
+        raise ValueError(f"{what} must be {' x '.join(str(s) for s in shape)}")
+    return t
+
+
+def _own_scratch(size, scratch, device, stream):
+    """The caller's scratch memory, or the call's own: of the stream's that its work runs on, so that it is not handed out to
+    another one's while it is in use."""
+    if scratch is not None:
+        if not (scratch.is_cuda and scratch.is_contiguous()):
+            raise TypeError("expected a contiguous CUDA tensor as scratch memory")
+        return scratch
+    if stream is not None and isinstance(stream, torch.cuda.Stream):
+        with torch.cuda.stream(stream):
+            return torch.empty(size, dtype=torch.uint8, device=device)
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def _bytes_of(t):
+    return t.numel() * t.element_size()
+
+
+def neuzip_embedding(table: Blob, rows: int, features: int, tokens: torch.Tensor, scale: float = 1.0, out: torch.Tensor = None,
+                     stream=None) -> torch.Tensor:
+    """The rows of a compressed embedding table (rows x features) that `tokens` (int64, any shape) name, times scale, rounded to
+    bf16; a number outside 0 .. rows - 1 names none and yields zeros."""
+    _expect(tokens, torch.int64, tokens.shape, "tokens")
+    if out is None:
+        out = torch.empty((*tokens.shape, features), dtype=torch.bfloat16, device=tokens.device)
+    _expect(out, torch.bfloat16, (tokens.numel(), features), "out")
+    rc = _lib.neuzip_embedding(table.handle, rows, features, _pointer(tokens), tokens.numel(), scale, _pointer(out), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_embedding")
+    return out
+
+
+def neuzip_embedding_grad_scratch_bytes(count: int, rows: int, features: int) -> int:
+    return int(_lib.neuzip_embedding_grad_scratch_bytes(count, rows, features))
+
+
+def neuzip_embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, rows: int, scale: float = 1.0, grad: torch.Tensor = None,
+                          scratch=None, stream=None) -> torch.Tensor:
+    """The gradient (bf16, rows x features, every row) of the table that was looked up, from grad_out (bf16, tokens x features)."""
+    _expect(tokens, torch.int64, tokens.shape, "tokens")
+    features = grad_out.shape[-1] if grad_out.dim() else 0
+    _expect(grad_out, torch.bfloat16, (tokens.numel(), features), "grad_out")
+    if grad is None:
+        grad = torch.empty((rows, features), dtype=torch.bfloat16, device=grad_out.device)
+    _expect(grad, torch.bfloat16, (rows, features), "grad")
+    scratch = _own_scratch(neuzip_embedding_grad_scratch_bytes(tokens.numel(), rows, features), scratch, grad_out.device, stream)
+    rc = _lib.neuzip_embedding_grad(_pointer(tokens), tokens.numel(), _pointer(grad_out), rows, features, scale, _pointer(grad),
+                                    _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_embedding_grad")
+    return grad
+
+
+def _tokens_of(x, in_features):
+    _check_tensor(x)
+    tokens = x.numel() // in_features if in_features else 0
+    if x.numel() != tokens * in_features:
+        raise ValueError("activations must be tokens x in_features")
+    return tokens
+
+
+def neuzip_gated_linear_scratch_bytes(out_features: int, in_features: int, tokens: int) -> int:
+    return int(_lib.neuzip_gated_linear_scratch_bytes(out_features, in_features, tokens))
+
+
+def neuzip_gated_linear(gate: Blob, up: Blob, out_features: int, in_features: int, x: torch.Tensor, activation: int = SILU,
+                        h: torch.Tensor = None, scratch=None, stream=None) -> torch.Tensor:
+    """h = act(x W_gate^T) * (x W_up^T), bf16, straight from the two compressed weights."""
+    tokens = _tokens_of(x, in_features)
+    if h is None:
+        h = torch.empty((tokens, out_features), dtype=torch.bfloat16, device=x.device)
+    _expect(h, torch.bfloat16, (tokens, out_features), "h")
+    scratch = _own_scratch(neuzip_gated_linear_scratch_bytes(out_features, in_features, tokens), scratch, x.device, stream)
+    rc = _lib.neuzip_gated_linear(gate.handle, up.handle, out_features, in_features, _pointer(x), tokens, activation, _pointer(h),
+                                  _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_gated_linear")
+    return h
+
+
+def _gated_shape(x, w_gate, w_up):
+    _check_tensor(w_gate)
+    if w_gate.dim() != 2:
+        raise ValueError("weights must be out_features x in_features")
+    out_features, in_features = w_gate.shape
+    _expect(w_up, torch.bfloat16, (out_features, in_features), "w_up")
+    return _tokens_of(x, in_features), out_features, in_features
+
+
+def neuzip_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: int = SILU, h: torch.Tensor = None,
+                         keep=False, stream=None):
+    """h = act(x W_gate^T) * (x W_up^T), bf16, from decompressed weights.  keep: returns (h, gate, up), with the two products that
+    neuzip_gated_backward takes (a pair of tensors: into these)."""
+    tokens, out_features, in_features = _gated_shape(x, w_gate, w_up)
+    shape = (tokens, out_features)
+    if h is None:
+        h = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+    _expect(h, torch.bfloat16, shape, "h")
+    gate = up = None
+    if keep is True:
+        gate, up = torch.empty_like(h), torch.empty_like(h)
+    elif keep:
+        gate, up = keep
+        _expect(gate, torch.bfloat16, shape, "gate")
+        _expect(up, torch.bfloat16, shape, "up")
+    rc = _lib.neuzip_gated_forward(_pointer(x), _pointer(w_gate), _pointer(w_up), tokens, out_features, in_features, activation,
+                                   _pointer(h), _pointer(gate), _pointer(up), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_gated_forward")
+    return (h, gate, up) if keep else h
+
+
+def neuzip_gated_backward_scratch_bytes(tokens: int, out_features: int, in_features: int) -> int:
+    return int(_lib.neuzip_gated_backward_scratch_bytes(tokens, out_features, in_features))
+
+
+def neuzip_gated_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, gate: torch.Tensor, up: torch.Tensor,
+                          grad_h: torch.Tensor, activation: int = SILU, grad_x=True, grad_weights=True, scratch=None, stream=None):
+    """(grad_x, grad_w_gate, grad_w_up), bf16.  grad_x and grad_weights: True, False (not wanted: None), or the tensor and the pair
+    of tensors that receive them."""
+    tokens, out_features, in_features = _gated_shape(x, w_gate, w_up)
+    for t, what in ((gate, "gate"), (up, "up"), (grad_h, "grad_h")):
+        _expect(t, torch.bfloat16, (tokens, out_features), what)
+    if grad_x is True:
+        grad_x = torch.empty((tokens, in_features), dtype=torch.bfloat16, device=x.device)
+    elif grad_x is False:
+        grad_x = None
+    if grad_weights is True:
+        grad_weights = (torch.empty_like(w_gate), torch.empty_like(w_up))
+    elif grad_weights is False:
+        grad_weights = (None, None)
+    if grad_x is not None:
+        _expect(grad_x, torch.bfloat16, (tokens, in_features), "grad_x")
+    for t in grad_weights:
+        if t is not None:
+            _expect(t, torch.bfloat16, (out_features, in_features), "grad_weights")
+    scratch = _own_scratch(neuzip_gated_backward_scratch_bytes(tokens, out_features, in_features), scratch, x.device, stream)
+    rc = _lib.neuzip_gated_backward(_pointer(x), _pointer(w_gate), _pointer(w_up), _pointer(gate), _pointer(up), _pointer(grad_h),
+                                    tokens, out_features, in_features, activation, _pointer(grad_x), _pointer(grad_weights[0]),
+                                    _pointer(grad_weights[1]), _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_gated_backward")
+    return grad_x, grad_weights[0], grad_weights[1]
+
+
+def neuzip_linear_adapters_scratch_bytes(out_features: int, in_features: int, tokens: int, rank: int) -> int:
+    return int(_lib.neuzip_linear_adapters_scratch_bytes(out_features, in_features, tokens, rank))
+
+
+def neuzip_linear_adapters(weight: Blob, out_features: int, in_features: int, x: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                           scales, ids: torch.Tensor, bias: torch.Tensor = None, y: torch.Tensor = None, scratch=None,
+                           stream=None) -> torch.Tensor:
+    """y[t] = x[t] W_hat^T + bias + scales[i] * b[i] (a[i] x[t]) with i = ids[t] (float32).  a: adapters x rank x in_features, b:
+    adapters x out_features x rank (bf16); scales: float32, or None (1); ids: int32, outside 0 .. adapters - 1: no adapter."""
+    tokens = _tokens_of(x, in_features)
+    if a.dim() != 3:
+        raise ValueError("a must be adapters x rank x in_features")
+    adapters, rank = a.shape[:2]
+    _expect(a, torch.bfloat16, (adapters, rank, in_features), "a")
+    _expect(b, torch.bfloat16, (adapters, out_features, rank), "b")
+    _expect(ids, torch.int32, (tokens,), "ids")
+    if scales is not None:
+        _expect(scales, torch.float32, (adapters,), "scales")
+    if bias is not None:
+        _expect(bias, torch.float32, (out_features,), "bias")
+    if y is None:
+        y = torch.empty((tokens, out_features), dtype=torch.float32, device=x.device)
+    _expect(y, torch.float32, (tokens, out_features), "y")
+    scratch = _own_scratch(neuzip_linear_adapters_scratch_bytes(out_features, in_features, tokens, rank), scratch, x.device, stream)
+    rc = _lib.neuzip_linear_adapters(weight.handle, out_features, in_features, _pointer(x), tokens, _pointer(bias), _pointer(a),
+                                     _pointer(b), rank, adapters, _pointer(scales), _pointer(ids), _pointer(y), _pointer(scratch),
+                                     _bytes_of(scratch), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_linear_adapters")
+    return y
 
 
 def neuzip_free(blob: Blob) -> None:

@@ -1,0 +1,78 @@
+// Low-rank adapters beside a projection for gfx950:  y[t] += s[a] B[a] (A[a] x[t]),  a = id[t].
+//
+// Two launches with the low products, rank floats a token, between them: every row of A is a sum over all input features, and every
+// output wants all of them.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+namespace nz {
+
+struct AdapterArgs {
+    const uint16_t *x;      // [tokens][in_features]
+    const uint16_t *a;      // [adapters][rank][in_features]
+    const uint16_t *b;      // [adapters][out_features][rank]
+    const float *scales;    // [adapters], or nullptr: 1
+    const int32_t *ids;     // [tokens]; outside 0 .. adapters - 1: none
+    float *low;             // [tokens][rank], with the scale
+    float *y;               // [tokens][out_features]
+    uint32_t tokens, adapters, rank, in_features, out_features;
+};
+
+__device__ __forceinline__ float adapter_low_half(uint32_t d) { return __uint_as_float(d << 16); }
+__device__ __forceinline__ float adapter_high_half(uint32_t d) { return __uint_as_float(d & 0xFFFF0000u); }
+__device__ __forceinline__ float adapter_dot(const uint4 &p, const uint4 &q, float sum)
+{
+    const uint32_t ps[4] = {p.x, p.y, p.z, p.w}, qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        sum = fmaf(adapter_low_half(ps[i]), adapter_low_half(qs[i]), sum);
+        sum = fmaf(adapter_high_half(ps[i]), adapter_high_half(qs[i]), sum);
+    }
+    return sum;
+}
+
+// low[t][r] = s (A[a] x[t])[r]: a wave to a token and a row of A.
+constexpr uint32_t kAdapterThreads = 256;
+__global__ __launch_bounds__(kAdapterThreads) void adapter_low_kernel(const AdapterArgs g)
+{
+    const uint32_t lane = threadIdx.x % 64, r = blockIdx.x * (kAdapterThreads / 64) + threadIdx.x / 64, t = blockIdx.y;
+    const int32_t id = g.ids[t];
+    if (r >= g.rank || id < 0 || static_cast<uint32_t>(id) >= g.adapters)
+        return;
+    const uint4 *x = reinterpret_cast<const uint4 *>(g.x + static_cast<uint64_t>(t) * g.in_features);
+    const uint4 *a = reinterpret_cast<const uint4 *>(g.a + (static_cast<uint64_t>(id) * g.rank + r) * g.in_features);
+    float sum = 0.0f;
+    for (uint32_t i = lane; i < g.in_features / 8; i += 64)
+        sum = adapter_dot(x[i], a[i], sum);
+#pragma unroll
+    for (int apart = 32; apart > 0; apart /= 2)
+        sum += __shfl_xor(sum, apart);
+    if (lane == 0)
+        g.low[static_cast<uint64_t>(t) * g.rank + r] = g.scales ? g.scales[id] * sum : sum;
+}
+
+// y[t][o] += B[a][o] . low[t]: a thread to an output.
+__global__ __launch_bounds__(kAdapterThreads) void adapter_high_kernel(const AdapterArgs g)
+{
+    const uint32_t o = blockIdx.x * kAdapterThreads + threadIdx.x, t = blockIdx.y;
+    const int32_t id = g.ids[t];
+    if (o >= g.out_features || id < 0 || static_cast<uint32_t>(id) >= g.adapters)
+        return;
+    const uint4 *b = reinterpret_cast<const uint4 *>(g.b + (static_cast<uint64_t>(id) * g.out_features + o) * g.rank);
+    const float *low = g.low + static_cast<uint64_t>(t) * g.rank;
+    float sum = 0.0f;
+    for (uint32_t i = 0; i < g.rank / 8; ++i) {
+        const uint4 v = b[i];
+        const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            sum = fmaf(adapter_low_half(d[p]), low[8 * i + 2 * p], sum);
+            sum = fmaf(adapter_high_half(d[p]), low[8 * i + 2 * p + 1], sum);
+        }
+    }
+    g.y[static_cast<uint64_t>(t) * g.out_features + o] += sum;
+}
+
+}  // namespace nz

@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "neuzip_format.h"
+#include "neuzip_walk.h"
 
 namespace nz {
 
@@ -107,23 +108,6 @@ __device__ __forceinline__ uint64_t fields_of(const uint32_t (&w)[4])
 // IEEE binary32 arithmetic, results rounded to the nearest-even bf16; NaNs are passed through
 // with the quiet bit set, without going through the FP unit.
 // ------------------------------------------------------------------------------------------
-// binary32 -> bf16, round to nearest even: the conversion instruction of gfx950
-__device__ __forceinline__ uint32_t bf16_of(float v)
-{
-    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
-}
-
-__device__ __forceinline__ bool bf16_is_nan(uint32_t u) { return (u & 0x7FFFu) > 0x7F80u; }
-
-__device__ __forceinline__ uint32_t normalise_word(uint32_t u, float c)
-{
-    if (bf16_is_nan(u))
-        return u | 0x40u;
-    return bf16_of(__uint_as_float(u << 16) / c);
-}
-
-__device__ __forceinline__ float coefficient(uint32_t coef) { return 1.0f + static_cast<float>(coef) * 0.0078125f; }
-
 // ------------------------------------------------------------------------------------------
 // Element types.  The method is stated for BFloat16 (Sec. 2.1).  A binary32 word carries the same
 // sign and exponent bits in its upper half, which is a bf16 word; that half goes through the
@@ -199,10 +183,6 @@ __device__ __forceinline__ uint32_t source_word(const void *__restrict__ src, ui
     }
 }
 
-// Stores and atomics issued so far by this wave have been performed (their acknowledgements are in)
-// before anything that follows.
-__device__ __forceinline__ void wait_for_memory_acks() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-
 // A store to host memory past the caches (system scope), 16 bytes per lane: a wave's neighbouring pieces travel together, while
 // 8-byte atomic stores are a transaction each (the statistics of seven tensors took 22 us).  (The wait states keep what
 // follows from writing the data registers before the store has read them, which the compiler sees to for its own stores only.)
@@ -235,59 +215,6 @@ __device__ __forceinline__ void store_through(const uint8_t *from, uint32_t at, 
 //   most frequent symbol (lowest value on a tie); an excess is taken one unit at a time from
 //   the symbol whose f is largest at that moment (lowest value on a tie).
 // ------------------------------------------------------------------------------------------
-// Inclusive scan of v over the 64 lanes of the wave with data-parallel-primitive moves (vector ALU
-// rate: no trip through the LDS crossbar as with a lane shuffle): inside each row of 16 lanes by
-// shifts of 1, 2, 4, 8 (a lane without a source keeps the identity), then the last lane of rows 0
-// and 2 is added into rows 1 and 3, then lane 31 into rows 2 and 3.  All 64 lanes must be active.
-template <class Op>
-__device__ __forceinline__ uint32_t row_scan_u32(uint32_t v, uint32_t identity, Op op)
-{
-#define NZ_DPP(ctrl, rows) \
-    static_cast<uint32_t>(__builtin_amdgcn_update_dpp(static_cast<int>(identity), static_cast<int>(v), ctrl, rows, 0xf, false))
-    v = op(v, NZ_DPP(0x111, 0xf));  // row_shr:1
-    v = op(v, NZ_DPP(0x112, 0xf));  // row_shr:2
-    v = op(v, NZ_DPP(0x114, 0xf));  // row_shr:4
-    v = op(v, NZ_DPP(0x118, 0xf));  // row_shr:8
-    return v;
-}
-
-template <class Op>
-__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v, uint32_t identity, Op op)
-{
-    v = row_scan_u32(v, identity, op);
-    v = op(v, NZ_DPP(0x142, 0xa));  // row_bcast:15 into rows 1 and 3
-    v = op(v, NZ_DPP(0x143, 0xc));  // row_bcast:31 into rows 2 and 3
-#undef NZ_DPP
-    return v;
-}
-
-struct OpAdd {
-    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a + b; }
-};
-struct OpMax {
-    __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
-};
-
-// Inclusive sum over the lanes of a row of 16 (all of them active).
-__device__ __forceinline__ uint32_t row_scan_u32(uint32_t v) { return row_scan_u32(v, 0u, OpAdd{}); }
-
-// ... and of a half of 32.
-__device__ __forceinline__ uint32_t half_scan_u32(uint32_t v)
-{
-    v = row_scan_u32(v);
-    // row_bcast:15 into rows 1 and 3
-    return v + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x142, 0xa, 0xf, false));
-}
-
-// Sum / maximum over the wave, the same value in every lane (lane 63 of the scan, read out as a scalar).
-__device__ __forceinline__ uint32_t wave_sum_u32(uint32_t v)
-{
-    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_scan_u32(v, 0u, OpAdd{})), 63));
-}
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v)
-{
-    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(wave_scan_u32(v, 0u, OpMax{})), 63));
-}
 
 // The frequencies (f) and exclusive cumulative frequencies (cum) of symbols 4 * lane .. 4 * lane + 3
 // from their counts, which add up to `total`; returns the tensor's only exponent value if it has

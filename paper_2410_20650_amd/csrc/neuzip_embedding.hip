@@ -1,0 +1,146 @@
+// Embedding on a compressed table: host side of the C ABI (see include/neuzip.h).
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <cstring>
+
+#include "neuzip.h"
+
+#include "neuzip_embedding_kernels.h"
+#include "neuzip_host.h"
+
+using namespace nz;
+
+namespace {
+
+inline bool valid_table(uint64_t rows, uint64_t features)
+{
+    return rows > 0 && features > 0 && features % kRun == 0 && rows < (1ull << 32) && features < (1ull << 32) &&
+           rows * features < (1ull << 32);
+}
+
+template <int KB, bool NORM>
+void launch_embedding(const EmbeddingArgs &a, hipStream_t stream)
+{
+    // Few units: workgroups of four waves, and the step without a branch, as long as a CU has one or two of them.
+    constexpr uint32_t kFew = 256, kMany = 512;
+    const uint32_t wgs = (a.units + kFew / kStates - 1) / (kFew / kStates);
+    if (wgs <= 512)
+        hipLaunchKernelGGL((embedding_kernel<KB, NORM, true, kFew>), dim3(wgs), dim3(kFew), 0, stream, a);
+    else
+        hipLaunchKernelGGL((embedding_kernel<KB, NORM, false, kMany>), dim3((a.units + kMany / kStates - 1) / (kMany / kStates)), dim3(kMany), 0,
+                           stream, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int neuzip_embedding(const neuzip_blob *table, uint64_t rows, uint64_t features, const int64_t *d_tokens, uint64_t count, float scale,
+                     void *d_out, void *hip_stream)
+{
+    if (!is_blob(table) || !table->has_table || !on_current_device(table) || !valid_table(rows, features) || rows * features != table->n)
+        return NEUZIP_EINVAL;
+    if (table->elem != NEUZIP_BF16)
+        return NEUZIP_EUNSUPPORTED;
+    if (count == 0)
+        return NEUZIP_OK;
+    if (!d_tokens || !d_out || (reinterpret_cast<uintptr_t>(d_tokens) & 7u) || (reinterpret_cast<uintptr_t>(d_out) & 15u))
+        return NEUZIP_EINVAL;
+    // units of a token: as many as a row's elements can touch
+    const uint64_t unit = has_entry_points(table->n_chunks) ? kMidTurn * kTurn : kChunk;
+    const uint64_t per_token = unit % features == 0 ? 1 : (features % unit == 0 ? features / unit : (features - 1) / unit + 2);
+    if (count >= (1ull << 31) || count * per_token >= (1ull << 31))
+        return NEUZIP_EUNSUPPORTED;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const int behind = follow(table, stream);
+    if (behind != NEUZIP_OK)
+        return behind;
+    EmbeddingArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.tb = table_of(table);
+    a.offsets = offsets_of(table);
+    a.states = states_of(table);
+    a.lens = lens_of(table);
+    a.mid_states = mid_states_of(table);
+    a.mid_lens = mid_lens_of(table);
+    a.words = reinterpret_cast<const uint16_t *>(table->words);
+    a.sm = sm_of(table);
+    a.coef = coef_of(table);
+    while (table->block && (1u << a.block_shift) < table->block)
+        ++a.block_shift;
+    a.n_chunks = table->n_chunks;
+    a.status = table_of(table)->status;
+    a.tokens = d_tokens;
+    a.out = static_cast<uint16_t *>(d_out);
+    a.rows = static_cast<uint32_t>(rows);
+    a.features = static_cast<uint32_t>(features);
+    a.per_token.set(static_cast<uint32_t>(per_token));
+    a.units = static_cast<uint32_t>(count * per_token);
+    a.scale = scale;
+    if (table->block) {
+        switch (table->k) {
+        case 3: launch_embedding<3, true>(a, stream); break;
+        case 1: launch_embedding<1, true>(a, stream); break;
+        default: launch_embedding<0, true>(a, stream); break;
+        }
+    } else {
+        switch (table->k) {
+        case 7: launch_embedding<7, false>(a, stream); break;
+        case 3: launch_embedding<3, false>(a, stream); break;
+        case 1: launch_embedding<1, false>(a, stream); break;
+        default: launch_embedding<0, false>(a, stream); break;
+        }
+    }
+    return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
+}
+
+uint64_t neuzip_embedding_grad_scratch_bytes(uint64_t count, uint64_t rows, uint64_t features)
+{
+    if (!valid_table(rows, features) || count >= (1ull << 31))
+        return 0;
+    const uint64_t runs = (count + kSortRun - 1) / kSortRun;
+    return runs * sizeof(SortedRun) + (count > kPieceTokens ? runs * kPiecesMost * features * sizeof(float) : 0);
+}
+
+int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d_grad_out, uint64_t rows, uint64_t features, float scale,
+                          void *d_grad, void *d_scratch, uint64_t scratch_bytes, void *hip_stream)
+{
+    if (!valid_table(rows, features) || !d_grad || (reinterpret_cast<uintptr_t>(d_grad) & 15u))
+        return NEUZIP_EINVAL;
+    if (count >= (1ull << 31))
+        return NEUZIP_EUNSUPPORTED;
+    if (count > 0 && (!d_tokens || !d_grad_out || !d_scratch || (reinterpret_cast<uintptr_t>(d_tokens) & 7u) ||
+                      (reinterpret_cast<uintptr_t>(d_grad_out) & 15u) || (reinterpret_cast<uintptr_t>(d_scratch) & 15u) ||
+                      scratch_bytes < neuzip_embedding_grad_scratch_bytes(count, rows, features)))
+        return NEUZIP_EINVAL;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    EmbeddingGradArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.tokens = d_tokens;
+    a.count = count;
+    a.grad_out = static_cast<const uint16_t *>(d_grad_out);
+    a.grad = static_cast<uint16_t *>(d_grad);
+    a.runs = static_cast<SortedRun *>(d_scratch);
+    a.n_runs = static_cast<uint32_t>((count + kSortRun - 1) / kSortRun);
+    a.partial = reinterpret_cast<float *>(a.runs + a.n_runs);
+    a.rows = static_cast<uint32_t>(rows);
+    a.features = static_cast<uint32_t>(features);
+    while (((rows - 1) >> a.range_shift) >= kSortRanges)
+        ++a.range_shift;
+    a.row_pieces.set(static_cast<uint32_t>(features / kRun));
+    a.scale = scale;
+    if (a.n_runs > 65535)
+        return NEUZIP_EUNSUPPORTED;
+    if (count > 0)
+        hipLaunchKernelGGL(embedding_sort_kernel, dim3(a.n_runs), dim3(kSortThreads), 0, stream, a);
+    if (count > kPieceTokens)
+        hipLaunchKernelGGL(embedding_pieces_kernel, dim3(kPiecesMost, a.n_runs, (a.row_pieces.by + kGradThreads - 1) / kGradThreads), dim3(kGradThreads), 0,
+                           stream, a);
+    const uint64_t pieces = rows * a.row_pieces.by, each = kGradThreads * kGradPieces;
+    hipLaunchKernelGGL(embedding_write_kernel, dim3(static_cast<uint32_t>((pieces + each - 1) / each)), dim3(kGradThreads), 0, stream, a);
+    return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
+}
+
+}  // extern "C"

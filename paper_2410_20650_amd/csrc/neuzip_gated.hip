@@ -1,0 +1,206 @@
+// Gated feed-forward block: host side of the C ABI (see include/neuzip.h).
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <cstring>
+
+#include "neuzip.h"
+
+#include "neuzip_gated_kernels.h"
+#include "neuzip_host.h"
+
+using namespace nz;
+
+namespace {
+
+// Widths of the matrices: offsets inside a tile (256 rows) have 32 bits.
+constexpr uint64_t kGatedWidest = 1ull << 22;
+constexpr uint64_t kGatedMostTokens = 1ull << 31;
+
+inline bool misaligned(const void *p) { return reinterpret_cast<uintptr_t>(p) & 15u; }
+inline bool valid_activation(int a) { return a == NEUZIP_SILU || a == NEUZIP_GELU_TANH; }
+inline bool valid_width(uint64_t w) { return w > 0 && w % 8 == 0 && w <= kGatedWidest; }
+
+inline uint32_t tiles_of(uint64_t n, uint32_t size) { return static_cast<uint32_t>((n + size - 1) / size); }
+
+struct GatedShape {
+    uint32_t size, slices;
+};
+
+// Tiles of 256 where there are enough of them for the CUs, else of 128; the input gradient's sum in slices where even these are few.
+template <GatedForm FORM>
+GatedShape gated_shape(uint64_t rows, uint64_t cols, uint64_t depth)
+{
+    auto tiles = [&](uint32_t size) {
+        return static_cast<uint64_t>(tiles_of(rows, size)) * tiles_of(cols, FORM == kForward ? size / 2 : size) * (FORM == kWeightGrad ? 2 : 1);
+    };
+    GatedShape s = {tiles(256) >= 256 ? 256u : 128u, 1u};
+    if (FORM == kInputGrad) {
+        const uint64_t steps = 2 * tiles_of(depth, kGatedDepth), have = tiles(s.size);
+        while (s.slices < 16 && have * s.slices * 2 <= 512 && steps / (s.slices * 2) >= 8)
+            s.slices *= 2;
+    }
+    return s;
+}
+
+template <GatedForm FORM>
+int launch_gated(GatedArgs &a, const GatedShape &shape, hipStream_t stream)
+{
+    a.tiles_i = tiles_of(a.rows, shape.size);
+    a.tiles_j = tiles_of(a.cols, FORM == kForward ? shape.size / 2 : shape.size);
+    a.slices = shape.slices;
+    const uint64_t grid = static_cast<uint64_t>(a.tiles_i) * a.tiles_j * shape.slices * (FORM == kWeightGrad ? 2 : 1);
+    if (grid >= (1ull << 31))
+        return NEUZIP_EUNSUPPORTED;
+    if (shape.size == 256)
+        hipLaunchKernelGGL((gated_kernel<FORM, 256>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedWaves<256> * 64), 0, stream, a);
+    else
+        hipLaunchKernelGGL((gated_kernel<FORM, 128>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedWaves<128> * 64), 0, stream, a);
+    return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
+}
+
+inline uint64_t wgs_for(uint64_t threads) { return (threads + kGatedSlopeThreads - 1) / kGatedSlopeThreads; }
+
+}  // namespace
+
+extern "C" {
+
+int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, uint64_t tokens,
+                         uint64_t out_features, uint64_t in_features, int activation, void *d_h, void *d_gate, void *d_up,
+                         void *hip_stream)
+{
+    if (!valid_activation(activation) || !valid_width(out_features) || !valid_width(in_features) || tokens >= kGatedMostTokens)
+        return NEUZIP_EINVAL;
+    if (tokens == 0)
+        return NEUZIP_OK;
+    if (!d_x || !d_gate_weight || !d_up_weight || !d_h || !d_gate != !d_up)
+        return NEUZIP_EINVAL;
+    for (const void *p : {d_x, d_gate_weight, d_up_weight, static_cast<const void *>(d_h), static_cast<const void *>(d_gate), static_cast<const void *>(d_up)})
+        if (misaligned(p))
+            return NEUZIP_EINVAL;
+    GatedArgs a;
+    std::memset(&a, 0, sizeof(a));
+    a.q[0] = a.q[1] = static_cast<const uint16_t *>(d_x);
+    a.p[0] = static_cast<const uint16_t *>(d_gate_weight);
+    a.p[1] = static_cast<const uint16_t *>(d_up_weight);
+    a.c[0] = static_cast<uint16_t *>(d_h);
+    a.gate = static_cast<uint16_t *>(d_gate);
+    a.up = static_cast<uint16_t *>(d_up);
+    a.rows = static_cast<uint32_t>(tokens);
+    a.cols = a.c_row = static_cast<uint32_t>(out_features);
+    a.depth = a.q_row = a.p_row = static_cast<uint32_t>(in_features);
+    a.activation = static_cast<uint32_t>(activation);
+    return launch_gated<kForward>(a, gated_shape<kForward>(a.rows, a.cols, a.depth), static_cast<hipStream_t>(hip_stream));
+}
+
+uint64_t neuzip_gated_backward_scratch_bytes(uint64_t tokens, uint64_t out_features, uint64_t in_features)
+{
+    if (!valid_width(out_features) || !valid_width(in_features) || tokens == 0 || tokens >= kGatedMostTokens)
+        return 0;
+    const GatedShape shape = gated_shape<kInputGrad>(tokens, in_features, out_features);
+    return 2 * pad_to(tokens * out_features * 2, 256) + (shape.slices > 1 ? shape.slices * tokens * in_features * sizeof(float) : 0);
+}
+
+int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, const void *d_gate, const void *d_up,
+                          const void *d_grad_h, uint64_t tokens, uint64_t out_features, uint64_t in_features, int activation,
+                          void *d_grad_x, void *d_grad_gate_weight, void *d_grad_up_weight, void *d_scratch, uint64_t scratch_bytes,
+                          void *hip_stream)
+{
+    if (!valid_activation(activation) || !valid_width(out_features) || !valid_width(in_features) || tokens >= kGatedMostTokens)
+        return NEUZIP_EINVAL;
+    if (!d_grad_gate_weight != !d_grad_up_weight)
+        return NEUZIP_EINVAL;
+    const bool weights = d_grad_gate_weight != nullptr;
+    if (tokens > 0 && (!d_gate || !d_up || !d_grad_h || !d_scratch || (weights && !d_x) || (d_grad_x && (!d_gate_weight || !d_up_weight)) ||
+                       scratch_bytes < neuzip_gated_backward_scratch_bytes(tokens, out_features, in_features)))
+        return NEUZIP_EINVAL;
+    for (const void *p : {d_x, d_gate_weight, d_up_weight, d_gate, d_up, d_grad_h, static_cast<const void *>(d_grad_x),
+                          static_cast<const void *>(d_grad_gate_weight), static_cast<const void *>(d_grad_up_weight),
+                          static_cast<const void *>(d_scratch)})
+        if (misaligned(p))
+            return NEUZIP_EINVAL;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    uint16_t *dg = static_cast<uint16_t *>(d_scratch);
+    uint16_t *du = dg + pad_to(tokens * out_features * 2, 256) / 2;
+    float *partial = reinterpret_cast<float *>(du + pad_to(tokens * out_features * 2, 256) / 2);
+    if (tokens > 0) {
+        const uint64_t pieces = tokens * out_features / 8;
+        if (wgs_for(pieces) >= (1ull << 31))
+            return NEUZIP_EUNSUPPORTED;
+        hipLaunchKernelGGL(gated_slope_kernel, dim3(static_cast<uint32_t>(wgs_for(pieces))), dim3(kGatedSlopeThreads), 0, stream,
+                           static_cast<const uint4 *>(d_gate), static_cast<const uint4 *>(d_up), static_cast<const uint4 *>(d_grad_h),
+                           reinterpret_cast<uint4 *>(dg), reinterpret_cast<uint4 *>(du), pieces, static_cast<uint32_t>(activation));
+        if (!hip_ok(hipGetLastError()))
+            return NEUZIP_EHIP;
+    }
+    GatedArgs a;
+    if (d_grad_x && tokens > 0) {
+        std::memset(&a, 0, sizeof(a));
+        a.q[0] = dg;
+        a.q[1] = du;
+        a.p[0] = static_cast<const uint16_t *>(d_gate_weight);
+        a.p[1] = static_cast<const uint16_t *>(d_up_weight);
+        a.c[0] = static_cast<uint16_t *>(d_grad_x);
+        a.rows = static_cast<uint32_t>(tokens);
+        a.cols = a.c_row = a.p_row = static_cast<uint32_t>(in_features);
+        a.depth = a.q_row = static_cast<uint32_t>(out_features);
+        const GatedShape shape = gated_shape<kInputGrad>(a.rows, a.cols, a.depth);
+        a.partial = shape.slices > 1 ? partial : nullptr;
+        const int rc = launch_gated<kInputGrad>(a, shape, stream);
+        if (rc != NEUZIP_OK)
+            return rc;
+        if (shape.slices > 1) {
+            const uint64_t pieces = tokens * in_features / 8;
+            hipLaunchKernelGGL(gated_join_kernel, dim3(static_cast<uint32_t>(wgs_for(pieces))), dim3(kGatedSlopeThreads), 0, stream,
+                               reinterpret_cast<const float4 *>(partial), static_cast<uint4 *>(d_grad_x), pieces, shape.slices);
+            if (!hip_ok(hipGetLastError()))
+                return NEUZIP_EHIP;
+        }
+    }
+    if (weights) {
+        std::memset(&a, 0, sizeof(a));
+        a.q[0] = dg;
+        a.q[1] = du;
+        a.p[0] = a.p[1] = static_cast<const uint16_t *>(d_x);
+        a.c[0] = static_cast<uint16_t *>(d_grad_gate_weight);
+        a.c[1] = static_cast<uint16_t *>(d_grad_up_weight);
+        a.rows = a.q_row = static_cast<uint32_t>(out_features);
+        a.cols = a.c_row = a.p_row = static_cast<uint32_t>(in_features);
+        a.depth = static_cast<uint32_t>(tokens);
+        return launch_gated<kWeightGrad>(a, gated_shape<kWeightGrad>(a.rows, a.cols, a.depth), stream);
+    }
+    return NEUZIP_OK;
+}
+
+uint64_t neuzip_gated_linear_scratch_bytes(uint64_t out_features, uint64_t in_features, uint32_t tokens)
+{
+    const uint64_t outs[2] = {out_features, out_features};
+    return 2 * pad_to(static_cast<uint64_t>(tokens) * out_features * sizeof(float), 256) +
+           neuzip_linear_scratch_bytes(outs, 2, in_features, tokens);
+}
+
+int neuzip_gated_linear(const neuzip_blob *gate, const neuzip_blob *up, uint64_t out_features, uint64_t in_features, const void *d_x,
+                        uint32_t tokens, int activation, void *d_h, void *d_scratch, uint64_t scratch_bytes, void *hip_stream)
+{
+    if (!valid_activation(activation) || !d_h || !d_scratch || misaligned(d_scratch) || (reinterpret_cast<uintptr_t>(d_h) & 1u) ||
+        tokens == 0 || out_features == 0 || out_features >= (1ull << 31) ||
+        scratch_bytes < neuzip_gated_linear_scratch_bytes(out_features, in_features, tokens))
+        return NEUZIP_EINVAL;
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const uint64_t count = tokens * out_features, each = pad_to(count * sizeof(float), 256);
+    if (wgs_for(count) >= (1ull << 31))
+        return NEUZIP_EUNSUPPORTED;
+    float *const sums[2] = {static_cast<float *>(d_scratch), static_cast<float *>(d_scratch) + each / sizeof(float)};
+    const neuzip_blob *const weights[2] = {gate, up};
+    const uint64_t outs[2] = {out_features, out_features};
+    const int rc = neuzip_linear_batch_scratch(weights, outs, 2, in_features, d_x, tokens, nullptr, sums, sums[1] + each / sizeof(float),
+                                               scratch_bytes - 2 * each, hip_stream);
+    if (rc != NEUZIP_OK)
+        return rc;
+    hipLaunchKernelGGL(gated_product_kernel, dim3(static_cast<uint32_t>(wgs_for(count))), dim3(kGatedSlopeThreads), 0, stream, sums[0],
+                       sums[1], static_cast<uint16_t *>(d_h), count, static_cast<uint32_t>(activation));
+    return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
+}
+
+}  // extern "C"

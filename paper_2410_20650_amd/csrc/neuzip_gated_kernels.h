@@ -1,0 +1,388 @@
+// Gated feed-forward block on dense bf16 weights for gfx950:  h = act(x Wg^T) * (x Wu^T)  and its gradients, as products of
+// matrices in the matrix cores.
+//
+// One kernel serves all of them.  It computes  C[i][j] = sum over k of Q(i, k) P(j, k)  for a tile of i and j at a time, the sums
+// in binary32:
+//   kForward     C = x Wg^T and x Wu^T side by side: half of a tile's j are rows of Wg, the other half the same rows of Wu, so
+//                that a lane holds both sums of an output and leaves h (and, for the backward pass, both sums) by itself
+//   kInputGrad   dx = dg Wg + du Wu, one sum over the 2 x out_features of both
+//   kWeightGrad  dWg = dg^T x and dWu = du^T x, sums over the tokens; half of the tiles are the one's, half the other's
+// The operand that supplies i or j lies with k along its rows (x and the weights in kForward, dg and du in kInputGrad), or with k
+// down its columns (the others).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+namespace nz {
+
+enum GatedForm { kForward, kInputGrad, kWeightGrad };
+
+struct GatedArgs {
+    const uint16_t *q[2];   // kForward: x, x;  kInputGrad: dg, du;  kWeightGrad: dg, du
+    const uint16_t *p[2];   // Wg, Wu;  Wg, Wu;  x, x
+    uint16_t *c[2];         // h, -;  dx, -;  dWg, dWu
+    uint16_t *gate, *up;    // kForward: the two sums, for the backward pass (nullptr: they are not kept)
+    float *partial;         // kInputGrad, several slices: the sums of a slice leave as they are, to partial[slice][i][j]
+    uint32_t rows;          // i: tokens, tokens, out_features
+    uint32_t cols;          // j: out_features, in_features, in_features
+    uint32_t depth;         // k: in_features, out_features (of each half), tokens
+    uint32_t q_row, p_row, c_row;  // elements from one row to the next
+    uint32_t tiles_i, tiles_j;     // of one half
+    uint32_t slices;        // of k
+    uint32_t activation;
+};
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 gated_bf16x8_t;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short gated_s16x4_t;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float gated_f32x4_t;
+
+// ---- activations: act(g) = g * sigmoid(z(g)), z = g (SiLU) or 2 sqrt(2 / pi) (g + 0.044715 g^3) (GELU, tanh form)
+constexpr float kGeluScale = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+__device__ __forceinline__ float gated_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+__device__ __forceinline__ float gated_argument(float g, uint32_t activation)
+{
+    return activation ? kGeluScale * (g + 0.044715f * g * g * g) : g;
+}
+__device__ __forceinline__ float gated_value(float g, uint32_t activation)
+{
+    return g * gated_sigmoid(gated_argument(g, activation));
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2_t;
+    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
+    const f32x2_t v = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+}
+
+// 16 bytes per lane from memory straight into LDS, lane l's to `to` + 16 l.  Not the builtin: the compiler would wait for such a
+// copy in front of the next read of LDS, whichever buffer it is from.  The waits are the caller's.
+__device__ __forceinline__ void gated_copy(const uint8_t *base, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base));
+}
+__device__ __forceinline__ void gated_copy(const uint8_t *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
+}
+
+// What lanes read that have no k of their own: zeros.
+__device__ const uint4 kGatedZeros[1] = {};
+
+// ---- one operand's tile in LDS: R values of i (or j) by 64 of k, R * 128 bytes.
+// Along k: a row of the tile is 64 k, 128 bytes, 8 pieces of 16 bytes, piece p of row r in place p ^ (r / 2 % 8).
+// Across k: a row is one k and its R values, in units of 16 values; unit u of row k in place u ^ f(k), f = k % 4 + 4 * (k / 8 % 2):
+// the eight rows that half a wave reads a unit of at a time then lie in different banks.
+constexpr uint32_t kGatedDepth = 64;
+template <int R, int WAVES, bool ALONG>
+struct GatedOperand {
+    static constexpr uint32_t kBytes = R * 128;
+    static constexpr uint32_t kCopies = R / 8 / WAVES;  // a wave's, 1 KB each
+    static constexpr uint32_t kPieces = R / 8;          // ACROSS: of a row
+    uint32_t offset[kCopies];  // of the lane's piece in the tile's first step
+    uint32_t k_of;             // ALONG: the k of copy 0 and (its row's parity is the same in all) of all copies; ACROSS: of copy 0
+
+    // row: first i; rows: how many there are from there on (values behind them are read from the last one: nobody looks at the
+    // sums).  swap_half > 0: values from swap_half on are rows of the other matrix (kForward), `apart` bytes away.
+    __device__ __forceinline__ void set_up(uint32_t wave, uint32_t lane, uint32_t left, uint32_t row_elems)
+    {
+#pragma unroll
+        for (uint32_t n = 0; n < kCopies; ++n) {
+            const uint32_t copy = n * WAVES + wave;
+            if constexpr (ALONG) {
+                uint32_t r = copy * 8 + lane / 8;
+                const uint32_t piece = (lane % 8) ^ (r / 2 % 8);
+                r = r < left ? r : left - 1;
+                offset[n] = (r * row_elems + piece * 8) * 2;
+                if (n == 0)
+                    k_of = piece * 8;
+            } else {
+                const uint32_t k = copy * (64 / kPieces) + lane / kPieces;
+                const uint32_t f = k % 4 + k / 8 % 2 * 4;
+                uint32_t piece = (((lane % kPieces) / 2) ^ f) * 2 + lane % 2;
+                piece = piece * 8 < left ? piece : 0u;
+                offset[n] = (k * row_elems + piece * 8) * 2;
+                if (n == 0)
+                    k_of = k;
+            }
+        }
+    }
+    // k of copy n
+    __device__ __forceinline__ uint32_t k_at(uint32_t n) const
+    {
+        return ALONG ? k_of : k_of + n * (WAVES * 64 / kPieces);
+    }
+    // requests the tile that begins at `from`, `depth` k of it (64, or fewer in the last step)
+    __device__ __forceinline__ void request(const uint8_t *from, uint32_t to, uint32_t wave, uint32_t depth) const
+    {
+        if (depth >= kGatedDepth) {
+#pragma unroll
+            for (uint32_t n = 0; n < kCopies; ++n)
+                gated_copy(from, offset[n], to + (n * WAVES + wave) * 1024);
+        } else {
+#pragma unroll
+            for (uint32_t n = 0; n < kCopies; ++n)
+                gated_copy(k_at(n) < depth ? from + offset[n] : reinterpret_cast<const uint8_t *>(kGatedZeros), to + (n * WAVES + wave) * 1024);
+        }
+    }
+    // the lane's address of the operand's first 16 values (first: their number in the tile), for read()
+    static __device__ __forceinline__ uint32_t lane_address(uint32_t first, uint32_t lane)
+    {
+        if constexpr (ALONG) {
+            const uint32_t r = first + lane % 16;
+            return r * 128 + (((lane / 16) ^ (lane % 16 / 2)) * 16);
+        } else {
+            const uint32_t i = lane % 16, g = lane / 16, f = i / 4 + (g % 2) * 4;
+            return (8 * g + i / 4) * (R * 2) + ((first / 16) ^ f) * 32 + i % 4 * 8;
+        }
+    }
+    // 16 values (the tile's `which`th from the first) by the 32 k of half `half`: lane l value l % 16, k = 8 * (l / 16) .. + 7
+    static __device__ __forceinline__ gated_bf16x8_t read(const uint8_t *tile, uint32_t address, uint32_t which, uint32_t half)
+    {
+        if constexpr (ALONG) {
+            return *reinterpret_cast<const gated_bf16x8_t *>(tile + (address ^ (half * 64)) + which * 2048);
+        } else {
+            typedef __attribute__((address_space(3))) gated_s16x4_t lds_s16x4_t;
+            const uint8_t *at = tile + (address ^ (which * 32)) + half * 32 * (R * 2);
+            union {
+                gated_s16x4_t s[2];
+                gated_bf16x8_t v;
+            } u;
+            u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(at));
+            u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(at + 4 * (R * 2)));
+            return u.v;
+        }
+    }
+};
+
+// Launch shape: tiles of SIZE i by SIZE j, waves of 64 i by SIZE / 2 j (256: eight waves, two to a SIMD; 128: four).
+template <int SIZE>
+constexpr uint32_t kGatedWaves = SIZE / 64 * 2;
+
+template <GatedForm FORM, int SIZE>
+__global__ __launch_bounds__(kGatedWaves<SIZE> * 64, 2) void gated_kernel(const GatedArgs a)
+{
+    constexpr int WAVES = kGatedWaves<SIZE>;
+    constexpr bool Q_ALONG = FORM != kWeightGrad, P_ALONG = FORM == kForward;
+    constexpr int JT = SIZE / 2 / 16, IT = 4;  // 16 x 16 sums of a wave
+    typedef GatedOperand<SIZE, WAVES, Q_ALONG> Q;
+    typedef GatedOperand<SIZE, WAVES, P_ALONG> P;
+    constexpr uint32_t kStage = Q::kBytes + P::kBytes;
+    __shared__ __align__(16) uint8_t lds[2 * kStage];
+
+    const uint32_t lane = threadIdx.x % 64;
+    const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / 64)));
+    // Which tile.  Workgroups go to the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, and in it columns of 8 tiles of
+    // i, so that what its L2 holds of both operands is used again.
+    const uint32_t all = gridDim.x, per = all / 8, more = all % 8, xcd = blockIdx.x % 8;
+    uint32_t tile = xcd * per + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t per_slice = a.tiles_i * a.tiles_j * (FORM == kWeightGrad ? 2 : 1);
+    const uint32_t slice = tile / per_slice;
+    tile -= slice * per_slice;
+    const uint32_t half = FORM == kWeightGrad ? tile / (a.tiles_i * a.tiles_j) : 0u;
+    tile -= half * (a.tiles_i * a.tiles_j);
+    constexpr uint32_t kBand = 8;
+    const uint32_t band = tile / (kBand * a.tiles_j), in_band = tile - band * (kBand * a.tiles_j);
+    const uint32_t band_rows = a.tiles_i - band * kBand < kBand ? a.tiles_i - band * kBand : kBand;
+    const uint32_t ti = band * kBand + in_band % band_rows, tj = in_band / band_rows;
+    // kForward: a tile's j are SIZE / 2 outputs, of both weights
+    constexpr uint32_t kTileJ = FORM == kForward ? SIZE / 2 : SIZE;
+    const uint32_t i0 = ti * SIZE, j0 = tj * kTileJ;
+
+    // ---- what this wave copies
+    Q q;
+    P p;
+    q.set_up(wave, lane, a.rows - i0, a.q_row);
+    const uint8_t *q_base[2], *p_base[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        q_base[h] = reinterpret_cast<const uint8_t *>(a.q[h]) + static_cast<uint64_t>(i0) * (Q_ALONG ? a.q_row : 1u) * 2;
+        p_base[h] = reinterpret_cast<const uint8_t *>(a.p[h]) + static_cast<uint64_t>(j0) * (P_ALONG ? a.p_row : 1u) * 2;
+    }
+    // kForward: j of the tile: the waves of column w / 4 .. take JT / 2 x 16 rows of Wg, then as many of Wu.  A copy is 8 rows, all
+    // of one weight.
+    GatedOperand<SIZE / 2, WAVES, true> pf;  // (rows of one weight: half as many)
+    if constexpr (FORM == kForward)
+        pf.set_up(wave, lane, a.cols - j0, a.p_row);
+    else
+        p.set_up(wave, lane, a.cols - j0, a.p_row);
+
+    const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds));
+
+    // steps of 64 k: all of one half, then (kInputGrad) all of the other
+    const uint32_t half_steps = (a.depth + kGatedDepth - 1) / kGatedDepth;
+    const uint32_t steps_all = FORM == kInputGrad ? 2 * half_steps : half_steps;
+    const uint32_t s_begin = static_cast<uint32_t>(static_cast<uint64_t>(steps_all) * slice / a.slices);
+    const uint32_t s_end = static_cast<uint32_t>(static_cast<uint64_t>(steps_all) * (slice + 1) / a.slices);
+    auto request = [&](uint32_t s, uint32_t buffer) {
+        uint32_t h = FORM == kWeightGrad ? half : 0u, in_half = s;
+        if constexpr (FORM == kInputGrad) {
+            if (s >= half_steps) {
+                h = 1;
+                in_half = s - half_steps;
+            }
+        }
+        const uint32_t k0 = in_half * kGatedDepth, depth = a.depth - k0;
+        const uint32_t to = lds_at + buffer * kStage;
+        q.request((h ? q_base[1] : q_base[0]) + static_cast<uint64_t>(k0) * (Q_ALONG ? 1u : a.q_row) * 2, to, wave, depth);
+        if constexpr (FORM == kForward) {
+            pf.request(p_base[0] + static_cast<uint64_t>(k0) * 2, to + Q::kBytes, wave, depth);
+            pf.request(p_base[1] + static_cast<uint64_t>(k0) * 2, to + Q::kBytes + P::kBytes / 2, wave, depth);
+        } else {
+            p.request((h ? p_base[1] : p_base[0]) + static_cast<uint64_t>(k0) * (P_ALONG ? 1u : a.p_row) * 2, to + Q::kBytes, wave, depth);
+        }
+    };
+
+    // ---- what this wave multiplies: 64 i, SIZE / 2 j (kForward: SIZE / 4 outputs of both weights)
+    const uint32_t wi = wave % (SIZE / 64), wj = wave / (SIZE / 64);
+    const uint32_t q_lane = Q::lane_address(wi * 64, lane);
+    const uint32_t p_lane = P::lane_address(FORM == kForward ? wj * (SIZE / 4) : wj * (SIZE / 2), lane);
+    gated_f32x4_t acc[JT][IT];
+#pragma unroll
+    for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+        for (int it = 0; it < IT; ++it)
+            acc[jt][it] = gated_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    if (s_begin < s_end)
+        request(s_begin, 0);
+    for (uint32_t s = s_begin; s < s_end; ++s) {
+        // what was requested for this step has come, and everyone has read the other buffer
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::"v"(lds) : "memory");
+        const uint32_t buffer = (s - s_begin) & 1u;
+        if (s + 1 < s_end)
+            request(s + 1, buffer ^ 1u);
+        const uint8_t *tq = lds + buffer * kStage, *tp = tq + Q::kBytes;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+            gated_bf16x8_t fq[IT], fp[JT];
+#pragma unroll
+            for (int it = 0; it < IT; ++it)
+                fq[it] = Q::read(tq, q_lane, it, h);
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt) {
+                // (kForward: the second half of the sums are the other weight's)
+                if constexpr (FORM == kForward)
+                    fp[jt] = P::read(tp + (jt >= JT / 2 ? P::kBytes / 2 : 0), p_lane, jt % (JT / 2), h);
+                else
+                    fp[jt] = P::read(tp, p_lane, jt, h);
+            }
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+                for (int it = 0; it < IT; ++it)
+                    acc[jt][it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[jt], fq[it], acc[jt][it], 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
+        }
+    }
+
+    // ---- a lane holds, of every 16 x 16 sums, i = lane % 16 and four neighbouring j from 4 * (lane / 16) on
+    const uint32_t quad = lane / 16 * 4;
+#pragma unroll
+    for (int it = 0; it < IT; ++it) {
+        const uint32_t i = i0 + wi * 64 + it * 16 + lane % 16;
+        if (i >= a.rows)
+            continue;
+        if constexpr (FORM == kForward) {
+#pragma unroll
+            for (int jt = 0; jt < JT / 2; ++jt) {
+                const uint32_t j = j0 + wj * (SIZE / 4) + jt * 16 + quad;
+                if (j >= a.cols)
+                    continue;
+                const gated_f32x4_t g = acc[jt][it], u = acc[jt + JT / 2][it];
+                const uint64_t at = static_cast<uint64_t>(i) * a.c_row + j;
+                uint2 v;
+                v.x = pack_bf16(gated_value(g[0], a.activation) * u[0], gated_value(g[1], a.activation) * u[1]);
+                v.y = pack_bf16(gated_value(g[2], a.activation) * u[2], gated_value(g[3], a.activation) * u[3]);
+                *reinterpret_cast<uint2 *>(a.c[0] + at) = v;
+                if (a.gate) {
+                    *reinterpret_cast<uint2 *>(a.gate + at) = make_uint2(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]));
+                    *reinterpret_cast<uint2 *>(a.up + at) = make_uint2(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt) {
+                const uint32_t j = j0 + wj * (SIZE / 2) + jt * 16 + quad;
+                if (j >= a.cols)
+                    continue;
+                const gated_f32x4_t v = acc[jt][it];
+                const uint64_t at = static_cast<uint64_t>(i) * a.c_row + j;
+                if (FORM == kInputGrad && a.partial) {
+                    *reinterpret_cast<gated_f32x4_t *>(a.partial + static_cast<uint64_t>(slice) * a.rows * a.c_row + at) = v;
+                    continue;
+                }
+                *reinterpret_cast<uint2 *>((half ? a.c[1] : a.c[0]) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            }
+        }
+    }
+}
+
+// dg = dh * u * act'(g), du = dh * act(g), each rounded to bf16 once, 8 elements to a thread.
+// act'(g) = s + g s (1 - s) z'(g), s = sigmoid(z(g)); z' of the GELU grows with g^2, where s (1 - s) has long been zero.
+constexpr uint32_t kGatedSlopeThreads = 256;
+__global__ __launch_bounds__(kGatedSlopeThreads) void gated_slope_kernel(const uint4 *__restrict__ gate, const uint4 *__restrict__ up,
+                                                                         const uint4 *__restrict__ grad_h, uint4 *__restrict__ dg,
+                                                                         uint4 *__restrict__ du, uint64_t pieces, uint32_t activation)
+{
+    const uint64_t at = static_cast<uint64_t>(blockIdx.x) * kGatedSlopeThreads + threadIdx.x;
+    if (at >= pieces)
+        return;
+    const uint4 g4 = gate[at], u4 = up[at], h4 = grad_h[at];
+    const uint32_t gs[4] = {g4.x, g4.y, g4.z, g4.w}, us[4] = {u4.x, u4.y, u4.z, u4.w}, hs[4] = {h4.x, h4.y, h4.z, h4.w};
+    uint32_t dgs[4], dus[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float dgv[2], duv[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float g = __uint_as_float(e ? gs[i] & 0xFFFF0000u : gs[i] << 16);
+            const float u = __uint_as_float(e ? us[i] & 0xFFFF0000u : us[i] << 16);
+            const float h = __uint_as_float(e ? hs[i] & 0xFFFF0000u : hs[i] << 16);
+            const float s = gated_sigmoid(gated_argument(g, activation));
+            const float slope = activation ? kGeluScale * (1.0f + 0.134145f * fminf(g * g, 1e4f)) : 1.0f;
+            dgv[e] = h * u * (s + g * (s * (1.0f - s)) * slope);
+            duv[e] = h * (g * s);
+        }
+        dgs[i] = pack_bf16(dgv[0], dgv[1]);
+        dus[i] = pack_bf16(duv[0], duv[1]);
+    }
+    dg[at] = make_uint4(dgs[0], dgs[1], dgs[2], dgs[3]);
+    du[at] = make_uint4(dus[0], dus[1], dus[2], dus[3]);
+}
+
+// dx from the sums of the slices of k, in their order, 8 elements to a thread.
+__global__ __launch_bounds__(kGatedSlopeThreads) void gated_join_kernel(const float4 *__restrict__ partial, uint4 *__restrict__ out,
+                                                                        uint64_t pieces, uint32_t slices)
+{
+    const uint64_t at = static_cast<uint64_t>(blockIdx.x) * kGatedSlopeThreads + threadIdx.x;
+    if (at >= pieces)
+        return;
+    float4 a = partial[2 * at], b = partial[2 * at + 1];
+    for (uint32_t s = 1; s < slices; ++s) {
+        const float4 c = partial[2 * (s * pieces + at)], d = partial[2 * (s * pieces + at) + 1];
+        a.x += c.x;
+        a.y += c.y;
+        a.z += c.z;
+        a.w += c.w;
+        b.x += d.x;
+        b.y += d.y;
+        b.z += d.z;
+        b.w += d.w;
+    }
+    out[at] = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+}
+
+// h from the two sums in binary32, as the compressed weights' product leaves them (serving).
+__global__ __launch_bounds__(kGatedSlopeThreads) void gated_product_kernel(const float *__restrict__ gate, const float *__restrict__ up,
+                                                                           uint16_t *__restrict__ h, uint64_t count, uint32_t activation)
+{
+    const uint64_t at = static_cast<uint64_t>(blockIdx.x) * kGatedSlopeThreads + threadIdx.x;
+    if (at < count)
+        h[at] = static_cast<uint16_t>(pack_bf16(gated_value(gate[at], activation) * up[at], 0.0f));
+}
+
+}  // namespace nz
