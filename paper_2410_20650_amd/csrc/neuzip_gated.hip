@@ -28,20 +28,32 @@ struct GatedShape {
     uint32_t size, slices;
 };
 
-// Tiles of 256 where there are enough of them for the CUs, else of 128; the input gradient's sum in slices where even these are few.
+// Tiles of 256 or of 128, and for the input gradient, whose tiles are few and their sums long, how many slices of k: the least of
+// what the forms are expected to take, in us.  A CU holds one workgroup of 256 or two of 128, and tiles come in rounds of as many as
+// there are places.  A step of 64 k of a tile of 256 takes 1.7 us with all CUs at work; a round of tiles of 128 0.65 of that (2048
+// tokens, 4096 -> 14336, forward: 896 tiles of 256 503 us, 3584 of 128 566; 1000 tokens 224 / 298), or 0.45 with one on a CU (333
+// tokens, 1160 -> 2808: 33.8 / 14.9).  The sums of slices are written and read again in binary32.
 template <GatedForm FORM>
 GatedShape gated_shape(uint64_t rows, uint64_t cols, uint64_t depth)
 {
-    auto tiles = [&](uint32_t size) {
-        return static_cast<uint64_t>(tiles_of(rows, size)) * tiles_of(cols, FORM == kForward ? size / 2 : size) * (FORM == kWeightGrad ? 2 : 1);
-    };
-    GatedShape s = {tiles(256) >= 256 ? 256u : 128u, 1u};
-    if (FORM == kInputGrad) {
-        const uint64_t steps = 2 * tiles_of(depth, kGatedDepth), have = tiles(s.size);
-        while (s.slices < 16 && have * s.slices * 2 <= 512 && steps / (s.slices * 2) >= 8)
-            s.slices *= 2;
+    const double steps = static_cast<double>(tiles_of(depth, kGatedDepth)) * (FORM == kInputGrad ? 2 : 1);
+    GatedShape best = {128, 1};
+    double least = 0;
+    for (uint32_t size = 128; size <= 256; size += 128) {
+        const uint64_t tiles = static_cast<uint64_t>(tiles_of(rows, size)) * tiles_of(cols, FORM == kForward ? size / 2 : size) * (FORM == kWeightGrad ? 2 : 1);
+        for (uint32_t slices = 1; slices <= (FORM == kInputGrad ? 16u : 1u) && steps >= 4.0 * slices; slices *= 2) {
+            const uint64_t all = tiles * slices;
+            const double rounds = size == 256 ? static_cast<double>((all + 255) / 256) : (all <= 256 ? 0.45 : 0.65 * static_cast<double>((all + 511) / 512));
+            double us = rounds * (1.7 * steps / slices + 5.0);
+            if (slices > 1)
+                us += 3.0 + static_cast<double>(rows) * cols * 4 * (2 * slices + 1) / 4e6;
+            if (least == 0 || us < least) {
+                least = us;
+                best = {size, slices};
+            }
+        }
     }
-    return s;
+    return best;
 }
 
 template <GatedForm FORM>
@@ -54,9 +66,9 @@ int launch_gated(GatedArgs &a, const GatedShape &shape, hipStream_t stream)
     if (grid >= (1ull << 31))
         return NEUZIP_EUNSUPPORTED;
     if (shape.size == 256)
-        hipLaunchKernelGGL((gated_kernel<FORM, 256>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedWaves<256> * 64), 0, stream, a);
+        hipLaunchKernelGGL((gated_kernel<FORM, 256>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedThreads), 0, stream, a);
     else
-        hipLaunchKernelGGL((gated_kernel<FORM, 128>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedWaves<128> * 64), 0, stream, a);
+        hipLaunchKernelGGL((gated_kernel<FORM, 128>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedThreads), 0, stream, a);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
 

@@ -13,6 +13,7 @@
 
 #include <hip/hip_runtime.h>
 #include <cstdint>
+#include <type_traits>
 
 namespace nz {
 
@@ -58,15 +59,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 }
 
 // 16 bytes per lane from memory straight into LDS, lane l's to `to` + 16 l.  Not the builtin: the compiler would wait for such a
-// copy in front of the next read of LDS, whichever buffer it is from.  The waits are the caller's.
-__device__ __forceinline__ void gated_copy(const uint8_t *base, uint32_t offset, uint32_t to)
+// copy in front of the next read of LDS, whichever buffer it is from.  The waits are the caller's.  (The place goes to M0, with
+// an instruction at least between that and the copy.)
+__device__ __forceinline__ void gated_copy_place(uint32_t to) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(to)); }
+__device__ __forceinline__ void gated_copy(const uint8_t *base, uint32_t offset)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base));
+    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base));
 }
-__device__ __forceinline__ void gated_copy(const uint8_t *from, uint32_t to)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from));
-}
+__device__ __forceinline__ void gated_copy(const uint8_t *from) { asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(from)); }
 
 // What lanes read that have no k of their own: zeros.
 __device__ const uint4 kGatedZeros[1] = {};
@@ -78,14 +78,13 @@ __device__ const uint4 kGatedZeros[1] = {};
 constexpr uint32_t kGatedDepth = 64;
 template <int R, int WAVES, bool ALONG>
 struct GatedOperand {
-    static constexpr uint32_t kBytes = R * 128;
-    static constexpr uint32_t kCopies = R / 8 / WAVES;  // a wave's, 1 KB each
-    static constexpr uint32_t kPieces = R / 8;          // ACROSS: of a row
-    uint32_t offset[kCopies];  // of the lane's piece in the tile's first step
-    uint32_t k_of;             // ALONG: the k of copy 0 and (its row's parity is the same in all) of all copies; ACROSS: of copy 0
+    static constexpr uint32_t kBytes = R * kGatedDepth * 2;
+    static constexpr uint32_t kCopies = kBytes / 1024 / WAVES;  // a wave's, 1 KB each
+    static constexpr uint32_t kPieces = R / 8;                  // ACROSS: of a row
+    uint32_t offset[kCopies];  // of the lane's pieces in the tile's first step
+    uint32_t k_of;             // ALONG: the k of the lane's piece in every copy; ACROSS: of copy 0
 
-    // row: first i; rows: how many there are from there on (values behind them are read from the last one: nobody looks at the
-    // sums).  swap_half > 0: values from swap_half on are rows of the other matrix (kForward), `apart` bytes away.
+    // left: values from the tile's first on (a lane that has none reads another's: nobody looks at the sums)
     __device__ __forceinline__ void set_up(uint32_t wave, uint32_t lane, uint32_t left, uint32_t row_elems)
     {
 #pragma unroll
@@ -96,8 +95,7 @@ struct GatedOperand {
                 const uint32_t piece = (lane % 8) ^ (r / 2 % 8);
                 r = r < left ? r : left - 1;
                 offset[n] = (r * row_elems + piece * 8) * 2;
-                if (n == 0)
-                    k_of = piece * 8;
+                k_of = piece * 8;
             } else {
                 const uint32_t k = copy * (64 / kPieces) + lane / kPieces;
                 const uint32_t f = k % 4 + k / 8 % 2 * 4;
@@ -109,43 +107,36 @@ struct GatedOperand {
             }
         }
     }
-    // k of copy n
-    __device__ __forceinline__ uint32_t k_at(uint32_t n) const
+    // requests copy n of the tile that begins at `from`.  RAGGED: only `depth` of its k are there, the others are zeros.
+    template <bool RAGGED>
+    __device__ __forceinline__ void request(uint32_t n, const uint8_t *from, uint32_t to, uint32_t wave, uint32_t depth) const
     {
-        return ALONG ? k_of : k_of + n * (WAVES * 64 / kPieces);
-    }
-    // requests the tile that begins at `from`, `depth` k of it (64, or fewer in the last step)
-    __device__ __forceinline__ void request(const uint8_t *from, uint32_t to, uint32_t wave, uint32_t depth) const
-    {
-        if (depth >= kGatedDepth) {
-#pragma unroll
-            for (uint32_t n = 0; n < kCopies; ++n)
-                gated_copy(from, offset[n], to + (n * WAVES + wave) * 1024);
+        gated_copy_place(to + (n * WAVES + wave) * 1024);
+        if constexpr (RAGGED) {
+            const uint32_t k = ALONG ? k_of : k_of + n * (WAVES * 64 / kPieces);
+            gated_copy(k < depth ? from + offset[n] : reinterpret_cast<const uint8_t *>(kGatedZeros));
         } else {
-#pragma unroll
-            for (uint32_t n = 0; n < kCopies; ++n)
-                gated_copy(k_at(n) < depth ? from + offset[n] : reinterpret_cast<const uint8_t *>(kGatedZeros), to + (n * WAVES + wave) * 1024);
+            gated_copy(from, offset[n]);
         }
     }
     // the lane's address of the operand's first 16 values (first: their number in the tile), for read()
     static __device__ __forceinline__ uint32_t lane_address(uint32_t first, uint32_t lane)
     {
         if constexpr (ALONG) {
-            const uint32_t r = first + lane % 16;
-            return r * 128 + (((lane / 16) ^ (lane % 16 / 2)) * 16);
+            return (first + lane % 16) * 128 + (((lane / 16) ^ (lane % 16 / 2)) * 16);
         } else {
             const uint32_t i = lane % 16, g = lane / 16, f = i / 4 + (g % 2) * 4;
             return (8 * g + i / 4) * (R * 2) + ((first / 16) ^ f) * 32 + i % 4 * 8;
         }
     }
-    // 16 values (the tile's `which`th from the first) by the 32 k of half `half`: lane l value l % 16, k = 8 * (l / 16) .. + 7
-    static __device__ __forceinline__ gated_bf16x8_t read(const uint8_t *tile, uint32_t address, uint32_t which, uint32_t half)
+    // 16 values (the tile's `which`th from the first) by the 32 k of half `h`: lane l value l % 16, k = 8 * (l / 16) .. + 7
+    static __device__ __forceinline__ gated_bf16x8_t read(const uint8_t *tile, uint32_t address, uint32_t which, uint32_t h)
     {
         if constexpr (ALONG) {
-            return *reinterpret_cast<const gated_bf16x8_t *>(tile + (address ^ (half * 64)) + which * 2048);
+            return *reinterpret_cast<const gated_bf16x8_t *>(tile + (address ^ (h * 64)) + which * 2048);
         } else {
             typedef __attribute__((address_space(3))) gated_s16x4_t lds_s16x4_t;
-            const uint8_t *at = tile + (address ^ (which * 32)) + half * 32 * (R * 2);
+            const uint8_t *at = tile + (address ^ (which * 32)) + h * 32 * (R * 2);
             union {
                 gated_s16x4_t s[2];
                 gated_bf16x8_t v;
@@ -157,20 +148,22 @@ struct GatedOperand {
     }
 };
 
-// Launch shape: tiles of SIZE i by SIZE j, waves of 64 i by SIZE / 2 j (256: eight waves, two to a SIMD; 128: four).
-template <int SIZE>
-constexpr uint32_t kGatedWaves = SIZE / 64 * 2;
+// Launch shape: tiles of SIZE i by SIZE j, four waves of SIZE / 2 by SIZE / 2.
+constexpr uint32_t kGatedWaves = 4, kGatedThreads = kGatedWaves * 64;
+// Steps whose operands LDS has room for.
+constexpr uint32_t kGatedRing = 2;
 
 template <GatedForm FORM, int SIZE>
-__global__ __launch_bounds__(kGatedWaves<SIZE> * 64, 2) void gated_kernel(const GatedArgs a)
+__global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kernel(const GatedArgs a)
 {
-    constexpr int WAVES = kGatedWaves<SIZE>;
+    constexpr int WAVES = kGatedWaves;
     constexpr bool Q_ALONG = FORM != kWeightGrad, P_ALONG = FORM == kForward;
-    constexpr int JT = SIZE / 2 / 16, IT = 4;  // 16 x 16 sums of a wave
+    constexpr int TILES = SIZE / 2 / 16;  // a wave has TILES x TILES sums of 16 x 16
     typedef GatedOperand<SIZE, WAVES, Q_ALONG> Q;
     typedef GatedOperand<SIZE, WAVES, P_ALONG> P;
+    typedef GatedOperand<SIZE / 2, WAVES, true> Half;  // kForward: the rows of one weight
     constexpr uint32_t kStage = Q::kBytes + P::kBytes;
-    __shared__ __align__(16) uint8_t lds[2 * kStage];
+    __shared__ __align__(16) uint8_t lds[kGatedRing * kStage];
 
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / 64)));
@@ -201,98 +194,161 @@ __global__ __launch_bounds__(kGatedWaves<SIZE> * 64, 2) void gated_kernel(const 
         q_base[h] = reinterpret_cast<const uint8_t *>(a.q[h]) + static_cast<uint64_t>(i0) * (Q_ALONG ? a.q_row : 1u) * 2;
         p_base[h] = reinterpret_cast<const uint8_t *>(a.p[h]) + static_cast<uint64_t>(j0) * (P_ALONG ? a.p_row : 1u) * 2;
     }
-    // kForward: j of the tile: the waves of column w / 4 .. take JT / 2 x 16 rows of Wg, then as many of Wu.  A copy is 8 rows, all
-    // of one weight.
-    GatedOperand<SIZE / 2, WAVES, true> pf;  // (rows of one weight: half as many)
+    Half half_p;
     if constexpr (FORM == kForward)
-        pf.set_up(wave, lane, a.cols - j0, a.p_row);
+        half_p.set_up(wave, lane, a.cols - j0, a.p_row);
     else
         p.set_up(wave, lane, a.cols - j0, a.p_row);
 
-    const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds));
-
-    // steps of 64 k: all of one half, then (kInputGrad) all of the other
+    // ---- steps of 32 k: all of one half, then (kInputGrad) all of the other
     const uint32_t half_steps = (a.depth + kGatedDepth - 1) / kGatedDepth;
     const uint32_t steps_all = FORM == kInputGrad ? 2 * half_steps : half_steps;
     const uint32_t s_begin = static_cast<uint32_t>(static_cast<uint64_t>(steps_all) * slice / a.slices);
-    const uint32_t s_end = static_cast<uint32_t>(static_cast<uint64_t>(steps_all) * (slice + 1) / a.slices);
-    auto request = [&](uint32_t s, uint32_t buffer) {
-        uint32_t h = FORM == kWeightGrad ? half : 0u, in_half = s;
-        if constexpr (FORM == kInputGrad) {
-            if (s >= half_steps) {
-                h = 1;
-                in_half = s - half_steps;
-            }
-        }
-        const uint32_t k0 = in_half * kGatedDepth, depth = a.depth - k0;
-        const uint32_t to = lds_at + buffer * kStage;
-        q.request((h ? q_base[1] : q_base[0]) + static_cast<uint64_t>(k0) * (Q_ALONG ? 1u : a.q_row) * 2, to, wave, depth);
-        if constexpr (FORM == kForward) {
-            pf.request(p_base[0] + static_cast<uint64_t>(k0) * 2, to + Q::kBytes, wave, depth);
-            pf.request(p_base[1] + static_cast<uint64_t>(k0) * 2, to + Q::kBytes + P::kBytes / 2, wave, depth);
-        } else {
-            p.request((h ? p_base[1] : p_base[0]) + static_cast<uint64_t>(k0) * (P_ALONG ? 1u : a.p_row) * 2, to + Q::kBytes, wave, depth);
-        }
+    const uint32_t steps = static_cast<uint32_t>(static_cast<uint64_t>(steps_all) * (slice + 1) / a.slices) - s_begin;
+    // what is requested next
+    const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds));
+    const uint64_t q_step = static_cast<uint64_t>(kGatedDepth) * (Q_ALONG ? 1u : a.q_row) * 2;
+    const uint64_t p_step = static_cast<uint64_t>(kGatedDepth) * (P_ALONG ? 1u : a.p_row) * 2;
+    uint32_t ahead = s_begin, left = 0;     // its number, and the k from its first on
+    const uint8_t *q_at = nullptr, *p_at = nullptr, *p_other = nullptr;
+    auto seek = [&](uint32_t s) {
+        const bool second = FORM == kInputGrad ? s >= half_steps : half != 0;
+        const uint32_t in_half = FORM == kInputGrad && second ? s - half_steps : s;
+        q_at = (second ? q_base[1] : q_base[0]) + in_half * q_step;
+        p_at = (second ? p_base[1] : p_base[0]) + in_half * p_step;
+        if constexpr (FORM == kForward)
+            p_other = p_base[1] + in_half * p_step;
+        left = a.depth - in_half * kGatedDepth;
     };
+    auto request_copy = [&](auto ragged, uint32_t n) {
+        constexpr bool RAGGED = decltype(ragged)::value;
+        const uint32_t to = lds_at + (ahead - s_begin) % kGatedRing * kStage;
+        if (n < Q::kCopies)
+            q.template request<RAGGED>(n, q_at, to, wave, left);
+        else if constexpr (FORM != kForward)
+            p.template request<RAGGED>(n - Q::kCopies, p_at, to + Q::kBytes, wave, left);
+        else if (n < Q::kCopies + Half::kCopies)
+            half_p.template request<RAGGED>(n - Q::kCopies, p_at, to + Q::kBytes, wave, left);
+        else
+            half_p.template request<RAGGED>(n - Q::kCopies - Half::kCopies, p_other, to + Q::kBytes + Half::kBytes, wave, left);
+    };
+    auto advance = [&]() {
+        ++ahead;
+        q_at += q_step;
+        p_at += p_step;
+        if constexpr (FORM == kForward)
+            p_other += p_step;
+        left -= kGatedDepth;
+        if constexpr (FORM == kInputGrad)
+            if (ahead == half_steps)
+                seek(ahead);
+    };
+    constexpr uint32_t kCopies = Q::kCopies + P::kCopies;
 
-    // ---- what this wave multiplies: 64 i, SIZE / 2 j (kForward: SIZE / 4 outputs of both weights)
-    const uint32_t wi = wave % (SIZE / 64), wj = wave / (SIZE / 64);
-    const uint32_t q_lane = Q::lane_address(wi * 64, lane);
+    // ---- what this wave multiplies
+    const uint32_t wi = wave % 2, wj = wave / 2;
+    const uint32_t q_lane = Q::lane_address(wi * (SIZE / 2), lane);
     const uint32_t p_lane = P::lane_address(FORM == kForward ? wj * (SIZE / 4) : wj * (SIZE / 2), lane);
-    gated_f32x4_t acc[JT][IT];
+    gated_f32x4_t acc[TILES][TILES];  // [j][i]
 #pragma unroll
-    for (int jt = 0; jt < JT; ++jt)
+    for (int jt = 0; jt < TILES; ++jt)
 #pragma unroll
-        for (int it = 0; it < IT; ++it)
+        for (int it = 0; it < TILES; ++it)
             acc[jt][it] = gated_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-    if (s_begin < s_end)
-        request(s_begin, 0);
-    for (uint32_t s = s_begin; s < s_end; ++s) {
-        // what was requested for this step has come, and everyone has read the other buffer
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::"v"(lds) : "memory");
-        const uint32_t buffer = (s - s_begin) & 1u;
-        if (s + 1 < s_end)
-            request(s + 1, buffer ^ 1u);
-        const uint8_t *tq = lds + buffer * kStage, *tp = tq + Q::kBytes;
+    // The operands of half a step are read into registers while the half before it is multiplied; once everyone has read the second
+    // half, the place in LDS is requested for the step after the next.
+    struct Operands {
+        gated_bf16x8_t q[TILES], p[TILES];
+    };
+    auto read_q = [&](Operands &o, const uint8_t *tile, int n, uint32_t h) { o.q[n] = Q::read(tile, q_lane, n, h); };
+    auto read_p = [&](Operands &o, const uint8_t *tile, int n, uint32_t h) {
+        // (kForward: the second half of the sums are the other weight's)
+        if constexpr (FORM == kForward)
+            o.p[n] = P::read(tile + Q::kBytes + (n >= TILES / 2 ? Half::kBytes : 0), p_lane, n % (TILES / 2), h);
+        else
+            o.p[n] = P::read(tile + Q::kBytes, p_lane, n, h);
+    };
+    static_assert(kCopies == 2 * TILES, "two copies to a row of sums");
+    auto arrive = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::"v"(lds) : "memory"); };
+    auto half_step = [&](auto requests, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
 #pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {
-            gated_bf16x8_t fq[IT], fp[JT];
+        for (int n = 0; n < TILES; ++n) {
+            // (what is not a product stands by itself between products, in their shadow)
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
-                fq[it] = Q::read(tq, q_lane, it, h);
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-                // (kForward: the second half of the sums are the other weight's)
-                if constexpr (FORM == kForward)
-                    fp[jt] = P::read(tp + (jt >= JT / 2 ? P::kBytes / 2 : 0), p_lane, jt % (JT / 2), h);
-                else
-                    fp[jt] = P::read(tp, p_lane, jt, h);
+            for (int it = 0; it < TILES; ++it) {
+                acc[n][it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.p[n], now.q[it], acc[n][it], 0, 0, 0);
+                if (it % (TILES / 4) == 0) {
+                    if (it / (TILES / 4) == 0)
+                        read_q(then, tile, n, h);
+                    if (it / (TILES / 4) == 1)
+                        read_p(then, tile, n, h);
+                    if constexpr (decltype(requests)::value) {
+                        if (it / (TILES / 4) >= 2)
+                            request_copy(std::false_type{}, 2 * n + it / (TILES / 4) - 2);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
-            __builtin_amdgcn_s_setprio(1);
+        }
+    };
+    auto request_all = [&]() {
+        if (left >= kGatedDepth) {
 #pragma unroll
-            for (int jt = 0; jt < JT; ++jt)
+            for (uint32_t n = 0; n < kCopies; ++n)
+                request_copy(std::false_type{}, n);
+        } else {
 #pragma unroll
-                for (int it = 0; it < IT; ++it)
-                    acc[jt][it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[jt], fq[it], acc[jt][it], 0, 0, 0);
-            __builtin_amdgcn_s_setprio(0);
+            for (uint32_t n = 0; n < kCopies; ++n)
+                request_copy(std::true_type{}, n);
+        }
+        advance();
+    };
+    if (steps > 0) {
+        Operands first, second;
+        seek(s_begin);
+        for (uint32_t r = 0; r < kGatedRing && r < steps; ++r)
+            request_all();
+        arrive();
+#pragma unroll
+        for (int n = 0; n < TILES; ++n) {
+            read_q(first, lds, n, 0);
+            read_p(first, lds, n, 0);
+        }
+        for (uint32_t s = 0; s < steps;) {
+            while (s + kGatedRing < steps && left >= kGatedDepth) {
+                const uint8_t *tile = lds + s % kGatedRing * kStage, *next = lds + (s + 1) % kGatedRing * kStage;
+                half_step(std::false_type{}, first, second, tile, 1);
+                arrive();
+                half_step(std::true_type{}, second, first, next, 0);
+                advance();
+                ++s;
+            }
+            // one by one: the last, and where half a sum ends
+            const uint8_t *tile = lds + s % kGatedRing * kStage, *next = lds + (s + 1) % kGatedRing * kStage;
+            half_step(std::false_type{}, first, second, tile, 1);
+            arrive();
+            if (s + kGatedRing < steps)
+                request_all();
+            half_step(std::false_type{}, second, first, next, 0);  // (behind the last step: what nobody uses)
+            ++s;
         }
     }
 
     // ---- a lane holds, of every 16 x 16 sums, i = lane % 16 and four neighbouring j from 4 * (lane / 16) on
     const uint32_t quad = lane / 16 * 4;
 #pragma unroll
-    for (int it = 0; it < IT; ++it) {
-        const uint32_t i = i0 + wi * 64 + it * 16 + lane % 16;
+    for (int it = 0; it < TILES; ++it) {
+        const uint32_t i = i0 + wi * (SIZE / 2) + it * 16 + lane % 16;
         if (i >= a.rows)
             continue;
         if constexpr (FORM == kForward) {
 #pragma unroll
-            for (int jt = 0; jt < JT / 2; ++jt) {
+            for (int jt = 0; jt < TILES / 2; ++jt) {
                 const uint32_t j = j0 + wj * (SIZE / 4) + jt * 16 + quad;
                 if (j >= a.cols)
                     continue;
-                const gated_f32x4_t g = acc[jt][it], u = acc[jt + JT / 2][it];
+                const gated_f32x4_t g = acc[jt][it], u = acc[jt + TILES / 2][it];
                 const uint64_t at = static_cast<uint64_t>(i) * a.c_row + j;
                 uint2 v;
                 v.x = pack_bf16(gated_value(g[0], a.activation) * u[0], gated_value(g[1], a.activation) * u[1]);
@@ -305,7 +361,7 @@ __global__ __launch_bounds__(kGatedWaves<SIZE> * 64, 2) void gated_kernel(const 
             }
         } else {
 #pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
+            for (int jt = 0; jt < TILES; ++jt) {
                 const uint32_t j = j0 + wj * (SIZE / 2) + jt * 16 + quad;
                 if (j >= a.cols)
                     continue;
