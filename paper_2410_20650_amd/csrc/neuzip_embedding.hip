@@ -101,7 +101,7 @@ uint64_t neuzip_embedding_grad_scratch_bytes(uint64_t count, uint64_t rows, uint
     if (!valid_table(rows, features) || count >= (1ull << 31))
         return 0;
     const uint64_t runs = (count + kSortRun - 1) / kSortRun;
-    return runs * sizeof(SortedRun) + (count > kPieceTokens ? runs * kPiecesMost * features * sizeof(float) : 0);
+    return runs * sizeof(SortedRun) + (count > kBlockTokens ? runs * kPieces * features * sizeof(float) : 0);
 }
 
 int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d_grad_out, uint64_t rows, uint64_t features, float scale,
@@ -133,13 +133,18 @@ int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d
     a.scale = scale;
     if (a.n_runs > 65535)
         return NEUZIP_EUNSUPPORTED;
+    const uint32_t most = count < kSortRun ? static_cast<uint32_t>(count) : kSortRun;  // tokens of a run
+    a.sort_wgs = count > 0 ? (most + kSortRanges + kSortQueries) / kSortQueries : 0u;
+    const uint64_t fill_wgs = (rows * a.row_pieces.by + kSortThreads - 1) / kSortThreads;
+    const uint32_t strips = (a.row_pieces.by + kGradThreads - 1) / kGradThreads;
+    if (strips > 65535)
+        return NEUZIP_EUNSUPPORTED;
+    hipLaunchKernelGGL(embedding_sort_kernel, dim3(static_cast<uint32_t>(static_cast<uint64_t>(a.sort_wgs) * a.n_runs + fill_wgs)), dim3(kSortThreads), 0,
+                       stream, a);
+    if (count > kBlockTokens)
+        hipLaunchKernelGGL(embedding_pieces_kernel, dim3(kPieces, a.n_runs, strips), dim3(kGradThreads), 0, stream, a);
     if (count > 0)
-        hipLaunchKernelGGL(embedding_sort_kernel, dim3(a.n_runs), dim3(kSortThreads), 0, stream, a);
-    if (count > kPieceTokens)
-        hipLaunchKernelGGL(embedding_pieces_kernel, dim3(kPiecesMost, a.n_runs, (a.row_pieces.by + kGradThreads - 1) / kGradThreads), dim3(kGradThreads), 0,
-                           stream, a);
-    const uint64_t pieces = rows * a.row_pieces.by, each = kGradThreads * kGradPieces;
-    hipLaunchKernelGGL(embedding_write_kernel, dim3(static_cast<uint32_t>((pieces + each - 1) / each)), dim3(kGradThreads), 0, stream, a);
+        hipLaunchKernelGGL(embedding_rows_kernel, dim3(most, a.n_runs, strips), dim3(kGradThreads), 0, stream, a);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
 

@@ -1,6 +1,8 @@
 // Embedding on a compressed table for gfx950: rows decoded by token, and the table's gradient.
 #pragma once
 
+#include <type_traits>
+
 #include "neuzip_format.h"
 #include "neuzip_walk.h"
 
@@ -211,28 +213,25 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
 // Gradient:  grad[r] = bf16(scale * sum of g[t] over the tokens t with token[t] = r, in their order), every row of the table.
 //
 // Three launches, and nothing that depends on the order in which atomics arrive.
-//   sort      the tokens in runs of 4096, each by one workgroup in LDS, by token and then position.  A run also tells where the
-//             rows of each of 2048 ranges begin in it, and lists the pieces of 64 tokens that its longer segments consist of.
-//   pieces    (more than 64 tokens) the sums of those pieces in binary32, so that a token that is very frequent is no workgroup's
-//             work alone
-//   write     a workgroup writes 16 KB of the gradient.  Two numbers per run tell whether any token belongs there; where none
-//             does, which is nearly everywhere in a large table, it writes zeros.
+//   sort      the tokens in runs of 4096, by token and then position: an element's place is the number of those that come before it,
+//             which is counted, 32 elements to a workgroup, so that a run is sorted by many CUs in one go (one workgroup with a
+//             bitonic network in LDS took 45 us for 4096 tokens).  Counted the same way: where the rows of each of 2048 ranges begin
+//             in the run.
+//   pieces    (more than 64 tokens) a row whose tokens pass the end of a block of 64 sorted places is summed block by block, in
+//             binary32, so that a token that is very frequent is no workgroup's work alone
+//   rows      a workgroup to a row with tokens, at the first of them, adds its tokens up, or its pieces, and stores it.
+// Most of the work for a large table is zeros: the first launch's other workgroups fill the gradient with them meanwhile (4096
+// tokens, 128256 x 4096: 159 us, in which the sort is done after 17; three quarters of the zeros beside the second launch gave nothing).
 // ------------------------------------------------------------------------------------------
-constexpr uint32_t kSortRun = 4096, kSortThreads = 1024, kSortRanges = 2048;
-constexpr uint32_t kPieceTokens = 64, kPiecesMost = 128;
+constexpr uint32_t kSortRun = 4096, kSortThreads = 256, kSortRanges = 2048, kSortQueries = 32;
+constexpr uint32_t kBlockTokens = 64, kBlocks = kSortRun / kBlockTokens;
+constexpr uint32_t kPieces = 2 * kBlocks;  // of a run: of a row that began before the block; of one that begins in it and passes its end
 struct SortedRun {
     uint32_t token[kSortRun];
-    uint32_t index[kSortRun];            // position of the token in the call's tokens
-    uint16_t piece_of[kSortRun];         // of the first token of a piece: its number
-    uint16_t first[kSortRanges + 8];     // the first of a range of rows; first[kSortRanges]: how many there are
-    uint16_t piece_at[kPiecesMost];
-    uint16_t piece_tokens[kPiecesMost];
-    uint32_t pieces;
-    uint32_t pad[3];
+    uint32_t index[kSortRun];         // position of the token in the call's tokens
+    uint32_t first[kSortRanges + 4];  // the first of a range of rows; first[kSortRanges]: how many there are
 };
 static_assert(sizeof(SortedRun) % 16 == 0, "runs lie side by side");
-// segments of more than 64 of 4096 tokens: at most 63, with at most 64 whole pieces and one more each
-static_assert(kSortRun / kPieceTokens + (kSortRun - 1) / (kPieceTokens + 1) <= kPiecesMost, "room for all pieces");
 
 struct EmbeddingGradArgs {
     const int64_t *tokens;
@@ -242,6 +241,7 @@ struct EmbeddingGradArgs {
     SortedRun *runs;
     float *partial;        // [run][piece][features]
     uint32_t n_runs, rows, features;
+    uint32_t sort_wgs;     // workgroups that sort a run
     uint32_t range_shift;  // rows of a range: 1 << range_shift
     Divisor row_pieces;    // features / 8
     float scale;
@@ -249,97 +249,71 @@ struct EmbeddingGradArgs {
 
 __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const EmbeddingGradArgs a)
 {
-    __shared__ uint64_t keys[kSortRun];  // row << 12 | position in the run; a token that is none counts as row `rows`
-    __shared__ uint32_t wave_sums[kSortThreads / 64];
-    const uint32_t tid = threadIdx.x;
-    const uint64_t base = static_cast<uint64_t>(blockIdx.x) * kSortRun;
+    const uint32_t sorting = a.sort_wgs * a.n_runs;
+    if (blockIdx.x >= sorting) {
+        // Zeros, 16 bytes to a thread: 1.05 GB take 155 us, with four or sixteen times as much 177 and 191.  (Fewer than 2^29 pieces.)
+        const uint32_t piece = (blockIdx.x - sorting) * kSortThreads + threadIdx.x;
+        if (piece < a.rows * a.row_pieces.by)
+            reinterpret_cast<uint4 *>(a.grad)[piece] = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const uint32_t of_run = a.sort_wgs == 0 ? 0u : blockIdx.x / a.sort_wgs, group = blockIdx.x - of_run * a.sort_wgs;
+    // Queries are the run's elements, then the ranges' first rows.  A wave's lanes hold the 32 queries twice, for two halves of
+    // the wave's quarter of the run.
+    constexpr uint32_t kParts = kSortThreads / kSortQueries;
+    __shared__ __align__(16) uint32_t rows[kSortRun];
+    __shared__ uint32_t before[kSortQueries];
+    const uint32_t tid = threadIdx.x, query = tid % kSortQueries, part = tid / kSortQueries;
+    const uint64_t base = static_cast<uint64_t>(of_run) * kSortRun;
     const uint32_t here = a.count - base < kSortRun ? static_cast<uint32_t>(a.count - base) : kSortRun;
-    SortedRun &run = a.runs[blockIdx.x];
-    uint32_t padded = 1;
-    while (padded < here)
-        padded *= 2;
+    const uint32_t padded = (here + 4 * kParts - 1) / (4 * kParts) * (4 * kParts), each = padded / kParts;
     for (uint32_t i = tid; i < padded; i += kSortThreads) {
-        uint64_t key = ~0ull;
+        uint32_t row = ~0u;  // of no row: behind them all
         if (i < here) {
             const int64_t token = a.tokens[base + i];
-            const uint64_t row = token >= 0 && token < static_cast<int64_t>(a.rows) ? static_cast<uint64_t>(token) : a.rows;
-            key = row << 12 | i;
+            row = token >= 0 && token < static_cast<int64_t>(a.rows) ? static_cast<uint32_t>(token) : ~0u;
         }
-        keys[i] = key;
+        rows[i] = row;
     }
+    if (tid < kSortQueries)
+        before[tid] = 0;
     __syncthreads();
-    // bitonic sort (keys are distinct, so its result is the stable one)
-    for (uint32_t size = 2; size <= padded; size *= 2) {
-        for (uint32_t apart = size / 2; apart > 0; apart /= 2) {
-            for (uint32_t i = tid; i < padded / 2; i += kSortThreads) {
-                const uint32_t at = 2 * i - (i & (apart - 1)), other = at + apart;
-                const uint64_t p = keys[at], q = keys[other];
-                if ((p > q) == ((at & size) == 0)) {
-                    keys[at] = q;
-                    keys[other] = p;
-                }
-            }
-            __syncthreads();
-        }
+    const uint32_t number = group * kSortQueries + query;
+    const bool is_element = number < here;
+    const uint32_t range = number - here;  // (of a query behind the elements)
+    const uint64_t range_row = static_cast<uint64_t>(range) << a.range_shift;
+    const uint32_t row = is_element ? rows[number] : (range_row < a.rows ? static_cast<uint32_t>(range_row) : a.rows);
+    // Elements in front of this one come before it if their rows are not above its own, those behind if they are below it.
+    const uint32_t not_above = is_element ? (row == ~0u ? row : row + 1) : row;
+    const uint32_t p0 = group * kSortQueries;
+    uint32_t count = 0;
+#pragma unroll 4
+    for (uint32_t j = part * each; j < (part + 1) * each; j += 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(rows + j);
+        const uint32_t limit = j < p0 ? not_above : row;
+        count += v.x < limit;
+        count += v.y < limit;
+        count += v.z < limit;
+        count += v.w < limit;
     }
-    // the first key that is not below `key`
-    auto lower = [&](uint64_t key) {
-        uint32_t low = 0, high = here;
-        while (low < high) {
-            const uint32_t mid = (low + high) / 2;
-            if (keys[mid] < key)
-                low = mid + 1;
-            else
-                high = mid;
-        }
-        return low;
-    };
-    const uint32_t valid = lower(static_cast<uint64_t>(a.rows) << 12);
-    for (uint32_t i = tid; i < valid; i += kSortThreads) {
-        run.token[i] = static_cast<uint32_t>(keys[i] >> 12);
-        run.index[i] = static_cast<uint32_t>(base) + (static_cast<uint32_t>(keys[i]) & (kSortRun - 1));
-    }
-    for (uint32_t i = tid; i <= kSortRanges; i += kSortThreads) {
-        const uint64_t row = static_cast<uint64_t>(i) << a.range_shift;
-        run.first[i] = static_cast<uint16_t>(row >= a.rows ? valid : lower(row << 12));
-    }
-    // ---- pieces of the longer segments: four neighbouring places to a thread
-    uint32_t starts = 0, lens[4] = {0, 0, 0, 0};
-    if (valid > kPieceTokens) {
-#pragma unroll
-        for (uint32_t k = 0; k < 4; ++k) {
-            const uint32_t i = tid * 4 + k;
-            if (i >= valid)
-                break;
-            const uint64_t row = keys[i] >> 12;
-            const uint32_t low = lower(row << 12);
-            if ((i - low) % kPieceTokens == 0 && low + kPieceTokens < valid && keys[low + kPieceTokens] >> 12 == row) {
-                const uint32_t end = lower((row + 1) << 12);
-                lens[k] = end - i < kPieceTokens ? end - i : kPieceTokens;
-                ++starts;
-            }
-        }
-    }
-    const uint32_t upto = wave_scan_u32(starts, 0u, OpAdd{});
-    if (tid % 64 == 63)
-        wave_sums[tid / 64] = upto;
+    // ... of the workgroup's own, those in front (the equal ones have not been counted)
+    if (part == 0 && is_element)
+        for (uint32_t j = p0; j < number; ++j)
+            count += rows[j] == row;
+    atomicAdd(&before[query], count);
     __syncthreads();
-    uint32_t number = upto - starts, total = 0;
-    for (uint32_t w = 0; w < kSortThreads / 64; ++w) {
-        number += w < tid / 64 ? wave_sums[w] : 0u;
-        total += wave_sums[w];
-    }
-#pragma unroll
-    for (uint32_t k = 0; k < 4; ++k)
-        if (lens[k]) {
-            const uint32_t i = tid * 4 + k;
-            run.piece_of[i] = static_cast<uint16_t>(number);
-            run.piece_at[number] = static_cast<uint16_t>(i);
-            run.piece_tokens[number] = static_cast<uint16_t>(lens[k]);
-            ++number;
+    if (tid >= kSortQueries)
+        return;
+    SortedRun &run = a.runs[of_run];
+    const uint32_t place = before[tid];
+    if (is_element) {
+        if (row != ~0u) {
+            run.token[place] = row;
+            run.index[place] = static_cast<uint32_t>(base) + number;
         }
-    if (tid == 0)
-        run.pieces = total;
+    } else if (range <= kSortRanges) {
+        run.first[range] = place;
+    }
 }
 
 // eight neighbouring elements added to their sums
@@ -353,104 +327,157 @@ __device__ __forceinline__ void add_eight(float (&sum)[8], const uint4 &v)
     }
 }
 
-// The rows of grad_out that sorted places at .. at + count - 1 name, in that order; eight requested at a time.
+// The rows of grad_out that sorted places at .. at + count - 1 name, in that order, sixteen requested at a time (count is the same for
+// the workgroup).
+constexpr uint32_t kGradThreads = 256;
 __device__ __forceinline__ void add_rows(float (&sum)[8], const uint32_t *__restrict__ index, uint32_t count,
                                          const uint4 *__restrict__ grad_out, uint32_t row_pieces, uint32_t piece)
 {
-    constexpr uint32_t kTogether = 8;
-    for (uint32_t s = 0; s < count; s += kTogether) {
-        uint4 v[kTogether];
+    auto take = [&](auto rows, uint32_t s) {
+        constexpr uint32_t N = decltype(rows)::value;
+        uint4 v[N];
 #pragma unroll
-        for (uint32_t r = 0; r < kTogether; ++r)
-            v[r] = grad_out[static_cast<uint64_t>(index[s + r < count ? s + r : s]) * row_pieces + piece];
+        for (uint32_t r = 0; r < N; ++r)
+            v[r] = grad_out[static_cast<uint64_t>(index[s + r]) * row_pieces + piece];
 #pragma unroll
-        for (uint32_t r = 0; r < kTogether; ++r)
-            if (s + r < count)
-                add_eight(sum, v[r]);
-    }
+        for (uint32_t r = 0; r < N; ++r)
+            add_eight(sum, v[r]);
+    };
+    uint32_t s = 0;
+    for (; s + 16 <= count; s += 16)
+        take(std::integral_constant<uint32_t, 16>{}, s);
+    for (; s + 4 <= count; s += 4)
+        take(std::integral_constant<uint32_t, 4>{}, s);
+    for (; s < count; ++s)
+        take(std::integral_constant<uint32_t, 1>{}, s);
 }
 
-constexpr uint32_t kGradThreads = 256;
 __global__ __launch_bounds__(kGradThreads) void embedding_pieces_kernel(const EmbeddingGradArgs a)
 {
     const SortedRun &run = a.runs[blockIdx.y];
-    const uint32_t number = blockIdx.x;
-    if (number >= run.pieces)
+    const uint32_t begin = blockIdx.x / 2 * kBlockTokens, valid = run.first[kSortRanges], lane = threadIdx.x % 64;
+    const bool begins_here = blockIdx.x % 2;
+    if (begin >= valid)
         return;
+    const uint32_t end = min(begin + kBlockTokens, valid);
+    const uint32_t before = begin > 0 ? run.token[begin - 1] : ~0u, behind = end < valid ? run.token[end] : ~0u;
+    const uint32_t token = begin + lane < end ? run.token[begin + lane] : ~0u;
+    // the row that began before the block, or the one that passes its end and is another
+    const uint32_t row = begins_here ? behind : before;
+    const uint64_t mine = __ballot(token == row && row != ~0u && (!begins_here || row != before));
+    if (!mine)
+        return;
+    const uint32_t from = begin + static_cast<uint32_t>(__builtin_ctzll(mine)), count = static_cast<uint32_t>(__builtin_popcountll(mine));
     const uint32_t piece = blockIdx.z * kGradThreads + threadIdx.x;
     if (piece >= a.row_pieces.by)
         return;
     float sum[8] = {};
-    add_rows(sum, run.index + run.piece_at[number], run.piece_tokens[number], reinterpret_cast<const uint4 *>(a.grad_out), a.row_pieces.by, piece);
-    float4 *to = reinterpret_cast<float4 *>(a.partial + (static_cast<uint64_t>(blockIdx.y) * kPiecesMost + number) * a.features) + 2 * piece;
+    add_rows(sum, run.index + from, count, reinterpret_cast<const uint4 *>(a.grad_out), a.row_pieces.by, piece);
+    float4 *to = reinterpret_cast<float4 *>(a.partial + (static_cast<uint64_t>(blockIdx.y) * kPieces + blockIdx.x) * a.features) + 2 * piece;
     to[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
     to[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
 }
 
-constexpr uint32_t kGradPieces = 4;  // of 16 bytes, a thread's
-__global__ __launch_bounds__(kGradThreads) void embedding_write_kernel(const EmbeddingGradArgs a)
+// run.token[...] of a row: the places from .. upto - 1
+__device__ __forceinline__ void places_of(const SortedRun &run, uint32_t row, uint32_t range_shift, uint32_t &from, uint32_t &upto)
 {
-    // (pieces of the table: fewer than 2^29)
-    const uint32_t all = a.rows * a.row_pieces.by, from = blockIdx.x * (kGradThreads * kGradPieces);
-    const uint32_t last = min(from + kGradThreads * kGradPieces, all) - 1;
-    const uint32_t range0 = a.row_pieces.quotient(from) >> a.range_shift, range1 = (a.row_pieces.quotient(last) >> a.range_shift) + 1;
-    uint4 *grad = reinterpret_cast<uint4 *>(a.grad);
-    bool any = false;
-    for (uint32_t r = 0; r < a.n_runs && !any; ++r)
-        any = a.runs[r].first[range0] < a.runs[r].first[range1];
-    if (!any) {
-#pragma unroll
-        for (uint32_t k = 0; k < kGradPieces; ++k)
-            if (from + k * kGradThreads + threadIdx.x < all)
-                grad[from + k * kGradThreads + threadIdx.x] = make_uint4(0, 0, 0, 0);
-        return;
+    uint32_t low = run.first[row >> range_shift], high = run.first[(row >> range_shift) + 1];
+    const uint32_t end = high;
+    while (low < high) {
+        const uint32_t mid = (low + high) / 2;
+        if (run.token[mid] < row)
+            low = mid + 1;
+        else
+            high = mid;
     }
-    for (uint32_t k = 0; k < kGradPieces; ++k) {
-        const uint32_t at = from + k * kGradThreads + threadIdx.x;
-        if (at >= all)
+    from = low;
+    high = end;
+    while (low < high) {
+        const uint32_t mid = (low + high) / 2;
+        if (run.token[mid] <= row)
+            low = mid + 1;
+        else
+            high = mid;
+    }
+    upto = low;
+}
+
+__global__ __launch_bounds__(kGradThreads) void embedding_rows_kernel(const EmbeddingGradArgs a)
+{
+    const uint32_t own = blockIdx.y, place = blockIdx.x, lane = threadIdx.x % 64;
+    const SortedRun &run = a.runs[own];
+    const uint32_t valid = run.first[kSortRanges];
+    if (place >= valid)
+        return;
+    const uint32_t row = run.token[place];
+    if (place > 0 && run.token[place - 1] == row)
+        return;
+    // the row's places in its own run: as many as follow the first without a gap, ...
+    const uint32_t block = place / kBlockTokens, block_end = (block + 1) * kBlockTokens;
+    const uint32_t next = place + 1 + lane < valid ? run.token[place + 1 + lane] : ~0u;
+    const uint32_t corner = block_end + lane * kBlockTokens < valid ? run.token[block_end + lane * kBlockTokens] : ~0u;
+    const uint64_t others = ~__ballot(next == row), others_far = ~__ballot(corner == row);
+    const uint32_t follow = others ? static_cast<uint32_t>(__builtin_ctzll(others)) : 64u;
+    // ... or the blocks whose ends it passes
+    const uint32_t passes = others_far ? static_cast<uint32_t>(__builtin_ctzll(others_far)) : 64u;
+    // a row that a run before this one has is that one's
+    for (uint32_t r0 = 0; r0 < own; r0 += 64) {
+        uint32_t from = 0, upto = 0;
+        if (r0 + lane < own)
+            places_of(a.runs[r0 + lane], row, a.range_shift, from, upto);
+        if (__ballot(from < upto))
             return;
-        const uint32_t row = a.row_pieces.quotient(at), piece = at - row * a.row_pieces.by;
-        float sum[8] = {};
-        for (uint32_t r = 0; r < a.n_runs; ++r) {
-            const SortedRun &run = a.runs[r];
-            uint32_t low = run.first[row >> a.range_shift], high = run.first[(row >> a.range_shift) + 1];
-            const uint32_t end = high;
-            while (low < high) {
-                const uint32_t mid = (low + high) / 2;
-                if (run.token[mid] < row)
-                    low = mid + 1;
+    }
+    const uint32_t piece = blockIdx.z * kGradThreads + threadIdx.x;
+    const bool live = piece < a.row_pieces.by;
+    const uint4 *grad_out = reinterpret_cast<const uint4 *>(a.grad_out);
+    float sum[8] = {};
+    // the sums of the pieces that the places from `from` on are in, in order
+    auto add_pieces = [&](uint32_t r, uint32_t from, uint32_t ends) {
+        for (uint32_t k = 0; k <= ends; ++k) {
+            const uint32_t number = 2 * (from / kBlockTokens + k) + (k == 0 ? 1 : 0);
+            const float4 *v = reinterpret_cast<const float4 *>(a.partial + (static_cast<uint64_t>(r) * kPieces + number) * a.features) + 2 * piece;
+            const float4 p = v[0], q = v[1];
+            sum[0] += p.x;
+            sum[1] += p.y;
+            sum[2] += p.z;
+            sum[3] += p.w;
+            sum[4] += q.x;
+            sum[5] += q.y;
+            sum[6] += q.z;
+            sum[7] += q.w;
+        }
+    };
+    if (live) {
+        if (passes)
+            add_pieces(own, place, passes);
+        else
+            add_rows(sum, run.index + place, 1 + follow, grad_out, a.row_pieces.by, piece);
+    }
+    // ... and in the runs behind it, a run to a lane
+    for (uint32_t r0 = own + 1; r0 < a.n_runs; r0 += 64) {
+        uint32_t from = 0, upto = 0;
+        if (r0 + lane < a.n_runs)
+            places_of(a.runs[r0 + lane], row, a.range_shift, from, upto);
+        for (uint64_t left = __ballot(from < upto); left; left &= left - 1) {
+            const int l = __builtin_ctzll(left);
+            const uint32_t begin = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(from), l));
+            const uint32_t end = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(upto), l));
+            const uint32_t ends = (end - 1) / kBlockTokens - begin / kBlockTokens;
+            if (live) {
+                if (ends)
+                    add_pieces(r0 + l, begin, ends);
                 else
-                    high = mid;
-            }
-            uint32_t upto = low;
-            if (low + kPieceTokens < end && run.token[low + kPieceTokens] == row) {
-                // a longer segment: its pieces, in order
-                for (uint32_t number = run.piece_of[low];; ++number) {
-                    const float4 *v = reinterpret_cast<const float4 *>(a.partial + (static_cast<uint64_t>(r) * kPiecesMost + number) * a.features) + 2 * piece;
-                    const float4 p = v[0], q = v[1];
-                    sum[0] += p.x;
-                    sum[1] += p.y;
-                    sum[2] += p.z;
-                    sum[3] += p.w;
-                    sum[4] += q.x;
-                    sum[5] += q.y;
-                    sum[6] += q.z;
-                    sum[7] += q.w;
-                    if (run.piece_tokens[number] < kPieceTokens || upto + kPieceTokens >= end || run.token[upto + kPieceTokens] != row)
-                        break;
-                    upto += kPieceTokens;
-                }
-            } else {
-                while (upto < end && run.token[upto] == row)
-                    ++upto;
-                add_rows(sum, run.index + low, upto - low, reinterpret_cast<const uint4 *>(a.grad_out), a.row_pieces.by, piece);
+                    add_rows(sum, a.runs[r0 + l].index + begin, end - begin, grad_out, a.row_pieces.by, piece);
             }
         }
+    }
+    if (live) {
         uint32_t d[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p)
             d[p] = bf16_of(sum[2 * p] * a.scale) | (bf16_of(sum[2 * p + 1] * a.scale) << 16);
-        grad[at] = make_uint4(d[0], d[1], d[2], d[3]);
+        reinterpret_cast<uint4 *>(a.grad)[static_cast<uint64_t>(row) * a.row_pieces.by + piece] = make_uint4(d[0], d[1], d[2], d[3]);
     }
 }
 
