@@ -40,41 +40,44 @@ struct EmbeddingArgs {
 constexpr uint32_t kEmbWindow = 7680;  // bytes of LDS for the words of a wave's four chunks
 constexpr uint32_t kEmbAhead = 4;      // turns whose fields are requested together
 
-template <int KB, bool LONE, bool NORM, bool EAGER, class WordSrc>
+// WHOLE: every unit of the wave is a whole chunk (or half of one), and all of it belongs to the row; turns is the same for all.
+template <int KB, bool LONE, bool NORM, bool EAGER, bool WHOLE, class WordSrc>
 __device__ __forceinline__ void embedding_walk(const uint32_t *__restrict__ lut, const WordSrc &src, uint32_t lone, uint32_t &x,
                                                uint32_t &wp, const EmbeddingArgs &a, uint32_t from, uint32_t lo, uint32_t hi,
                                                uint32_t turns, uint32_t most_turns, uint16_t *__restrict__ out)
 {
-    // this lane's runs begin at from, from + 128, ...; those inside lo .. hi - 1 belong to the row, which begins at out
+    // this lane's runs begin at from, from + 128, ...; those inside lo .. hi - 1 belong to the row, whose part here goes to out
     uint32_t next = LONE ? 0u : src.peek(wp);
     auto request = [&](uint32_t q) {
         const uint32_t at = from + q * kTurn;
-        const uint32_t here = at < lo ? lo : (at < hi ? at : hi - kRun);  // (some run of the row)
+        const uint32_t here = WHOLE ? at : max(lo, min(at, hi - kRun));  // (some run of the row)
         uint64_t f = load_fields<KB>(a.sm, here);
         if constexpr (NORM)
             f |= static_cast<uint64_t>(a.coef[here >> a.block_shift]) << 32;
         return f;
     };
     uint64_t fields[kEmbAhead] = {};
-    if (turns > 0)
+    if (WHOLE || turns > 0)
 #pragma unroll
         for (uint32_t r = 0; r < kEmbAhead; ++r)
             fields[r] = request(r);
     for (uint32_t q0 = 0; q0 < most_turns; q0 += kEmbAhead) {
         uint64_t ahead[kEmbAhead] = {};
-        if (q0 + kEmbAhead < turns)
+        if (WHOLE || q0 + kEmbAhead < turns)
 #pragma unroll
             for (uint32_t r = 0; r < kEmbAhead; ++r)
-                ahead[r] = request(q0 + kEmbAhead + r);
+                ahead[r] = request(WHOLE && q0 + kEmbAhead >= most_turns ? r : q0 + kEmbAhead + r);  // (behind the last: the first again)
 #pragma unroll
         for (uint32_t r = 0; r < kEmbAhead; ++r) {
             const uint32_t at = from + (q0 + r) * kTurn;
-            if (q0 + r < turns && at < hi) {
+            // (lanes whose own unit is done go on with the wave's, to no effect: a state that is fed what is not its own stays in
+            // the table, and reads at most a word per symbol)
+            if (WHOLE || q0 + r < most_turns) {
                 uint32_t e[8];
 #pragma unroll
                 for (int t = 0; t < 8; ++t)
                     e[t] = LONE ? lone : rans_get<EAGER>(lut, x, wp, next, src);
-                if (at >= lo) {
+                if (WHOLE || at - lo < hi - lo) {
                     uint32_t d[4] = {merge_pair<KB>(fields[r], 0, e[0], e[1]), merge_pair<KB>(fields[r], 1, e[2], e[3]),
                                      merge_pair<KB>(fields[r], 2, e[4], e[5]), merge_pair<KB>(fields[r], 3, e[6], e[7])};
                     if constexpr (NORM) {
@@ -112,6 +115,22 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
     const uint32_t granule_shift = split ? 11u : 12u;
     static_assert(kChunk == 1u << 12 && kMidTurn * kTurn == 1u << 11, "log2 of a unit's elements");
 
+    fetch_arguments(a);
+    // ---- the tensor's table: the blob's slot table, or the steps that it is made from.  Nothing else depends on it, and it on nothing.
+    const bool make_lut = !holds_table(a.n_chunks);
+    constexpr uint32_t kTablePieces = kM / 4 / THREADS;  // of 16 bytes, a thread's
+    uint4 table_piece[kTablePieces];
+    const uint32_t begins[2] = {make_lut ? a.tb->step_of[tid] : 0u, make_lut && THREADS < kM / 8 ? a.tb->step_of[(tid + THREADS) % (kM / 8)] : 0u};
+#pragma unroll
+    for (uint32_t r = 0; r < kTablePieces; ++r) {
+        const uint32_t i = tid + r * THREADS;
+        table_piece[r] = make_uint4(0, 0, 0, 0);
+        if (!make_lut)
+            table_piece[r] = reinterpret_cast<const uint4 *>(a.tb->lut)[i];
+        else if (i < kSteps / 4)
+            table_piece[r] = reinterpret_cast<const uint4 *>(a.tb->steps)[i];
+    }
+
     // ---- which share of which row
     const uint32_t unit = blockIdx.x * (THREADS / kStates) + tid / kStates;
     const uint32_t t = unit < a.units ? a.per_token.quotient(unit) : 0u, part = unit - t * a.per_token.by;
@@ -123,7 +142,8 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
     const bool live = valid && first < row1;
     const uint32_t begin = live ? static_cast<uint32_t>(first) : 0u;
     const uint32_t lo = live ? max(row0, begin) : 0u;
-    const uint32_t hi = live ? static_cast<uint32_t>(min(static_cast<uint64_t>(row1), first + (1ull << granule_shift))) : kRun;
+    // (of a unit without work: 0, and no run lies in lo .. hi - 1)
+    const uint32_t hi = live ? static_cast<uint32_t>(min(static_cast<uint64_t>(row1), first + (1ull << granule_shift))) : 0u;
     const uint32_t turns = live ? (hi - begin + kTurn - 1) / kTurn : 0u;
     const uint32_t c = begin / kChunk, behind = split && live ? granule & 1u : 0u;
     uint16_t *out = a.out + static_cast<uint64_t>(t) * a.features + (lo - row0);
@@ -163,17 +183,19 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
                     copy_to_lds(from + i + lane, to + i * 16);
         }
     }
-    // ---- the slot table, beside it: the blob's, or made from its steps
-    if (holds_table(a.n_chunks)) {
-        for (uint32_t i = tid; i < kM / 4; i += THREADS)
-            reinterpret_cast<uint4 *>(lds.lut)[i] = reinterpret_cast<const uint4 *>(a.tb->lut)[i];
-    } else {
-        const uint32_t begins[2] = {a.tb->step_of[tid], THREADS < kM / 8 ? a.tb->step_of[tid + THREADS < kM / 8 ? tid + THREADS : 0u] : 0u};
-        for (uint32_t i = tid; i < kSteps / 4; i += THREADS)
-            reinterpret_cast<uint4 *>(lds.steps)[i] = reinterpret_cast<const uint4 *>(a.tb->steps)[i];
+    // ---- the slot table, beside it
+    if (make_lut) {
+#pragma unroll
+        for (uint32_t r = 0; r < kTablePieces; ++r)
+            if (tid + r * THREADS < kSteps / 4)
+                reinterpret_cast<uint4 *>(lds.steps)[tid + r * THREADS] = table_piece[r];
         lds_barrier();
         if (lone >= 256)
             make_table(lds.steps, begins, a.tb, lds.lut);
+    } else {
+#pragma unroll
+        for (uint32_t r = 0; r < kTablePieces; ++r)
+            reinterpret_cast<uint4 *>(lds.lut)[tid + r * THREADS] = table_piece[r];
     }
     wait_for_memory_acks();  // the words
     __syncthreads();
@@ -191,14 +213,18 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
         most_turns = max(most_turns, static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(turns), static_cast<int>(r * kStates))));
     const uint32_t from = begin + j * kRun;
     uint32_t wp = 0, wp_begin = 0;
+    const bool whole = __all(!live || (lo == begin && hi - begin == (1u << granule_shift)));
     if (lone < 256) {
-        embedding_walk<KB, true, NORM, EAGER>(lds.lut, NoWords{}, lone, x, wp, a, from, lo, hi, turns, most_turns, out);
+        embedding_walk<KB, true, NORM, EAGER, false>(lds.lut, NoWords{}, lone, x, wp, a, from, lo, hi, turns, most_turns, out);
     } else if (staged) {
         wp = wp_begin = wave * kEmbWindow + place + static_cast<uint32_t>(run_byte - aligned0);
-        embedding_walk<KB, false, NORM, EAGER>(lds.lut, LdsWords{lds.stage}, 0u, x, wp, a, from, lo, hi, turns, most_turns, out);
+        if (!whole)
+            embedding_walk<KB, false, NORM, EAGER, false>(lds.lut, LdsWords{lds.stage}, 0u, x, wp, a, from, lo, hi, turns, most_turns, out);
+        else if (live)
+            embedding_walk<KB, false, NORM, EAGER, true>(lds.lut, LdsWords{lds.stage}, 0u, x, wp, a, from, lo, hi, turns, most_turns, out);
     } else {
         const GlobalWords direct{reinterpret_cast<const uint8_t *>(a.words) + run_byte};
-        embedding_walk<KB, false, NORM, false>(lds.lut, direct, 0u, x, wp, a, from, lo, hi, turns, most_turns, out);
+        embedding_walk<KB, false, NORM, false, false>(lds.lut, direct, 0u, x, wp, a, from, lo, hi, turns, most_turns, out);
     }
     // a walk that has come to the chunk's end or the entry points is checked there
     if (live && turns == (split ? kMidTurn : kTurns) && hi - begin == (1u << granule_shift)) {
