@@ -43,9 +43,22 @@ __global__ __launch_bounds__(kAdapterThreads) void adapter_low_kernel(const Adap
         return;
     const uint4 *x = reinterpret_cast<const uint4 *>(g.x + static_cast<uint64_t>(t) * g.in_features);
     const uint4 *a = reinterpret_cast<const uint4 *>(g.a + (static_cast<uint64_t>(id) * g.rank + r) * g.in_features);
+    // (eight pieces of both requested together; in_features is a multiple of 128, so lanes end apart)
+    const uint32_t pieces = g.in_features / 8;
     float sum = 0.0f;
-    for (uint32_t i = lane; i < g.in_features / 8; i += 64)
-        sum = adapter_dot(x[i], a[i], sum);
+    for (uint32_t i0 = lane; i0 < pieces; i0 += 64 * 8) {
+        uint4 xs[8], as[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+            const uint32_t i = min(i0 + k * 64, pieces - 1);
+            xs[k] = x[i];
+            as[k] = a[i];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k)
+            if (i0 + k * 64 < pieces)
+                sum = adapter_dot(xs[k], as[k], sum);
+    }
 #pragma unroll
     for (int apart = 32; apart > 0; apart /= 2)
         sum += __shfl_xor(sum, apart);
@@ -63,6 +76,7 @@ __global__ __launch_bounds__(kAdapterThreads) void adapter_high_kernel(const Ada
     const uint4 *b = reinterpret_cast<const uint4 *>(g.b + (static_cast<uint64_t>(id) * g.out_features + o) * g.rank);
     const float *low = g.low + static_cast<uint64_t>(t) * g.rank;
     float sum = 0.0f;
+#pragma unroll 4
     for (uint32_t i = 0; i < g.rank / 8; ++i) {
         const uint4 v = b[i];
         const uint32_t d[4] = {v.x, v.y, v.z, v.w};
