@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
     else
         p.set_up(wave, lane, a.cols - j0, a.p_row);
 
-    // ---- steps of 32 k: all of one half, then (kInputGrad) all of the other
+    // ---- steps of 64 k: all of one half, then (kInputGrad) all of the other
     const uint32_t half_steps = (a.depth + kGatedDepth - 1) / kGatedDepth;
     const uint32_t steps_all = FORM == kInputGrad ? 2 * half_steps : half_steps;
     const uint32_t s_begin = static_cast<uint32_t>(static_cast<uint64_t>(steps_all) * slice / a.slices);
@@ -335,43 +335,71 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
         }
     }
 
-    // ---- a lane holds, of every 16 x 16 sums, i = lane % 16 and four neighbouring j from 4 * (lane / 16) on
-    const uint32_t quad = lane / 16 * 4;
+    // ---- A lane holds, of every 16 x 16 sums, i = lane % 16 and four neighbouring j from 4 * (lane / 16) on.  Of four such
+    // (two by two), rounded, the rows of 16 lanes trade pieces until a lane holds eight neighbouring j and a wave's store 64 bytes
+    // each of 16 rows: 8 bytes to a lane, as they come, were 32 bytes each, and twice the stores.
+    constexpr int kOutputs = FORM == kForward ? TILES / 2 : TILES;  // tiles of j
+    const uint32_t j_lane = j0 + wj * (kOutputs * 16) + lane / 16 % 2 * 16 + lane / 32 * 8;
+    const uint32_t i_lane = i0 + wi * (SIZE / 2) + lane % 16;
+    auto leave = [&](uint16_t *c, int jt, int it, auto words) {
+        uint32_t v[2][4];  // [jt, jt + 1]
 #pragma unroll
-    for (int it = 0; it < TILES; ++it) {
-        const uint32_t i = i0 + wi * (SIZE / 2) + it * 16 + lane % 16;
-        if (i >= a.rows)
-            continue;
-        if constexpr (FORM == kForward) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int jt = 0; jt < TILES / 2; ++jt) {
-                const uint32_t j = j0 + wj * (SIZE / 4) + jt * 16 + quad;
-                if (j >= a.cols)
-                    continue;
-                const gated_f32x4_t g = acc[jt][it], u = acc[jt + TILES / 2][it];
-                const uint64_t at = static_cast<uint64_t>(i) * a.c_row + j;
-                uint2 v;
-                v.x = pack_bf16(gated_value(g[0], a.activation) * u[0], gated_value(g[1], a.activation) * u[1]);
-                v.y = pack_bf16(gated_value(g[2], a.activation) * u[2], gated_value(g[3], a.activation) * u[3]);
-                *reinterpret_cast<uint2 *>(a.c[0] + at) = v;
-                if (a.gate) {
-                    *reinterpret_cast<uint2 *>(a.gate + at) = make_uint2(pack_bf16(g[0], g[1]), pack_bf16(g[2], g[3]));
-                    *reinterpret_cast<uint2 *>(a.up + at) = make_uint2(pack_bf16(u[0], u[1]), pack_bf16(u[2], u[3]));
-                }
+            for (int e = 0; e < 2; ++e) {
+                const auto r = __builtin_amdgcn_permlane16_swap(words(jt + t, it, e), words(jt + t, it + 1, e), false, false);
+                v[t][e] = r[0];
+                v[t][2 + e] = r[1];
             }
-        } else {
+        uint32_t at[2][4];  // [it, it + 1]
 #pragma unroll
-            for (int jt = 0; jt < TILES; ++jt) {
-                const uint32_t j = j0 + wj * (SIZE / 2) + jt * 16 + quad;
-                if (j >= a.cols)
-                    continue;
+        for (int d = 0; d < 4; ++d) {
+            const auto r = __builtin_amdgcn_permlane16_swap(v[0][d], v[1][d], false, false);
+            at[0][d] = r[0];
+            at[1][d] = r[1];
+        }
+        const uint32_t j = j_lane + jt * 16;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t i = i_lane + (it + t) * 16;
+            if (i < a.rows && j < a.cols)
+                *reinterpret_cast<uint4 *>(c + static_cast<uint64_t>(i) * a.c_row + j) = make_uint4(at[t][0], at[t][1], at[t][2], at[t][3]);
+        }
+    };
+    if (FORM == kInputGrad && a.partial) {
+#pragma unroll
+        for (int jt = 0; jt < TILES; ++jt)
+#pragma unroll
+            for (int it = 0; it < TILES; ++it) {
+                const uint32_t i = i_lane + it * 16, j = j0 + wj * (SIZE / 2) + jt * 16 + lane / 16 * 4;
+                asm volatile("" : "+a"(acc[jt][it]));  // (see below)
                 const gated_f32x4_t v = acc[jt][it];
-                const uint64_t at = static_cast<uint64_t>(i) * a.c_row + j;
-                if (FORM == kInputGrad && a.partial) {
-                    *reinterpret_cast<gated_f32x4_t *>(a.partial + static_cast<uint64_t>(slice) * a.rows * a.c_row + at) = v;
-                    continue;
+                if (i < a.rows && j < a.cols)
+                    *reinterpret_cast<float4 *>(a.partial + (static_cast<uint64_t>(slice) * a.rows + i) * a.c_row + j) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+        return;
+    }
+#pragma unroll
+    for (int jt = 0; jt < kOutputs; jt += 2) {
+#pragma unroll
+        for (int it = 0; it < TILES; it += 2) {
+            // (a group's sums leave the accumulation registers when it is their turn, not all at once)
+#pragma unroll
+            for (int t = 0; t < (FORM == kForward ? 8 : 4); ++t)
+                asm volatile("" : "+a"(acc[jt + t % 2 + t / 4 * (TILES / 2)][it + t / 2 % 2]));
+            auto sums = [&](int j, int i, int e) { return pack_bf16(acc[j][i][2 * e], acc[j][i][2 * e + 1]); };
+            if constexpr (FORM == kForward) {
+                auto products = [&](int j, int i, int e) {
+                    const gated_f32x4_t &g = acc[j][i], &u = acc[j + TILES / 2][i];
+                    return pack_bf16(gated_value(g[2 * e], a.activation) * u[2 * e], gated_value(g[2 * e + 1], a.activation) * u[2 * e + 1]);
+                };
+                leave(a.c[0], jt, it, products);
+                if (a.gate) {
+                    leave(a.gate, jt, it, sums);
+                    leave(a.up, jt, it, [&](int j, int i, int e) { return sums(j + TILES / 2, i, e); });
                 }
-                *reinterpret_cast<uint2 *>((half ? a.c[1] : a.c[0]) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+            } else {
+                leave(half ? a.c[1] : a.c[0], jt, it, sums);
             }
         }
     }
