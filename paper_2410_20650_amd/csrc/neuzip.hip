@@ -1531,6 +1531,17 @@ int neuzip_linear_batch_scratch(const neuzip_blob *const *weights, const uint64_
                                 uint64_t in_features, const void *d_x, uint32_t tokens, const float *const *d_bias,
                                 float *const *d_y, void *d_scratch, uint64_t scratch_bytes, void *hip_stream)
 {
+    return linear_behind(weights, out_features, count, in_features, d_x, tokens, d_bias, d_y, d_scratch, scratch_bytes, nullptr, nullptr,
+                         static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"
+
+// (see neuzip_host.h; without a front, the launch in front is the layer's own)
+int nz::linear_behind(const neuzip_blob *const *weights, const uint64_t *out_features, uint32_t count, uint64_t in_features,
+                      const void *d_x, uint32_t tokens, const float *const *d_bias, float *const *d_y, void *d_scratch,
+                      uint64_t scratch_bytes, LinearFront front, const void *context, hipStream_t stream)
+{
     if (count == 0)
         return NEUZIP_OK;
     if (!weights || !out_features || !d_y || !d_x || tokens == 0 || count > kLinBatchMax)
@@ -1552,7 +1563,6 @@ int neuzip_linear_batch_scratch(const neuzip_blob *const *weights, const uint64_
         if (w->k != weights[0]->k || (w->block != 0) != (weights[0]->block != 0))
             return NEUZIP_EINVAL;
     }
-    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const int behind = follow(weights, count, stream);
     if (behind != NEUZIP_OK)
         return behind;
@@ -1627,7 +1637,11 @@ int neuzip_linear_batch_scratch(const neuzip_blob *const *weights, const uint64_
         init.row_pieces = static_cast<uint32_t>(in_features / kRun);
         init_wgs += static_cast<uint32_t>((static_cast<uint64_t>(init.row_pieces) * tokens + kLinInitThreads - 1) / kLinInitThreads);
     }
-    if (init_wgs > 0)
+    if (front) {
+        const int rc = front(init, init_wgs, context, stream);
+        if (rc != NEUZIP_OK)
+            return rc;
+    } else if (init_wgs > 0)
         hipLaunchKernelGGL(linear_init_kernel, dim3(init_wgs), dim3(kLinInitThreads), 0, stream, init);
     // the kernel holds the partial sums of at most 64 tokens: larger batches go through in tiles of 64
     // (each tile decodes the weights again: beyond a few tiles decompressing once and a dense product win)
@@ -1681,8 +1695,6 @@ int neuzip_linear_batch_scratch(const neuzip_blob *const *weights, const uint64_
     }
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
-
-}  // extern "C"
 
 namespace {
 

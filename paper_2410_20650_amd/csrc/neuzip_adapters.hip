@@ -19,6 +19,16 @@ constexpr uint32_t kAdapterMostTokens = 65535;  // a grid's second dimension
 
 inline uint64_t low_bytes(uint32_t tokens, uint32_t rank) { return pad_to(static_cast<uint64_t>(tokens) * rank * sizeof(float), 256); }
 
+int launch_low(const LinearInitArgs &init, uint32_t wgs, const void *context, hipStream_t stream)
+{
+    const AdapterArgs &g = *static_cast<const AdapterArgs *>(context);
+    const uint64_t low_wgs = static_cast<uint64_t>((g.rank + kAdapterRows - 1) / kAdapterRows) * g.tokens;
+    if (wgs + low_wgs >= (1ull << 31))
+        return NEUZIP_EUNSUPPORTED;
+    hipLaunchKernelGGL(adapter_low_kernel, dim3(static_cast<uint32_t>(wgs + low_wgs)), dim3(kAdapterThreads), 0, stream, init, wgs, g);
+    return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -44,10 +54,6 @@ int neuzip_linear_adapters(const neuzip_blob *weight, uint64_t out_features, uin
     if (scratch_bytes < neuzip_linear_adapters_scratch_bytes(out_features, in_features, tokens, rank))
         return NEUZIP_EINVAL;
     const uint64_t own = low_bytes(tokens, rank);
-    const int rc = neuzip_linear_batch_scratch(&weight, &out_features, 1, in_features, d_x, tokens, &d_bias, &d_y,
-                                               static_cast<uint8_t *>(d_scratch) + own, scratch_bytes - own, hip_stream);
-    if (rc != NEUZIP_OK)
-        return rc;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     AdapterArgs g;
     std::memset(&g, 0, sizeof(g));
@@ -63,7 +69,11 @@ int neuzip_linear_adapters(const neuzip_blob *weight, uint64_t out_features, uin
     g.rank = rank;
     g.in_features = static_cast<uint32_t>(in_features);
     g.out_features = static_cast<uint32_t>(out_features);
-    hipLaunchKernelGGL(adapter_low_kernel, dim3((rank + 3) / 4, tokens), dim3(kAdapterThreads), 0, stream, g);
+    // (the low products are launched once the layer's own arguments have been found right)
+    const int rc = linear_behind(&weight, &out_features, 1, in_features, d_x, tokens, &d_bias, &d_y, static_cast<uint8_t *>(d_scratch) + own,
+                                 scratch_bytes - own, launch_low, &g, stream);
+    if (rc != NEUZIP_OK)
+        return rc;
     hipLaunchKernelGGL(adapter_high_kernel, dim3((g.out_features + kAdapterThreads - 1) / kAdapterThreads, tokens), dim3(kAdapterThreads), 0,
                        stream, g);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;

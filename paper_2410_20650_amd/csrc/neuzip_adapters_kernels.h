@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <cstdint>
 
+#include "neuzip_linear_front.h"
+
 namespace nz {
 
 struct AdapterArgs {
@@ -33,11 +35,18 @@ __device__ __forceinline__ float adapter_dot(const uint4 &p, const uint4 &q, flo
     return sum;
 }
 
-// low[t][r] = s (A[a] x[t])[r]: a wave to a token and a row of A.
-constexpr uint32_t kAdapterThreads = 256;
-__global__ __launch_bounds__(kAdapterThreads) void adapter_low_kernel(const AdapterArgs g)
+// low[t][r] = s (A[a] x[t])[r]: a wave to a token and a row of A, beside what the linear layer has its outputs and activations set up
+// with (48 tokens, 14336 -> 4096, rank 64: 4.0 and 11.0 us one behind the other).
+constexpr uint32_t kAdapterThreads = 256, kAdapterRows = kAdapterThreads / 64;  // rows of A of a workgroup
+static_assert(kAdapterThreads == kLinInitThreads, "both in one launch");
+__global__ __launch_bounds__(kAdapterThreads) void adapter_low_kernel(const LinearInitArgs init, uint32_t init_wgs, const AdapterArgs g)
 {
-    const uint32_t lane = threadIdx.x % 64, r = blockIdx.x * (kAdapterThreads / 64) + threadIdx.x / 64, t = blockIdx.y;
+    if (blockIdx.x < init_wgs) {
+        linear_init_workgroup(init, blockIdx.x);
+        return;
+    }
+    const uint32_t groups = (g.rank + kAdapterRows - 1) / kAdapterRows, wg = blockIdx.x - init_wgs, t = wg / groups;
+    const uint32_t lane = threadIdx.x % 64, r = (wg - t * groups) * kAdapterRows + threadIdx.x / 64;
     const int32_t id = g.ids[t];
     if (r >= g.rank || id < 0 || static_cast<uint32_t>(id) >= g.adapters)
         return;

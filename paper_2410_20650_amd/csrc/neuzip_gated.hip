@@ -201,7 +201,8 @@ int neuzip_gated_linear(const neuzip_blob *gate, const neuzip_blob *up, uint64_t
         return NEUZIP_EINVAL;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint64_t count = tokens * out_features, each = pad_to(count * sizeof(float), 256);
-    if (wgs_for(count) >= (1ull << 31))
+    const uint64_t wgs = wgs_for((count + 3) / 4);
+    if (wgs >= (1ull << 31))
         return NEUZIP_EUNSUPPORTED;
     float *const sums[2] = {static_cast<float *>(d_scratch), static_cast<float *>(d_scratch) + each / sizeof(float)};
     const neuzip_blob *const weights[2] = {gate, up};
@@ -210,7 +211,7 @@ int neuzip_gated_linear(const neuzip_blob *gate, const neuzip_blob *up, uint64_t
                                                scratch_bytes - 2 * each, hip_stream);
     if (rc != NEUZIP_OK)
         return rc;
-    hipLaunchKernelGGL(gated_product_kernel, dim3(static_cast<uint32_t>(wgs_for(count))), dim3(kGatedSlopeThreads), 0, stream, sums[0],
+    hipLaunchKernelGGL(gated_product_kernel, dim3(static_cast<uint32_t>(wgs)), dim3(kGatedSlopeThreads), 0, stream, sums[0],
                        sums[1], static_cast<uint16_t *>(d_h), count, static_cast<uint32_t>(activation));
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }

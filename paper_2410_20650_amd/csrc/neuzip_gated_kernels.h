@@ -460,13 +460,19 @@ __global__ __launch_bounds__(kGatedSlopeThreads) void gated_join_kernel(const fl
     out[at] = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
 }
 
-// h from the two sums in binary32, as the compressed weights' product leaves them (serving).
+// h from the two sums in binary32, as the compressed weights' product leaves them (serving), four to a thread.
 __global__ __launch_bounds__(kGatedSlopeThreads) void gated_product_kernel(const float *__restrict__ gate, const float *__restrict__ up,
                                                                            uint16_t *__restrict__ h, uint64_t count, uint32_t activation)
 {
-    const uint64_t at = static_cast<uint64_t>(blockIdx.x) * kGatedSlopeThreads + threadIdx.x;
-    if (at < count)
-        h[at] = static_cast<uint16_t>(pack_bf16(gated_value(gate[at], activation) * up[at], 0.0f));
+    const uint64_t at = (static_cast<uint64_t>(blockIdx.x) * kGatedSlopeThreads + threadIdx.x) * 4;
+    if (at + 4 <= count && (reinterpret_cast<uintptr_t>(h) & 7u) == 0) {
+        const float4 g = *reinterpret_cast<const float4 *>(gate + at), u = *reinterpret_cast<const float4 *>(up + at);
+        *reinterpret_cast<uint2 *>(h + at) = make_uint2(pack_bf16(gated_value(g.x, activation) * u.x, gated_value(g.y, activation) * u.y),
+                                                        pack_bf16(gated_value(g.z, activation) * u.z, gated_value(g.w, activation) * u.w));
+        return;
+    }
+    for (uint64_t i = at; i < at + 4 && i < count; ++i)
+        h[i] = static_cast<uint16_t>(pack_bf16(gated_value(gate[i], activation) * up[i], 0.0f));
 }
 
 }  // namespace nz
