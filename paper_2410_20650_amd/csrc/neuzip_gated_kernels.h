@@ -58,18 +58,35 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
-// 16 bytes per lane from memory straight into LDS, lane l's to `to` + 16 l.  Not the builtin: the compiler would wait for such a
-// copy in front of the next read of LDS, whichever buffer it is from.  The waits are the caller's.  (The place goes to M0, with
-// an instruction at least between that and the copy.)
+// 16 bytes per lane from memory straight into LDS, lane l's to M0 + OFFSET + 16 l.  Not the builtin: the compiler would wait for such
+// a copy in front of the next read of LDS, whichever buffer it is from.  The waits are the caller's.  The offset counts on both
+// sides, so the lane's address is given without it; up to four copies, 1 KB apart, share a place in M0 (between whose writing and the
+// copy an instruction has to stand).
+constexpr uint32_t kGatedShared = 4, kGatedBias = (kGatedShared - 1) * 1024;
 __device__ __forceinline__ void gated_copy_place(uint32_t to) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(to)); }
+template <uint32_t OFFSET>
 __device__ __forceinline__ void gated_copy(const uint8_t *base, uint32_t offset)
 {
-    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base));
+    asm volatile("global_load_lds_dwordx4 %0, %1 offset:%2" ::"v"(offset), "s"(base), "n"(OFFSET));
 }
-__device__ __forceinline__ void gated_copy(const uint8_t *from) { asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(from)); }
+template <uint32_t OFFSET>
+__device__ __forceinline__ void gated_copy(const uint8_t *from)
+{
+    asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from), "n"(OFFSET));
+}
 
 // What lanes read that have no k of their own: zeros.
 __device__ const uint4 kGatedZeros[1] = {};
+
+// f(0), f(1), ... f(N - 1), each with its number known to the compiler
+template <int N, int AT = 0, class F>
+__device__ __forceinline__ void each_of(const F &f)
+{
+    if constexpr (AT < N) {
+        f(std::integral_constant<uint32_t, AT>{});
+        each_of<N, AT + 1>(f);
+    }
+}
 
 // ---- one operand's tile in LDS: R values of i (or j) by 64 of k, R * 128 bytes.
 // Along k: a row of the tile is 64 k, 128 bytes, 8 pieces of 16 bytes, piece p of row r in place p ^ (r / 2 % 8).
@@ -81,42 +98,47 @@ struct GatedOperand {
     static constexpr uint32_t kBytes = R * kGatedDepth * 2;
     static constexpr uint32_t kCopies = kBytes / 1024 / WAVES;  // a wave's, 1 KB each
     static constexpr uint32_t kPieces = R / 8;                  // ACROSS: of a row
-    uint32_t offset[kCopies];  // of the lane's pieces in the tile's first step
-    uint32_t k_of;             // ALONG: the k of the lane's piece in every copy; ACROSS: of copy 0
+    uint32_t offset[kCopies];  // of the lane's pieces in the tile's first step, less what the copy adds, plus kGatedBias
+    uint32_t k_of;             // the k of the lane's piece in copy 0
 
     // left: values from the tile's first on (a lane that has none reads another's: nobody looks at the sums)
     __device__ __forceinline__ void set_up(uint32_t wave, uint32_t lane, uint32_t left, uint32_t row_elems)
     {
 #pragma unroll
         for (uint32_t n = 0; n < kCopies; ++n) {
-            const uint32_t copy = n * WAVES + wave;
+            const uint32_t copy = wave * kCopies + n, shift = kGatedBias - n % kGatedShared * 1024;
             if constexpr (ALONG) {
                 uint32_t r = copy * 8 + lane / 8;
                 const uint32_t piece = (lane % 8) ^ (r / 2 % 8);
                 r = r < left ? r : left - 1;
-                offset[n] = (r * row_elems + piece * 8) * 2;
-                k_of = piece * 8;
+                offset[n] = (r * row_elems + piece * 8) * 2 + shift;
+                if (n == 0)
+                    k_of = piece * 8;
             } else {
                 const uint32_t k = copy * (64 / kPieces) + lane / kPieces;
                 const uint32_t f = k % 4 + k / 8 % 2 * 4;
                 uint32_t piece = (((lane % kPieces) / 2) ^ f) * 2 + lane % 2;
                 piece = piece * 8 < left ? piece : 0u;
-                offset[n] = (k * row_elems + piece * 8) * 2;
+                offset[n] = (k * row_elems + piece * 8) * 2 + shift;
                 if (n == 0)
                     k_of = k;
             }
         }
     }
-    // requests copy n of the tile that begins at `from`.  RAGGED: only `depth` of its k are there, the others are zeros.
-    template <bool RAGGED>
-    __device__ __forceinline__ void request(uint32_t n, const uint8_t *from, uint32_t to, uint32_t wave, uint32_t depth) const
+    // requests copy N of the tile that begins at from + kGatedBias.  RAGGED: only `depth` of its k are there, the others are zeros.
+    template <bool RAGGED, uint32_t N>
+    __device__ __forceinline__ void request(const uint8_t *from, uint32_t to, uint32_t wave, uint32_t depth) const
     {
-        gated_copy_place(to + (n * WAVES + wave) * 1024);
+        if constexpr (N % kGatedShared == 0)
+            gated_copy_place(to + (wave * kCopies + N) * 1024);
+        constexpr uint32_t kOffset = N % kGatedShared * 1024;
         if constexpr (RAGGED) {
-            const uint32_t k = ALONG ? k_of : k_of + n * (WAVES * 64 / kPieces);
-            gated_copy(k < depth ? from + offset[n] : reinterpret_cast<const uint8_t *>(kGatedZeros));
+            // (along k, every other copy's rows hold their halves of 32 k the other way round)
+            static_assert(kCopies % 2 == 0, "a wave's first copy is an even one");
+            const uint32_t k = ALONG ? k_of ^ (N % 2 * 32) : k_of + N * (64 / kPieces);
+            gated_copy<kOffset>(k < depth ? from + offset[N] : reinterpret_cast<const uint8_t *>(kGatedZeros) - kOffset);
         } else {
-            gated_copy(from, offset[n]);
+            gated_copy<kOffset>(from, offset[N]);
         }
     }
     // the lane's address of the operand's first 16 values (first: their number in the tile), for read()
@@ -214,23 +236,24 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
     auto seek = [&](uint32_t s) {
         const bool second = FORM == kInputGrad ? s >= half_steps : half != 0;
         const uint32_t in_half = FORM == kInputGrad && second ? s - half_steps : s;
-        q_at = (second ? q_base[1] : q_base[0]) + in_half * q_step;
-        p_at = (second ? p_base[1] : p_base[0]) + in_half * p_step;
+        q_at = (second ? q_base[1] : q_base[0]) + in_half * q_step - kGatedBias;
+        p_at = (second ? p_base[1] : p_base[0]) + in_half * p_step - kGatedBias;
         if constexpr (FORM == kForward)
-            p_other = p_base[1] + in_half * p_step;
+            p_other = p_base[1] + in_half * p_step - kGatedBias;
         left = a.depth - in_half * kGatedDepth;
     };
-    auto request_copy = [&](auto ragged, uint32_t n) {
+    auto request_copy = [&](auto ragged, auto number) {
         constexpr bool RAGGED = decltype(ragged)::value;
+        constexpr uint32_t N = decltype(number)::value;
         const uint32_t to = lds_at + (ahead - s_begin) % kGatedRing * kStage;
-        if (n < Q::kCopies)
-            q.template request<RAGGED>(n, q_at, to, wave, left);
+        if constexpr (N < Q::kCopies)
+            q.template request<RAGGED, N>(q_at, to, wave, left);
         else if constexpr (FORM != kForward)
-            p.template request<RAGGED>(n - Q::kCopies, p_at, to + Q::kBytes, wave, left);
-        else if (n < Q::kCopies + Half::kCopies)
-            half_p.template request<RAGGED>(n - Q::kCopies, p_at, to + Q::kBytes, wave, left);
+            p.template request<RAGGED, N - Q::kCopies>(p_at, to + Q::kBytes, wave, left);
+        else if constexpr (N < Q::kCopies + Half::kCopies)
+            half_p.template request<RAGGED, N - Q::kCopies>(p_at, to + Q::kBytes, wave, left);
         else
-            half_p.template request<RAGGED>(n - Q::kCopies - Half::kCopies, p_other, to + Q::kBytes + Half::kBytes, wave, left);
+            half_p.template request<RAGGED, N - Q::kCopies - Half::kCopies>(p_other, to + Q::kBytes + Half::kBytes, wave, left);
     };
     auto advance = [&]() {
         ++ahead;
@@ -271,37 +294,37 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
     };
     static_assert(kCopies == 2 * TILES, "two copies to a row of sums");
     auto arrive = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::"v"(lds) : "memory"); };
-    auto half_step = [&](auto requests, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
+    // (what is not a product stands by itself between products, in their shadow)
+    auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
+        constexpr int n = decltype(number)::value, kEach = TILES / 4;
+        auto some = [&](int from) {
 #pragma unroll
-        for (int n = 0; n < TILES; ++n) {
-            // (what is not a product stands by itself between products, in their shadow)
-#pragma unroll
-            for (int it = 0; it < TILES; ++it) {
+            for (int it = from * kEach; it < (from + 1) * kEach; ++it)
                 acc[n][it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.p[n], now.q[it], acc[n][it], 0, 0, 0);
-                if (it % (TILES / 4) == 0) {
-                    if (it / (TILES / 4) == 0)
-                        read_q(then, tile, n, h);
-                    if (it / (TILES / 4) == 1)
-                        read_p(then, tile, n, h);
-                    if constexpr (decltype(requests)::value) {
-                        if (it / (TILES / 4) >= 2)
-                            request_copy(std::false_type{}, 2 * n + it / (TILES / 4) - 2);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
-        }
+        };
+        some(0);
+        read_q(then, tile, n, h);
+        __builtin_amdgcn_sched_barrier(0);
+        some(1);
+        read_p(then, tile, n, h);
+        __builtin_amdgcn_sched_barrier(0);
+        some(2);
+        if constexpr (decltype(requests)::value)
+            request_copy(std::false_type{}, std::integral_constant<uint32_t, 2 * n>{});
+        __builtin_amdgcn_sched_barrier(0);
+        some(3);
+        if constexpr (decltype(requests)::value)
+            request_copy(std::false_type{}, std::integral_constant<uint32_t, 2 * n + 1>{});
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto half_step = [&](auto requests, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
+        each_of<TILES>([&](auto n) { row_of_sums(requests, n, now, then, tile, h); });
     };
     auto request_all = [&]() {
-        if (left >= kGatedDepth) {
-#pragma unroll
-            for (uint32_t n = 0; n < kCopies; ++n)
-                request_copy(std::false_type{}, n);
-        } else {
-#pragma unroll
-            for (uint32_t n = 0; n < kCopies; ++n)
-                request_copy(std::true_type{}, n);
-        }
+        if (left >= kGatedDepth)
+            each_of<kCopies>([&](auto n) { request_copy(std::false_type{}, n); });
+        else
+            each_of<kCopies>([&](auto n) { request_copy(std::true_type{}, n); });
         advance();
     };
     if (steps > 0) {
