@@ -25,31 +25,37 @@ inline bool valid_width(uint64_t w) { return w > 0 && w % 8 == 0 && w <= kGatedW
 inline uint32_t tiles_of(uint64_t n, uint32_t size) { return static_cast<uint32_t>((n + size - 1) / size); }
 
 struct GatedShape {
-    uint32_t size, slices;
+    uint32_t size, ring, slices;
 };
 
 // Tiles of 256 or of 128, and for the input gradient, whose tiles are few and their sums long, how many slices of k: the least of
-// what the forms are expected to take, in us.  A CU holds one workgroup of 256 or two of 128, and tiles come in rounds of as many as
-// there are places.  A step of 64 k of a tile of 256 takes 1.7 us with all CUs at work; a round of tiles of 128 0.65 of that (2048
-// tokens, 4096 -> 14336, forward: 896 tiles of 256 503 us, 3584 of 128 566; 1000 tokens 224 / 298), or 0.45 with one on a CU (333
-// tokens, 1160 -> 2808: 33.8 / 14.9).  The sums of slices are written and read again in binary32.
+// what the forms are expected to take, in us, with tiles in rounds of as many as the CUs have places for.
+//   256             1.7 a step of 64 k and 9 a tile, 256 places  (2048 tokens, 4096 -> 14336, weight gradients: 480; forward 1000 tokens 204)
+//   128             1.1 and 4, 512 places                        (576; 288)
+//   128, four steps held, no more tiles than CUs: 0.63 and 5     (input gradient, 1000 tokens, unsliced: 283, with two held 380; forward of 200
+//                   tokens, 4096 -> 4096, 30.8 / 42.8, of one, 4096 -> 14336, 36.2 / 45.2; beyond a round the two of a CU are the faster ones,
+//                   weight gradients of 200 tokens 46.5 / 31.1)
+// and the sums of slices are written and read again in binary32.
 template <GatedForm FORM>
 GatedShape gated_shape(uint64_t rows, uint64_t cols, uint64_t depth)
 {
     const double steps = static_cast<double>(tiles_of(depth, kGatedDepth)) * (FORM == kInputGrad ? 2 : 1);
-    GatedShape best = {128, 1};
+    GatedShape best = {128, 2, 1};
     double least = 0;
     for (uint32_t size = 128; size <= 256; size += 128) {
         const uint64_t tiles = static_cast<uint64_t>(tiles_of(rows, size)) * tiles_of(cols, FORM == kForward ? size / 2 : size) * (FORM == kWeightGrad ? 2 : 1);
         for (uint32_t slices = 1; slices <= (FORM == kInputGrad ? 16u : 1u) && steps >= 4.0 * slices; slices *= 2) {
             const uint64_t all = tiles * slices;
-            const double rounds = size == 256 ? static_cast<double>((all + 255) / 256) : (all <= 256 ? 0.45 : 0.65 * static_cast<double>((all + 511) / 512));
-            double us = rounds * (1.7 * steps / slices + 5.0);
+            const uint32_t ring = size == 128 && all <= 256 ? 4 : 2;
+            const double each = steps / slices;
+            double us = size == 256 ? static_cast<double>((all + 255) / 256) * (1.7 * each + 9)
+                        : ring == 4 ? 0.63 * each + 5
+                                    : static_cast<double>((all + 511) / 512) * (1.1 * each + 4);
             if (slices > 1)
-                us += 3.0 + static_cast<double>(rows) * cols * 4 * (2 * slices + 1) / 4e6;
+                us += 3.0 + static_cast<double>(rows) * cols * 4 * (slices + 0.5) / 6e6;
             if (least == 0 || us < least) {
                 least = us;
-                best = {size, slices};
+                best = {size, ring, slices};
             }
         }
     }
@@ -65,10 +71,13 @@ int launch_gated(GatedArgs &a, const GatedShape &shape, hipStream_t stream)
     const uint64_t grid = static_cast<uint64_t>(a.tiles_i) * a.tiles_j * shape.slices * (FORM == kWeightGrad ? 2 : 1);
     if (grid >= (1ull << 31))
         return NEUZIP_EUNSUPPORTED;
+    const dim3 wgs(static_cast<uint32_t>(grid)), threads(kGatedThreads);
     if (shape.size == 256)
-        hipLaunchKernelGGL((gated_kernel<FORM, 256>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedThreads), 0, stream, a);
+        hipLaunchKernelGGL((gated_kernel<FORM, 256, 2>), wgs, threads, 0, stream, a);
+    else if (shape.ring == 4)
+        hipLaunchKernelGGL((gated_kernel<FORM, 128, 4>), wgs, threads, 0, stream, a);
     else
-        hipLaunchKernelGGL((gated_kernel<FORM, 128>), dim3(static_cast<uint32_t>(grid)), dim3(kGatedThreads), 0, stream, a);
+        hipLaunchKernelGGL((gated_kernel<FORM, 128, 2>), wgs, threads, 0, stream, a);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
 

@@ -172,11 +172,10 @@ struct GatedOperand {
 
 // Launch shape: tiles of SIZE i by SIZE j, four waves of SIZE / 2 by SIZE / 2.
 constexpr uint32_t kGatedWaves = 4, kGatedThreads = kGatedWaves * 64;
-// Steps whose operands LDS has room for.
-constexpr uint32_t kGatedRing = 2;
-
-template <GatedForm FORM, int SIZE>
-__global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kernel(const GatedArgs a)
+// RING: the steps that LDS holds.  Two are 128 KB for a tile of 256, or 64 KB for one of 128, of which two share a CU.  Where there are
+// fewer of those than CUs, nothing else hides the wait for memory, and four are held.
+template <GatedForm FORM, int SIZE, int RING>
+__global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) void gated_kernel(const GatedArgs a)
 {
     constexpr int WAVES = kGatedWaves;
     constexpr bool Q_ALONG = FORM != kWeightGrad, P_ALONG = FORM == kForward;
@@ -185,7 +184,7 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
     typedef GatedOperand<SIZE, WAVES, P_ALONG> P;
     typedef GatedOperand<SIZE / 2, WAVES, true> Half;  // kForward: the rows of one weight
     constexpr uint32_t kStage = Q::kBytes + P::kBytes;
-    __shared__ __align__(16) uint8_t lds[kGatedRing * kStage];
+    __shared__ __align__(16) uint8_t lds[RING * kStage];
 
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / 64)));
@@ -245,7 +244,7 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
     auto request_copy = [&](auto ragged, auto number) {
         constexpr bool RAGGED = decltype(ragged)::value;
         constexpr uint32_t N = decltype(number)::value;
-        const uint32_t to = lds_at + (ahead - s_begin) % kGatedRing * kStage;
+        const uint32_t to = lds_at + (ahead - s_begin) % RING * kStage;
         if constexpr (N < Q::kCopies)
             q.template request<RAGGED, N>(q_at, to, wave, left);
         else if constexpr (FORM != kForward)
@@ -293,7 +292,13 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
             o.p[n] = P::read(tile + Q::kBytes, p_lane, n, h);
     };
     static_assert(kCopies == 2 * TILES, "two copies to a row of sums");
-    auto arrive = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::"v"(lds) : "memory"); };
+    // the next step has come, and everyone holds this one in registers; `pass` copies that were requested later may still travel
+    auto arrive = [&](auto pass) {
+        asm volatile("s_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"v"(lds), "n"(decltype(pass)::value) : "memory");
+    };
+    constexpr std::integral_constant<uint32_t, 0> kNone{};
+    constexpr std::integral_constant<uint32_t, (RING - 2) * kCopies> kLater{};
+    static_assert(kLater.value < 64, "as many as the counter counts");
     // (what is not a product stands by itself between products, in their shadow)
     auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
         constexpr int n = decltype(number)::value, kEach = TILES / 4;
@@ -330,28 +335,28 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 256 ? 1 : 2) void gated_kern
     if (steps > 0) {
         Operands first, second;
         seek(s_begin);
-        for (uint32_t r = 0; r < kGatedRing && r < steps; ++r)
+        for (uint32_t r = 0; r < RING && r < steps; ++r)
             request_all();
-        arrive();
+        arrive(kNone);
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
             read_q(first, lds, n, 0);
             read_p(first, lds, n, 0);
         }
         for (uint32_t s = 0; s < steps;) {
-            while (s + kGatedRing < steps && left >= kGatedDepth) {
-                const uint8_t *tile = lds + s % kGatedRing * kStage, *next = lds + (s + 1) % kGatedRing * kStage;
+            while (s + RING < steps && left >= kGatedDepth) {
+                const uint8_t *tile = lds + s % RING * kStage, *next = lds + (s + 1) % RING * kStage;
                 half_step(std::false_type{}, first, second, tile, 1);
-                arrive();
+                arrive(kLater);
                 half_step(std::true_type{}, second, first, next, 0);
                 advance();
                 ++s;
             }
             // one by one: the last, and where half a sum ends
-            const uint8_t *tile = lds + s % kGatedRing * kStage, *next = lds + (s + 1) % kGatedRing * kStage;
+            const uint8_t *tile = lds + s % RING * kStage, *next = lds + (s + 1) % RING * kStage;
             half_step(std::false_type{}, first, second, tile, 1);
-            arrive();
-            if (s + kGatedRing < steps)
+            arrive(kNone);
+            if (s + RING < steps)
                 request_all();
             half_step(std::false_type{}, second, first, next, 0);  // (behind the last step: what nobody uses)
             ++s;
