@@ -401,20 +401,20 @@ uint64_t neuzip_gated_linear_scratch_bytes(uint64_t out_features, uint64_t in_fe
  *   d_gate_weight, d_up_weight   out_features x in_features bf16 words.
  *   in_features, out_features    multiples of 8, at most 2^22; tokens below 2^31, also 0.
  *   d_h               tokens x out_features bf16 words; overwritten.
- *   d_gate, d_up      NULL, or room for g and u (bf16, as d_h), which the backward pass takes; both or neither.
+ *   d_gate, d_up      NULL, or room for g and u (floats, as many as d_h has words), which the backward pass takes; both or neither.
  *   d_grad_h          tokens x out_features bf16 words.
  *   d_grad_x          tokens x in_features bf16 words, or NULL: not wanted.
  *   d_grad_gate_weight, d_grad_up_weight   out_features x in_features bf16 words each, as neuzip_update takes them; or both NULL: not
  *                     wanted.  (No tokens: zeros.)
  *   d_scratch         device buffer of scratch_bytes bytes, at least neuzip_gated_backward_scratch_bytes(), in use until the call's
  *                     work has run.
- * All pointers are aligned to 16 bytes.  Products are exact, sums binary32; h, g, u and the three gradients are rounded once, to nearest
+ * All pointers are aligned to 16 bytes.  Products are exact, sums binary32; h and the three gradients are rounded once, to nearest
  * even, and so are dg and du, which the matrix cores take as bf16.  Results do not change from run to run.  Never allocates, never
  * synchronises.
  */
 int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, uint64_t tokens, uint64_t out_features,
-                         uint64_t in_features, int activation, void *d_h, void *d_gate, void *d_up, void *hip_stream);
-int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, const void *d_gate, const void *d_up,
+                         uint64_t in_features, int activation, void *d_h, float *d_gate, float *d_up, void *hip_stream);
+int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, const float *d_gate, const float *d_up,
                           const void *d_grad_h, uint64_t tokens, uint64_t out_features, uint64_t in_features, int activation,
                           void *d_grad_x, void *d_grad_gate_weight, void *d_grad_up_weight, void *d_scratch, uint64_t scratch_bytes,
                           void *hip_stream);

@@ -573,8 +573,8 @@ def _gated_shape(x, w_gate, w_up):
 
 def neuzip_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: int = SILU, h: torch.Tensor = None,
                          keep=False, stream=None):
-    """h = act(x W_gate^T) * (x W_up^T), bf16, from decompressed weights.  keep: returns (h, gate, up), with the two products that
-    neuzip_gated_backward takes (a pair of tensors: into these)."""
+    """h = act(x W_gate^T) * (x W_up^T), bf16, from decompressed weights.  keep: returns (h, gate, up), with the two products
+    (float32) that neuzip_gated_backward takes (a pair of tensors: into these)."""
     tokens, out_features, in_features = _gated_shape(x, w_gate, w_up)
     shape = (tokens, out_features)
     if h is None:
@@ -582,11 +582,11 @@ def neuzip_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tens
     _expect(h, torch.bfloat16, shape, "h")
     gate = up = None
     if keep is True:
-        gate, up = torch.empty_like(h), torch.empty_like(h)
+        gate, up = (torch.empty(shape, dtype=torch.float32, device=x.device) for _ in range(2))
     elif keep:
         gate, up = keep
-        _expect(gate, torch.bfloat16, shape, "gate")
-        _expect(up, torch.bfloat16, shape, "up")
+        _expect(gate, torch.float32, shape, "gate")
+        _expect(up, torch.float32, shape, "up")
     rc = _lib.neuzip_gated_forward(_pointer(x), _pointer(w_gate), _pointer(w_up), tokens, out_features, in_features, activation,
                                    _pointer(h), _pointer(gate), _pointer(up), _stream_handle(stream))
     if rc != OK:
@@ -603,8 +603,8 @@ def neuzip_gated_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Ten
     """(grad_x, grad_w_gate, grad_w_up), bf16.  grad_x and grad_weights: True, False (not wanted: None), or the tensor and the pair
     of tensors that receive them."""
     tokens, out_features, in_features = _gated_shape(x, w_gate, w_up)
-    for t, what in ((gate, "gate"), (up, "up"), (grad_h, "grad_h")):
-        _expect(t, torch.bfloat16, (tokens, out_features), what)
+    for t, dtype, what in ((gate, torch.float32, "gate"), (up, torch.float32, "up"), (grad_h, torch.bfloat16, "grad_h")):
+        _expect(t, dtype, (tokens, out_features), what)
     if grad_x is True:
         grad_x = torch.empty((tokens, in_features), dtype=torch.bfloat16, device=x.device)
     elif grad_x is False:

@@ -88,7 +88,7 @@ inline uint64_t wgs_for(uint64_t threads) { return (threads + kGatedSlopeThreads
 extern "C" {
 
 int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, uint64_t tokens,
-                         uint64_t out_features, uint64_t in_features, int activation, void *d_h, void *d_gate, void *d_up,
+                         uint64_t out_features, uint64_t in_features, int activation, void *d_h, float *d_gate, float *d_up,
                          void *hip_stream)
 {
     if (!valid_activation(activation) || !valid_width(out_features) || !valid_width(in_features) || tokens >= kGatedMostTokens)
@@ -97,7 +97,8 @@ int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void 
         return NEUZIP_OK;
     if (!d_x || !d_gate_weight || !d_up_weight || !d_h || !d_gate != !d_up)
         return NEUZIP_EINVAL;
-    for (const void *p : {d_x, d_gate_weight, d_up_weight, static_cast<const void *>(d_h), static_cast<const void *>(d_gate), static_cast<const void *>(d_up)})
+    const void *const pointers[] = {d_x, d_gate_weight, d_up_weight, d_h, d_gate, d_up};
+    for (const void *p : pointers)
         if (misaligned(p))
             return NEUZIP_EINVAL;
     GatedArgs a;
@@ -106,8 +107,8 @@ int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void 
     a.p[0] = static_cast<const uint16_t *>(d_gate_weight);
     a.p[1] = static_cast<const uint16_t *>(d_up_weight);
     a.c[0] = static_cast<uint16_t *>(d_h);
-    a.gate = static_cast<uint16_t *>(d_gate);
-    a.up = static_cast<uint16_t *>(d_up);
+    a.gate = d_gate;
+    a.up = d_up;
     a.rows = static_cast<uint32_t>(tokens);
     a.cols = a.c_row = static_cast<uint32_t>(out_features);
     a.depth = a.q_row = a.p_row = static_cast<uint32_t>(in_features);
@@ -123,7 +124,7 @@ uint64_t neuzip_gated_backward_scratch_bytes(uint64_t tokens, uint64_t out_featu
     return 2 * pad_to(tokens * out_features * 2, 256) + (shape.slices > 1 ? shape.slices * tokens * in_features * sizeof(float) : 0);
 }
 
-int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, const void *d_gate, const void *d_up,
+int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, const float *d_gate, const float *d_up,
                           const void *d_grad_h, uint64_t tokens, uint64_t out_features, uint64_t in_features, int activation,
                           void *d_grad_x, void *d_grad_gate_weight, void *d_grad_up_weight, void *d_scratch, uint64_t scratch_bytes,
                           void *hip_stream)
@@ -136,9 +137,8 @@ int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void
     if (tokens > 0 && (!d_gate || !d_up || !d_grad_h || !d_scratch || (weights && !d_x) || (d_grad_x && (!d_gate_weight || !d_up_weight)) ||
                        scratch_bytes < neuzip_gated_backward_scratch_bytes(tokens, out_features, in_features)))
         return NEUZIP_EINVAL;
-    for (const void *p : {d_x, d_gate_weight, d_up_weight, d_gate, d_up, d_grad_h, static_cast<const void *>(d_grad_x),
-                          static_cast<const void *>(d_grad_gate_weight), static_cast<const void *>(d_grad_up_weight),
-                          static_cast<const void *>(d_scratch)})
+    const void *const pointers[] = {d_x, d_gate_weight, d_up_weight, d_gate, d_up, d_grad_h, d_grad_x, d_grad_gate_weight, d_grad_up_weight, d_scratch};
+    for (const void *p : pointers)
         if (misaligned(p))
             return NEUZIP_EINVAL;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -150,7 +150,7 @@ int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void
         if (wgs_for(pieces) >= (1ull << 31))
             return NEUZIP_EUNSUPPORTED;
         hipLaunchKernelGGL(gated_slope_kernel, dim3(static_cast<uint32_t>(wgs_for(pieces))), dim3(kGatedSlopeThreads), 0, stream,
-                           static_cast<const uint4 *>(d_gate), static_cast<const uint4 *>(d_up), static_cast<const uint4 *>(d_grad_h),
+                           reinterpret_cast<const float4 *>(d_gate), reinterpret_cast<const float4 *>(d_up), static_cast<const uint4 *>(d_grad_h),
                            reinterpret_cast<uint4 *>(dg), reinterpret_cast<uint4 *>(du), pieces, static_cast<uint32_t>(activation));
         if (!hip_ok(hipGetLastError()))
             return NEUZIP_EHIP;

@@ -23,7 +23,7 @@ struct GatedArgs {
     const uint16_t *q[2];   // kForward: x, x;  kInputGrad: dg, du;  kWeightGrad: dg, du
     const uint16_t *p[2];   // Wg, Wu;  Wg, Wu;  x, x
     uint16_t *c[2];         // h, -;  dx, -;  dWg, dWu
-    uint16_t *gate, *up;    // kForward: the two sums, for the backward pass (nullptr: they are not kept)
+    float *gate, *up;       // kForward: the two sums, for the backward pass (nullptr: they are not kept)
     float *partial;         // kInputGrad, several slices: the sums of a slice leave as they are, to partial[slice][i][j]
     uint32_t rows;          // i: tokens, tokens, out_features
     uint32_t cols;          // j: out_features, in_features, in_features
@@ -394,16 +394,20 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
                 *reinterpret_cast<uint4 *>(c + static_cast<uint64_t>(i) * a.c_row + j) = make_uint4(at[t][0], at[t][1], at[t][2], at[t][3]);
         }
     };
+    // (in binary32 four neighbouring j are 16 bytes, and a wave's store 64 of each row as it is)
+    auto leave_sum = [&](float *c, const gated_f32x4_t &v, int jt, int it) {
+        const uint32_t i = i_lane + it * 16, j = j0 + wj * (kOutputs * 16) + jt * 16 + lane / 16 * 4;
+        if (i < a.rows && j < a.cols)
+            *reinterpret_cast<float4 *>(c + static_cast<uint64_t>(i) * a.c_row + j) = make_float4(v[0], v[1], v[2], v[3]);
+    };
     if (FORM == kInputGrad && a.partial) {
+        float *c = a.partial + static_cast<uint64_t>(slice) * a.rows * a.c_row;
 #pragma unroll
         for (int jt = 0; jt < TILES; ++jt)
 #pragma unroll
             for (int it = 0; it < TILES; ++it) {
-                const uint32_t i = i_lane + it * 16, j = j0 + wj * (SIZE / 2) + jt * 16 + lane / 16 * 4;
                 asm volatile("" : "+a"(acc[jt][it]));  // (see below)
-                const gated_f32x4_t v = acc[jt][it];
-                if (i < a.rows && j < a.cols)
-                    *reinterpret_cast<float4 *>(a.partial + (static_cast<uint64_t>(slice) * a.rows + i) * a.c_row + j) = make_float4(v[0], v[1], v[2], v[3]);
+                leave_sum(c, acc[jt][it], jt, it);
             }
         return;
     }
@@ -423,8 +427,11 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
                 };
                 leave(a.c[0], jt, it, products);
                 if (a.gate) {
-                    leave(a.gate, jt, it, sums);
-                    leave(a.up, jt, it, [&](int j, int i, int e) { return sums(j + TILES / 2, i, e); });
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        leave_sum(a.gate, acc[jt + t % 2][it + t / 2], jt + t % 2, it + t / 2);
+                        leave_sum(a.up, acc[jt + t % 2 + TILES / 2][it + t / 2], jt + t % 2, it + t / 2);
+                    }
                 }
             } else {
                 leave(half ? a.c[1] : a.c[0], jt, it, sums);
@@ -433,26 +440,29 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     }
 }
 
-// dg = dh * u * act'(g), du = dh * act(g), each rounded to bf16 once, 8 elements to a thread.
+// dg = dh * u * act'(g), du = dh * act(g), each rounded to bf16 once (the matrix cores take bf16; with g and u rounded before, the
+// gradients were off by 3.1e-3 in the mean, 2.4e-3 now, of which the roundings of the results are 1.7e-3), 8 elements to a thread.
 // act'(g) = s + g s (1 - s) z'(g), s = sigmoid(z(g)); z' of the GELU grows with g^2, where s (1 - s) has long been zero.
+// Bound by memory: 14 bytes an element (2048 x 14336: see the figures of the backward pass).
 constexpr uint32_t kGatedSlopeThreads = 256;
-__global__ __launch_bounds__(kGatedSlopeThreads) void gated_slope_kernel(const uint4 *__restrict__ gate, const uint4 *__restrict__ up,
+__global__ __launch_bounds__(kGatedSlopeThreads) void gated_slope_kernel(const float4 *__restrict__ gate, const float4 *__restrict__ up,
                                                                          const uint4 *__restrict__ grad_h, uint4 *__restrict__ dg,
                                                                          uint4 *__restrict__ du, uint64_t pieces, uint32_t activation)
 {
     const uint64_t at = static_cast<uint64_t>(blockIdx.x) * kGatedSlopeThreads + threadIdx.x;
     if (at >= pieces)
         return;
-    const uint4 g4 = gate[at], u4 = up[at], h4 = grad_h[at];
-    const uint32_t gs[4] = {g4.x, g4.y, g4.z, g4.w}, us[4] = {u4.x, u4.y, u4.z, u4.w}, hs[4] = {h4.x, h4.y, h4.z, h4.w};
+    const float4 g0 = gate[2 * at], g1 = gate[2 * at + 1], u0 = up[2 * at], u1 = up[2 * at + 1];
+    const uint4 h4 = grad_h[at];
+    const float gs[8] = {g0.x, g0.y, g0.z, g0.w, g1.x, g1.y, g1.z, g1.w}, us[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
+    const uint32_t hs[4] = {h4.x, h4.y, h4.z, h4.w};
     uint32_t dgs[4], dus[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float dgv[2], duv[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const float g = __uint_as_float(e ? gs[i] & 0xFFFF0000u : gs[i] << 16);
-            const float u = __uint_as_float(e ? us[i] & 0xFFFF0000u : us[i] << 16);
+            const float g = gs[2 * i + e], u = us[2 * i + e];
             const float h = __uint_as_float(e ? hs[i] & 0xFFFF0000u : hs[i] << 16);
             const float s = gated_sigmoid(gated_argument(g, activation));
             const float slope = activation ? kGeluScale * (1.0f + 0.134145f * fminf(g * g, 1e4f)) : 1.0f;

@@ -4,7 +4,7 @@ Products of bf16 words are exact and sums are binary32: a sum of n terms in any 
 magnitudes.  sigmoid(z) = 1 / (1 + exp(-z)) is taken with the hardware's exponential and reciprocal: exp(-z) is 2^(-z log2 e), whose
 argument is rounded (2^-24 of it) and doubles as a relative error of the power, and both instructions are good to a unit or two in the
 last place, so 2^-20 + |z| * 2^-23 of the value is ample.  A result in bf16 has a rounding of 2^-8 at most on top of that.  The backward pass
-takes g and u as bf16 words and rounds dg and du to bf16 (2^-8 each) before the matrix cores take them.
+rounds dg and du to bf16 (2^-8 each) before the matrix cores take them.
 """
 import math
 
@@ -27,10 +27,10 @@ def nz():
     return binding
 
 
-def guarded(shape, fill=7.0):
-    """A bf16 tensor with GUARD elements on either side that nobody may touch."""
+def guarded(shape, dtype=torch.bfloat16):
+    """A tensor with GUARD elements on either side that nobody may touch."""
     n = int(np.prod(shape))
-    whole = torch.full((n + 2 * GUARD,), fill, dtype=torch.bfloat16, device=DEV)
+    whole = torch.full((n + 2 * GUARD,), 7.0, dtype=dtype, device=DEV)
     return whole, whole[GUARD:GUARD + n].view(shape)
 
 
@@ -117,7 +117,8 @@ def test_serving_on_a_stream_of_its_own_and_in_a_graph(nz):
     nz.neuzip_gated_linear(gate, up, outfeat, infeat, x, nz.SILU, h, stream=second)
     torch.cuda.synchronize()
     check_h(h, *products(x, wg, wu), 0, infeat)
-    h2, g2, u2 = (torch.empty_like(h) for _ in range(3))
+    h2 = torch.empty_like(h)
+    g2, u2 = (torch.empty((tokens, outfeat), device=DEV) for _ in range(2))
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         nz.neuzip_gated_linear(gate, up, outfeat, infeat, x, nz.SILU, h)
@@ -145,15 +146,14 @@ SHAPES = [(1, 8, 8), (3, 40, 16), (1, 1024, 512), (17, 200, 136), (64, 64, 64), 
 @pytest.mark.parametrize("tokens,infeat,outfeat", SHAPES)
 def test_forward(nz, tokens, infeat, outfeat, act):
     x, wg, wu = data(tokens, infeat, outfeat, 9200 + tokens, std=1.5 / math.sqrt(infeat))
-    wholes, (h, gate, up) = zip(*[guarded((tokens, outfeat)) for _ in range(3)])
+    wholes, (h, gate, up) = zip(*[guarded((tokens, outfeat), dtype) for dtype in (torch.bfloat16, torch.float32, torch.float32)])
     nz.neuzip_gated_forward(x, wg, wu, act, h, keep=(gate, up))
     torch.cuda.synchronize()
     assert untouched(*wholes)
     g, u, g_size, u_size = products(x, wg, wu)
     check_h(h, g, u, g_size, u_size, act, infeat)
     for kept, want, size in ((gate, g, g_size), (up, u, u_size)):
-        off = (infeat + 64) * EPS * size
-        assert bool(((kept.double() - want).abs() <= off + BF * (want.abs() + off) + 1e-30).all())
+        assert bool(((kept.double() - want).abs() <= (infeat + 64) * EPS * size + 1e-30).all())
     assert torch.equal(nz.neuzip_gated_forward(x, wg, wu, act), h)
 
 
@@ -161,7 +161,7 @@ def test_forward(nz, tokens, infeat, outfeat, act):
 @pytest.mark.parametrize("tokens,infeat,outfeat", SHAPES)
 def test_backward(nz, tokens, infeat, outfeat, act):
     x, wg, wu = data(tokens, infeat, outfeat, 9300 + tokens, std=1.5 / math.sqrt(infeat))
-    gate, up = (inputs.gaussian_bf16((tokens, outfeat), 9310 + i, std=1.5, device=DEV) for i in range(2))
+    gate, up = (inputs.gaussian_f32((tokens, outfeat), 9310 + i, std=1.5, device=DEV) for i in range(2))
     grad_h = inputs.gaussian_bf16((tokens, outfeat), 9320, std=0.1, device=DEV)
     whole_x, grad_x = guarded((tokens, infeat))
     whole_g, grad_g = guarded((outfeat, infeat))
@@ -225,7 +225,7 @@ def test_large_and_infinite_values(nz, act):
     ones[:, n - 1] = 1.0
     x[:, n - 1] = 1.0       # (u = 1)
     h, gate, up = nz.neuzip_gated_forward(x, eye, ones, act, keep=True)
-    assert torch.equal(gate, x) and bool((up == 1).all())
+    assert torch.equal(gate, x.float()) and bool((up == 1).all())
     want = torch.where(x.double() > 50, x.double(), torch.where(x.double() < -50, torch.zeros_like(x.double()), value(x.double(), act)))
     assert bool(((h.double() - want).abs() <= BF * want.abs() * 1.01 + 1e-38).all())
     grad_h = torch.ones_like(h)
@@ -261,7 +261,7 @@ def test_gradients_against_differences(nz, act):
             moved[which][row, col] += sign * step
             ends.append(loss(moved))
         difference = (ends[0] - ends[1]) / (2 * step)
-        # (g, u, dg and du are bf16 words: each term of the sum is off by 2^-8 of itself, some four times)
+        # (dg and du are bf16 words, and so is the gradient: each term of the sum is off by 2^-8 of itself, and the sum too)
         assert abs(difference - float(grads[which][row, col])) <= 6 * BF * scale[which]
 
 

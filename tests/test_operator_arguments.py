@@ -54,13 +54,13 @@ def gated_linear(x=Stub((TOKENS, IN)), h=Stub((TOKENS, OUT)), scratch=SCRATCH):
 
 
 def gated_forward(x=Stub((TOKENS, IN)), w_gate=Stub((OUT, IN)), w_up=Stub((OUT, IN)), h=Stub((TOKENS, OUT)),
-                  keep=(Stub((TOKENS, OUT)), Stub((TOKENS, OUT)))):
+                  keep=(Stub((TOKENS, OUT), F32), Stub((TOKENS, OUT), F32))):
     nz.neuzip_gated_forward(x, w_gate, w_up, nz.SILU, h, keep)
 
 
-def gated_backward(x=Stub((TOKENS, IN)), w_gate=Stub((OUT, IN)), gate=Stub((TOKENS, OUT)), grad_h=Stub((TOKENS, OUT)),
+def gated_backward(x=Stub((TOKENS, IN)), w_gate=Stub((OUT, IN)), gate=Stub((TOKENS, OUT), F32), grad_h=Stub((TOKENS, OUT)),
                    grad_x=Stub((TOKENS, IN)), grad_weights=(Stub((OUT, IN)), Stub((OUT, IN))), scratch=SCRATCH):
-    nz.neuzip_gated_backward(x, w_gate, Stub((OUT, IN)), gate, Stub((TOKENS, OUT)), grad_h, nz.SILU, grad_x, grad_weights, scratch)
+    nz.neuzip_gated_backward(x, w_gate, Stub((OUT, IN)), gate, Stub((TOKENS, OUT), F32), grad_h, nz.SILU, grad_x, grad_weights, scratch)
 
 
 def adapters(x=Stub((TOKENS, IN)), a=Stub((ADAPTERS, RANK, IN)), b=Stub((ADAPTERS, OUT, RANK)), scales=Stub((ADAPTERS,), F32),
@@ -73,7 +73,7 @@ CALLS = {
     embedding_grad: dict(tokens=((TOKENS,), I64), grad_out=((TOKENS, IN), BF), grad=((ROWS, IN), BF)),
     gated_linear: dict(x=((TOKENS, IN), BF), h=((TOKENS, OUT), BF)),
     gated_forward: dict(x=((TOKENS, IN), BF), w_gate=((OUT, IN), BF), w_up=((OUT, IN), BF), h=((TOKENS, OUT), BF)),
-    gated_backward: dict(x=((TOKENS, IN), BF), w_gate=((OUT, IN), BF), gate=((TOKENS, OUT), BF), grad_h=((TOKENS, OUT), BF),
+    gated_backward: dict(x=((TOKENS, IN), BF), w_gate=((OUT, IN), BF), gate=((TOKENS, OUT), F32), grad_h=((TOKENS, OUT), BF),
                          grad_x=((TOKENS, IN), BF)),
     adapters: dict(x=((TOKENS, IN), BF), a=((ADAPTERS, RANK, IN), BF), b=((ADAPTERS, OUT, RANK), BF), scales=((ADAPTERS,), F32),
                    ids=((TOKENS,), I32), bias=((OUT,), F32), y=((TOKENS, OUT), F32)),
