@@ -351,7 +351,7 @@ uint64_t neuzip_linear_scratch_bytes(const uint64_t *out_features, uint32_t coun
  *   scale      the product is formed in binary32 and rounded once, to nearest even; with scale = 1 every word leaves as it is.
  *   d_out      count x features bf16 words, row-major, 16-byte aligned; overwritten.
  * count = 0 is a call that does nothing.  Never allocates, never synchronises; a malformed stream is reported by neuzip_check
- * where a row ends with its chunk.  More than 2^31 - 1 pieces of rows (a row has one, two, or one more than the chunks that it is long) -> EUNSUPPORTED.
+ * where a row ends with its chunk.  2^27 pieces of rows and more (a piece lies in one chunk, or half of one) -> EUNSUPPORTED.
  */
 int neuzip_embedding(const neuzip_blob *table, uint64_t rows, uint64_t features, const int64_t *d_tokens, uint64_t count, float scale,
                      void *d_out, void *hip_stream);
@@ -399,7 +399,7 @@ uint64_t neuzip_gated_linear_scratch_bytes(uint64_t out_features, uint64_t in_fe
  *
  *   d_x               tokens x in_features bf16 words, row-major, like all matrices here.
  *   d_gate_weight, d_up_weight   out_features x in_features bf16 words.
- *   in_features, out_features    multiples of 8, at most 2^22; tokens below 2^31, also 0.
+ *   in_features, out_features    multiples of 8, at most 2^22; tokens below 2^31, also 0; tokens x features from about 2^35 on -> EUNSUPPORTED.
  *   d_h               tokens x out_features bf16 words; overwritten.
  *   d_gate, d_up      NULL, or room for g and u (floats, as many as d_h has words), which the backward pass takes; both or neither.
  *   d_grad_h          tokens x out_features bf16 words.

@@ -23,7 +23,7 @@ int launch_low(const LinearInitArgs &init, uint32_t wgs, const void *context, hi
 {
     const AdapterArgs &g = *static_cast<const AdapterArgs *>(context);
     const uint64_t low_wgs = static_cast<uint64_t>((g.rank + kAdapterRows - 1) / kAdapterRows) * g.tokens;
-    if (wgs + low_wgs >= (1ull << 31))
+    if (too_many_wgs(wgs + low_wgs, kAdapterThreads))
         return NEUZIP_EUNSUPPORTED;
     hipLaunchKernelGGL(adapter_low_kernel, dim3(static_cast<uint32_t>(wgs + low_wgs)), dim3(kAdapterThreads), 0, stream, init, wgs, g);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;

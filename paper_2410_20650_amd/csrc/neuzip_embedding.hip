@@ -51,7 +51,7 @@ int neuzip_embedding(const neuzip_blob *table, uint64_t rows, uint64_t features,
     // units of a token: as many as a row's elements can touch
     const uint64_t unit = has_entry_points(table->n_chunks) ? kMidTurn * kTurn : kChunk;
     const uint64_t per_token = unit % features == 0 ? 1 : (features % unit == 0 ? features / unit : (features - 1) / unit + 2);
-    if (count >= (1ull << 31) || count * per_token >= (1ull << 31))
+    if (count >= (1ull << 27) || count * per_token >= (1ull << 27))  // (16 threads to each, of fewer than 2^32)
         return NEUZIP_EUNSUPPORTED;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const int behind = follow(table, stream);

@@ -69,7 +69,7 @@ int launch_gated(GatedArgs &a, const GatedShape &shape, hipStream_t stream)
     a.tiles_j = tiles_of(a.cols, FORM == kForward ? shape.size / 2 : shape.size);
     a.slices = shape.slices;
     const uint64_t grid = static_cast<uint64_t>(a.tiles_i) * a.tiles_j * shape.slices * (FORM == kWeightGrad ? 2 : 1);
-    if (grid >= (1ull << 31))
+    if (too_many_wgs(grid, kGatedThreads))
         return NEUZIP_EUNSUPPORTED;
     const dim3 wgs(static_cast<uint32_t>(grid)), threads(kGatedThreads);
     if (shape.size == 256)
@@ -145,10 +145,10 @@ int neuzip_gated_backward(const void *d_x, const void *d_gate_weight, const void
     uint16_t *dg = static_cast<uint16_t *>(d_scratch);
     uint16_t *du = dg + pad_to(tokens * out_features * 2, 256) / 2;
     float *partial = reinterpret_cast<float *>(du + pad_to(tokens * out_features * 2, 256) / 2);
+    if (too_many_wgs(wgs_for(tokens * out_features / 8), kGatedSlopeThreads) || too_many_wgs(wgs_for(tokens * in_features / 8), kGatedSlopeThreads))
+        return NEUZIP_EUNSUPPORTED;
     if (tokens > 0) {
         const uint64_t pieces = tokens * out_features / 8;
-        if (wgs_for(pieces) >= (1ull << 31))
-            return NEUZIP_EUNSUPPORTED;
         hipLaunchKernelGGL(gated_slope_kernel, dim3(static_cast<uint32_t>(wgs_for(pieces))), dim3(kGatedSlopeThreads), 0, stream,
                            reinterpret_cast<const float4 *>(d_gate), reinterpret_cast<const float4 *>(d_up), static_cast<const uint4 *>(d_grad_h),
                            reinterpret_cast<uint4 *>(dg), reinterpret_cast<uint4 *>(du), pieces, static_cast<uint32_t>(activation));
@@ -211,7 +211,7 @@ int neuzip_gated_linear(const neuzip_blob *gate, const neuzip_blob *up, uint64_t
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint64_t count = tokens * out_features, each = pad_to(count * sizeof(float), 256);
     const uint64_t wgs = wgs_for((count + 3) / 4);
-    if (wgs >= (1ull << 31))
+    if (too_many_wgs(wgs, kGatedSlopeThreads))
         return NEUZIP_EUNSUPPORTED;
     float *const sums[2] = {static_cast<float *>(d_scratch), static_cast<float *>(d_scratch) + each / sizeof(float)};
     const neuzip_blob *const weights[2] = {gate, up};

@@ -26,14 +26,14 @@ inline bool hip_ok(hipError_t e)
             return NEUZIP_EHIP;      \
     } while (0)
 
+// A launch's threads in one dimension are fewer than 2^32.
+constexpr bool too_many_wgs(uint64_t wgs, uint32_t threads) { return wgs >= (1ull << 32) / threads; }
+
 constexpr uint64_t pad_to(uint64_t v, uint64_t a) { return (v + a - 1) / a * a; }
 inline bool valid_k(int k) { return k == 7 || k == 3 || k == 1 || k == 0; }
 inline uint64_t signmant_bytes(uint64_t n, int k) { return (n * static_cast<uint64_t>(k + 1) + 7) / 8; }
 inline uint32_t chunks_of(uint64_t n) { return static_cast<uint32_t>((n + kChunk - 1) / kChunk); }
 
-// ------------------------------------------------------------------------------------------
-// Host side
-// ------------------------------------------------------------------------------------------
 inline bool valid_block(uint32_t b) { return b == 32 || b == 64 || b == 128 || b == 256 || b == 512; }
 inline uint64_t block_count(uint64_t n, uint32_t block) { return block ? (n + block - 1) / block : 0; }
 
