@@ -492,8 +492,11 @@ def _own_scratch(size, scratch, device, stream):
         return scratch
     if stream is not None and isinstance(stream, torch.cuda.Stream):
         with torch.cuda.stream(stream):
-            return torch.empty(size, dtype=torch.uint8, device=device)
-    return torch.empty(size, dtype=torch.uint8, device=device)
+            return _own_scratch(size, None, device, None)
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(size, dtype=torch.uint8, device=device)
+    with _OutsideOfCaptures():
+        return torch.empty(size, dtype=torch.uint8, device=device)
 
 
 def _bytes_of(t):
