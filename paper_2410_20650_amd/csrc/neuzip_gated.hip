@@ -30,7 +30,7 @@ struct GatedShape {
 
 // Tiles of 256 or of 128, and for the input gradient, whose tiles are few and their sums long, how many slices of k: the least of
 // what the forms are expected to take, in us, with tiles in rounds of as many as the CUs have places for.
-//   256             1.7 a step of 64 k and 9 a tile, 256 places  (2048 tokens, 4096 -> 14336, weight gradients: 480; forward 1000 tokens 204)
+//   256             1.7 a step of 64 k and 9 a tile, 256 places  (2048 tokens, 4096 -> 14336, weight gradients: 426 to 480; forward 1000 tokens 188)
 //   128             1.1 and 4, 512 places                        (576; 288)
 //   128, four steps held, no more tiles than CUs: 0.63 and 5     (input gradient, 1000 tokens, unsliced: 283, with two held 380; forward of 200
 //                   tokens, 4096 -> 4096, 30.8 / 42.8, of one, 4096 -> 14336, 36.2 / 45.2; beyond a round the two of a CU are the faster ones,

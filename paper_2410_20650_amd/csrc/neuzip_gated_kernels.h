@@ -172,8 +172,11 @@ struct GatedOperand {
 
 // Launch shape: tiles of SIZE i by SIZE j, four waves of SIZE / 2 by SIZE / 2.
 constexpr uint32_t kGatedWaves = 4, kGatedThreads = kGatedWaves * 64;
-// RING: the steps that LDS holds.  Two are 128 KB for a tile of 256, or 64 KB for one of 128, of which two share a CU.  Where there are
-// fewer of those than CUs, nothing else hides the wait for memory, and four are held.
+// RING: the steps that LDS holds.  Two are 128 KB for a tile of 256, or 64 KB for one of 128, of which two share a CU; what is left of
+// the 160 KB goes to a third step of the operand for j, the weights or x, whose requests then have a step more to arrive (forward of
+// 600 and 1000 tokens, 4096 -> 14336, 193 / 167 and 196 / 188 us, input gradient of 1500, 4096 -> 11008, 324 / 304; the gradients in tiles of
+// 128 are as fast without or faster, 64 tokens 49.4 / 52.1).  Where there are fewer tiles of 128 than CUs, nothing else hides the wait for
+// memory, and four are held.
 template <GatedForm FORM, int SIZE, int RING>
 __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) void gated_kernel(const GatedArgs a)
 {
@@ -183,8 +186,9 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     typedef GatedOperand<SIZE, WAVES, Q_ALONG> Q;
     typedef GatedOperand<SIZE, WAVES, P_ALONG> P;
     typedef GatedOperand<SIZE / 2, WAVES, true> Half;  // kForward: the rows of one weight
-    constexpr uint32_t kStage = Q::kBytes + P::kBytes;
-    __shared__ __align__(16) uint8_t lds[RING * kStage];
+    constexpr uint32_t kQRing = RING, kPRing = RING == 2 && (SIZE == 256 || FORM == kForward) ? 3 : RING;
+    constexpr uint32_t kQEnd = kQRing * Q::kBytes, kPEnd = kQEnd + kPRing * P::kBytes;
+    __shared__ __align__(16) uint8_t lds[kPEnd];
 
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / 64)));
@@ -230,40 +234,65 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds));
     const uint64_t q_step = static_cast<uint64_t>(kGatedDepth) * (Q_ALONG ? 1u : a.q_row) * 2;
     const uint64_t p_step = static_cast<uint64_t>(kGatedDepth) * (P_ALONG ? 1u : a.p_row) * 2;
-    uint32_t ahead = s_begin, left = 0;     // its number, and the k from its first on
+    // (their numbers, and the k from their first on)
+    uint32_t q_ahead = s_begin, p_ahead = s_begin, q_left = 0, p_left = 0;
     const uint8_t *q_at = nullptr, *p_at = nullptr, *p_other = nullptr;
-    auto seek = [&](uint32_t s) {
-        const bool second = FORM == kInputGrad ? s >= half_steps : half != 0;
-        const uint32_t in_half = FORM == kInputGrad && second ? s - half_steps : s;
-        q_at = (second ? q_base[1] : q_base[0]) + in_half * q_step - kGatedBias;
-        p_at = (second ? p_base[1] : p_base[0]) + in_half * p_step - kGatedBias;
-        if constexpr (FORM == kForward)
-            p_other = p_base[1] + in_half * p_step - kGatedBias;
-        left = a.depth - in_half * kGatedDepth;
+    auto in_half = [&](uint32_t s) { return FORM == kInputGrad && s >= half_steps ? s - half_steps : s; };
+    auto in_second = [&](uint32_t s) { return FORM == kInputGrad ? s >= half_steps : half != 0; };
+    auto seek_q = [&]() {
+        q_at = (in_second(q_ahead) ? q_base[1] : q_base[0]) + in_half(q_ahead) * q_step - kGatedBias;
+        q_left = a.depth - in_half(q_ahead) * kGatedDepth;
     };
-    auto request_copy = [&](auto ragged, auto number) {
+    auto seek_p = [&]() {
+        p_at = (in_second(p_ahead) ? p_base[1] : p_base[0]) + in_half(p_ahead) * p_step - kGatedBias;
+        if constexpr (FORM == kForward)
+            p_other = p_base[1] + p_ahead * p_step - kGatedBias;
+        p_left = a.depth - in_half(p_ahead) * kGatedDepth;
+    };
+    auto request_q = [&](auto ragged, auto number, uint32_t place) {
+        q.template request<decltype(ragged)::value, decltype(number)::value>(q_at, lds_at + place, wave, q_left);
+    };
+    auto request_p = [&](auto ragged, auto number, uint32_t place) {
         constexpr bool RAGGED = decltype(ragged)::value;
         constexpr uint32_t N = decltype(number)::value;
-        const uint32_t to = lds_at + (ahead - s_begin) % RING * kStage;
-        if constexpr (N < Q::kCopies)
-            q.template request<RAGGED, N>(q_at, to, wave, left);
-        else if constexpr (FORM != kForward)
-            p.template request<RAGGED, N - Q::kCopies>(p_at, to + Q::kBytes, wave, left);
-        else if constexpr (N < Q::kCopies + Half::kCopies)
-            half_p.template request<RAGGED, N - Q::kCopies>(p_at, to + Q::kBytes, wave, left);
+        if constexpr (FORM != kForward)
+            p.template request<RAGGED, N>(p_at, lds_at + place, wave, p_left);
+        else if constexpr (N < Half::kCopies)
+            half_p.template request<RAGGED, N>(p_at, lds_at + place, wave, p_left);
         else
-            half_p.template request<RAGGED, N - Q::kCopies - Half::kCopies>(p_other, to + Q::kBytes + Half::kBytes, wave, left);
+            half_p.template request<RAGGED, N - Half::kCopies>(p_other, lds_at + place + Half::kBytes, wave, p_left);
     };
-    auto advance = [&]() {
-        ++ahead;
+    auto advance_q = [&]() {
+        ++q_ahead;
         q_at += q_step;
+        q_left -= kGatedDepth;
+        if constexpr (FORM == kInputGrad)
+            if (q_ahead == half_steps)
+                seek_q();
+    };
+    auto advance_p = [&]() {
+        ++p_ahead;
         p_at += p_step;
         if constexpr (FORM == kForward)
             p_other += p_step;
-        left -= kGatedDepth;
+        p_left -= kGatedDepth;
         if constexpr (FORM == kInputGrad)
-            if (ahead == half_steps)
-                seek(ahead);
+            if (p_ahead == half_steps)
+                seek_p();
+    };
+    auto request_all_q = [&](uint32_t place) {
+        if (q_left >= kGatedDepth)
+            each_of<Q::kCopies>([&](auto n) { request_q(std::false_type{}, n, place); });
+        else
+            each_of<Q::kCopies>([&](auto n) { request_q(std::true_type{}, n, place); });
+        advance_q();
+    };
+    auto request_all_p = [&](uint32_t place) {
+        if (p_left >= kGatedDepth)
+            each_of<P::kCopies>([&](auto n) { request_p(std::false_type{}, n, place); });
+        else
+            each_of<P::kCopies>([&](auto n) { request_p(std::true_type{}, n, place); });
+        advance_p();
     };
     constexpr uint32_t kCopies = Q::kCopies + P::kCopies;
 
@@ -283,13 +312,13 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     struct Operands {
         gated_bf16x8_t q[TILES], p[TILES];
     };
-    auto read_q = [&](Operands &o, const uint8_t *tile, int n, uint32_t h) { o.q[n] = Q::read(tile, q_lane, n, h); };
-    auto read_p = [&](Operands &o, const uint8_t *tile, int n, uint32_t h) {
+    auto read_q = [&](Operands &o, uint32_t place, int n, uint32_t h) { o.q[n] = Q::read(lds + place, q_lane, n, h); };
+    auto read_p = [&](Operands &o, uint32_t place, int n, uint32_t h) {
         // (kForward: the second half of the sums are the other weight's)
         if constexpr (FORM == kForward)
-            o.p[n] = P::read(tile + Q::kBytes + (n >= TILES / 2 ? Half::kBytes : 0), p_lane, n % (TILES / 2), h);
+            o.p[n] = P::read(lds + place + (n >= TILES / 2 ? Half::kBytes : 0), p_lane, n % (TILES / 2), h);
         else
-            o.p[n] = P::read(tile + Q::kBytes, p_lane, n, h);
+            o.p[n] = P::read(lds + place, p_lane, n, h);
     };
     static_assert(kCopies == 2 * TILES, "two copies to a row of sums");
     // the next step has come, and everyone holds this one in registers; `pass` copies that were requested later may still travel
@@ -297,68 +326,87 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
         asm volatile("s_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"v"(lds), "n"(decltype(pass)::value) : "memory");
     };
     constexpr std::integral_constant<uint32_t, 0> kNone{};
-    constexpr std::integral_constant<uint32_t, (RING - 2) * kCopies> kLater{};
-    static_assert(kLater.value < 64, "as many as the counter counts");
+    constexpr std::integral_constant<uint32_t, (kQRing - 2) * kCopies + (kPRing - kQRing) * P::kCopies> kLater{};
+    constexpr std::integral_constant<uint32_t, (kQRing - 1) * Q::kCopies + (kPRing - 1) * P::kCopies> kOthers{};  // than the first step's
+    static_assert(kLater.value < 64 && kOthers.value < 64, "as many as the counter counts");
     // (what is not a product stands by itself between products, in their shadow)
-    auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
+    auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, uint32_t h,
+                           uint32_t q_to, uint32_t p_to) {
         constexpr int n = decltype(number)::value, kEach = TILES / 4;
         auto some = [&](int from) {
 #pragma unroll
             for (int it = from * kEach; it < (from + 1) * kEach; ++it)
                 acc[n][it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.p[n], now.q[it], acc[n][it], 0, 0, 0);
         };
+        auto request = [&](auto copy) {
+            constexpr uint32_t N = decltype(copy)::value;
+            if constexpr (N < Q::kCopies)
+                request_q(std::false_type{}, copy, q_to);
+            else
+                request_p(std::false_type{}, std::integral_constant<uint32_t, N - Q::kCopies>{}, p_to);
+        };
         some(0);
-        read_q(then, tile, n, h);
+        read_q(then, q_place, n, h);
         __builtin_amdgcn_sched_barrier(0);
         some(1);
-        read_p(then, tile, n, h);
+        read_p(then, p_place, n, h);
         __builtin_amdgcn_sched_barrier(0);
         some(2);
         if constexpr (decltype(requests)::value)
-            request_copy(std::false_type{}, std::integral_constant<uint32_t, 2 * n>{});
+            request(std::integral_constant<uint32_t, 2 * n>{});
         __builtin_amdgcn_sched_barrier(0);
         some(3);
         if constexpr (decltype(requests)::value)
-            request_copy(std::false_type{}, std::integral_constant<uint32_t, 2 * n + 1>{});
+            request(std::integral_constant<uint32_t, 2 * n + 1>{});
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto half_step = [&](auto requests, const Operands &now, Operands &then, const uint8_t *tile, uint32_t h) {
-        each_of<TILES>([&](auto n) { row_of_sums(requests, n, now, then, tile, h); });
-    };
-    auto request_all = [&]() {
-        if (left >= kGatedDepth)
-            each_of<kCopies>([&](auto n) { request_copy(std::false_type{}, n); });
-        else
-            each_of<kCopies>([&](auto n) { request_copy(std::true_type{}, n); });
-        advance();
+    auto half_step = [&](auto requests, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, uint32_t h, uint32_t q_to = 0,
+                         uint32_t p_to = 0) {
+        each_of<TILES>([&](auto n) { row_of_sums(requests, n, now, then, q_place, p_place, h, q_to, p_to); });
     };
     if (steps > 0) {
         Operands first, second;
-        seek(s_begin);
-        for (uint32_t r = 0; r < RING && r < steps; ++r)
-            request_all();
-        arrive(kNone);
+        uint32_t q_now = 0, p_now = kQEnd;  // the step's places
+        auto after = [](uint32_t place, uint32_t bytes, uint32_t begin, uint32_t end) { return place + bytes == end ? begin : place + bytes; };
+        seek_q();
+        seek_p();
+        for (uint32_t r = 0; r < kPRing && r < steps; ++r) {
+            if (r < kQRing)
+                request_all_q(r * Q::kBytes);
+            request_all_p(kQEnd + r * P::kBytes);
+        }
+        if (steps >= kPRing)
+            arrive(kOthers);
+        else
+            arrive(kNone);
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
-            read_q(first, lds, n, 0);
-            read_p(first, lds, n, 0);
+            read_q(first, 0, n, 0);
+            read_p(first, kQEnd, n, 0);
         }
         for (uint32_t s = 0; s < steps;) {
-            while (s + RING < steps && left >= kGatedDepth) {
-                const uint8_t *tile = lds + s % RING * kStage, *next = lds + (s + 1) % RING * kStage;
-                half_step(std::false_type{}, first, second, tile, 1);
+            while (s + kPRing < steps && q_left >= kGatedDepth && p_left >= kGatedDepth) {
+                const uint32_t q_next = after(q_now, Q::kBytes, 0, kQEnd), p_next = after(p_now, P::kBytes, kQEnd, kPEnd);
+                half_step(std::false_type{}, first, second, q_now, p_now, 1);
                 arrive(kLater);
-                half_step(std::true_type{}, second, first, next, 0);
-                advance();
+                half_step(std::true_type{}, second, first, q_next, p_next, 0, q_now, p_now);
+                advance_q();
+                advance_p();
+                q_now = q_next;
+                p_now = p_next;
                 ++s;
             }
             // one by one: the last, and where half a sum ends
-            const uint8_t *tile = lds + s % RING * kStage, *next = lds + (s + 1) % RING * kStage;
-            half_step(std::false_type{}, first, second, tile, 1);
+            const uint32_t q_next = after(q_now, Q::kBytes, 0, kQEnd), p_next = after(p_now, P::kBytes, kQEnd, kPEnd);
+            half_step(std::false_type{}, first, second, q_now, p_now, 1);
             arrive(kNone);
-            if (s + RING < steps)
-                request_all();
-            half_step(std::false_type{}, second, first, next, 0);  // (behind the last step: what nobody uses)
+            if (s + kQRing < steps)
+                request_all_q(q_now);
+            if (s + kPRing < steps)
+                request_all_p(p_now);
+            half_step(std::false_type{}, second, first, q_next, p_next, 0);  // (behind the last step: what nobody uses)
+            q_now = q_next;
+            p_now = p_next;
             ++s;
         }
     }
