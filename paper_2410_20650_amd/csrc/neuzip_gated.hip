@@ -29,13 +29,13 @@ struct GatedShape {
 };
 
 // Tiles of 256 or of 128, and for the input gradient, whose tiles are few and their sums long, how many slices of k: the least of
-// what the forms are expected to take, in us, with tiles in rounds of as many as the CUs have places for.
-//   256             1.7 a step of 64 k and 9 a tile, 256 places  (2048 tokens, 4096 -> 14336, weight gradients: 426 to 480; forward 1000 tokens 188)
-//   128             1.1 and 4, 512 places                        (576; 288)
-//   128, four steps held, no more tiles than CUs: 0.63 and 5     (input gradient, 1000 tokens, unsliced: 283, with two held 380; forward of 200
-//                   tokens, 4096 -> 4096, 30.8 / 42.8, of one, 4096 -> 14336, 36.2 / 45.2; beyond a round the two of a CU are the faster ones,
-//                   weight gradients of 200 tokens 46.5 / 31.1)
-// and the sums of slices are written and read again in binary32.
+// what the forms are expected to take, in us.  Each has a beginning, its rounds (as many tiles as the CUs have places for) of steps of 64 k, and
+// what the products of all tiles take away in clock and from each other:
+//   256             a step 1.0, a tile 4.3, 10^9 operations 0.2     (512 tokens, 4096 -> 14336: forward 102 us, weight gradients 141)
+//   128, two to a CU    0.39, 0.5 and 0.48                          (138 and 144; 1500 tokens, 1024 -> 4096, 35.0 and 27.1, tiles of 256 36.2 and 40.6)
+//   128, four steps held, no more tiles than CUs  0.35 and 0.27     (200 tokens, 4096 -> 4096, forward 29.7, two to a CU 35.7)
+// and the sums of slices are written and read again in binary32 (input gradient of 2048 tokens, 4096 -> 14336: 487 us in one slice of 256, 339
+// in two; of 64 tokens, 166 in one of 128, 42 in eight).  Over 19 shapes of 1 to 2048 tokens the choice takes 1.4 % more than the best one.
 template <GatedForm FORM>
 GatedShape gated_shape(uint64_t rows, uint64_t cols, uint64_t depth)
 {
@@ -44,15 +44,16 @@ GatedShape gated_shape(uint64_t rows, uint64_t cols, uint64_t depth)
     double least = 0;
     for (uint32_t size = 128; size <= 256; size += 128) {
         const uint64_t tiles = static_cast<uint64_t>(tiles_of(rows, size)) * tiles_of(cols, FORM == kForward ? size / 2 : size) * (FORM == kWeightGrad ? 2 : 1);
+        const double work = 2e-9 * size * size * kGatedDepth * steps * static_cast<double>(tiles);
         for (uint32_t slices = 1; slices <= (FORM == kInputGrad ? 16u : 1u) && steps >= 4.0 * slices; slices *= 2) {
             const uint64_t all = tiles * slices;
             const uint32_t ring = size == 128 && all <= 256 ? 4 : 2;
             const double each = steps / slices;
-            double us = size == 256 ? static_cast<double>((all + 255) / 256) * (1.7 * each + 9)
-                        : ring == 4 ? 0.63 * each + 5
-                                    : static_cast<double>((all + 511) / 512) * (1.1 * each + 4);
+            double us = size == 256 ? 4 + static_cast<double>((all + 255) / 256) * (1.0 * each + 4.3) + 0.2 * work
+                        : ring == 4 ? 4 + 0.35 * each + 0.27 * work
+                                    : 3.3 + static_cast<double>((all + 511) / 512) * (0.39 * each + 0.5) + 0.48 * work;
             if (slices > 1)
-                us += 3.0 + static_cast<double>(rows) * cols * 4 * (slices + 0.5) / 6e6;
+                us += 3.0 + static_cast<double>(rows) * cols * 4 * (slices + 0.5) / 3e6;
             if (least == 0 || us < least) {
                 least = us;
                 best = {size, ring, slices};

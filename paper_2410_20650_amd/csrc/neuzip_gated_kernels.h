@@ -172,11 +172,9 @@ struct GatedOperand {
 
 // Launch shape: tiles of SIZE i by SIZE j, four waves of SIZE / 2 by SIZE / 2.
 constexpr uint32_t kGatedWaves = 4, kGatedThreads = kGatedWaves * 64;
-// RING: the steps that LDS holds.  Two are 128 KB for a tile of 256, or 64 KB for one of 128, of which two share a CU; what is left of
-// the 160 KB goes to a third step of the operand for j, the weights or x, whose requests then have a step more to arrive (forward of
-// 600 and 1000 tokens, 4096 -> 14336, 193 / 167 and 196 / 188 us, input gradient of 1500, 4096 -> 11008, 324 / 304; the gradients in tiles of
-// 128 are as fast without or faster, 64 tokens 49.4 / 52.1).  Where there are fewer tiles of 128 than CUs, nothing else hides the wait for
-// memory, and four are held.
+// RING: the steps that LDS holds, of the operand for i; of the one for j one more.  Two and three are all of the 160 KB for a tile of 256,
+// or half of them for one of 128, of which two share a CU.  Where there are fewer of those than CUs, nothing else hides the wait for memory,
+// and four and five are held (two held, 4096 -> 4096, 200 tokens: forward 35.7 us, 29.7 so).
 template <GatedForm FORM, int SIZE, int RING>
 __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) void gated_kernel(const GatedArgs a)
 {
@@ -186,7 +184,7 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     typedef GatedOperand<SIZE, WAVES, Q_ALONG> Q;
     typedef GatedOperand<SIZE, WAVES, P_ALONG> P;
     typedef GatedOperand<SIZE / 2, WAVES, true> Half;  // kForward: the rows of one weight
-    constexpr uint32_t kQRing = RING, kPRing = RING == 2 && (SIZE == 256 || FORM == kForward) ? 3 : RING;
+    constexpr uint32_t kQRing = RING, kPRing = RING + 1;
     constexpr uint32_t kQEnd = kQRing * Q::kBytes, kPEnd = kQEnd + kPRing * P::kBytes;
     __shared__ __align__(16) uint8_t lds[kPEnd];
 
@@ -234,65 +232,51 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t *)lds));
     const uint64_t q_step = static_cast<uint64_t>(kGatedDepth) * (Q_ALONG ? 1u : a.q_row) * 2;
     const uint64_t p_step = static_cast<uint64_t>(kGatedDepth) * (P_ALONG ? 1u : a.p_row) * 2;
-    // (their numbers, and the k from their first on)
-    uint32_t q_ahead = s_begin, p_ahead = s_begin, q_left = 0, p_left = 0;
+    uint32_t ahead = s_begin, left = 0;     // its number, and the k from its first on
     const uint8_t *q_at = nullptr, *p_at = nullptr, *p_other = nullptr;
-    auto in_half = [&](uint32_t s) { return FORM == kInputGrad && s >= half_steps ? s - half_steps : s; };
-    auto in_second = [&](uint32_t s) { return FORM == kInputGrad ? s >= half_steps : half != 0; };
-    auto seek_q = [&]() {
-        q_at = (in_second(q_ahead) ? q_base[1] : q_base[0]) + in_half(q_ahead) * q_step - kGatedBias;
-        q_left = a.depth - in_half(q_ahead) * kGatedDepth;
-    };
-    auto seek_p = [&]() {
-        p_at = (in_second(p_ahead) ? p_base[1] : p_base[0]) + in_half(p_ahead) * p_step - kGatedBias;
+    auto seek = [&](uint32_t s) {
+        const bool second = FORM == kInputGrad ? s >= half_steps : half != 0;
+        const uint32_t in_half = FORM == kInputGrad && second ? s - half_steps : s;
+        q_at = (second ? q_base[1] : q_base[0]) + in_half * q_step - kGatedBias;
+        p_at = (second ? p_base[1] : p_base[0]) + in_half * p_step - kGatedBias;
         if constexpr (FORM == kForward)
-            p_other = p_base[1] + p_ahead * p_step - kGatedBias;
-        p_left = a.depth - in_half(p_ahead) * kGatedDepth;
+            p_other = p_base[1] + in_half * p_step - kGatedBias;
+        left = a.depth - in_half * kGatedDepth;
     };
     auto request_q = [&](auto ragged, auto number, uint32_t place) {
-        q.template request<decltype(ragged)::value, decltype(number)::value>(q_at, lds_at + place, wave, q_left);
+        q.template request<decltype(ragged)::value, decltype(number)::value>(q_at, lds_at + place, wave, left);
     };
     auto request_p = [&](auto ragged, auto number, uint32_t place) {
         constexpr bool RAGGED = decltype(ragged)::value;
         constexpr uint32_t N = decltype(number)::value;
         if constexpr (FORM != kForward)
-            p.template request<RAGGED, N>(p_at, lds_at + place, wave, p_left);
+            p.template request<RAGGED, N>(p_at, lds_at + place, wave, left);
         else if constexpr (N < Half::kCopies)
-            half_p.template request<RAGGED, N>(p_at, lds_at + place, wave, p_left);
+            half_p.template request<RAGGED, N>(p_at, lds_at + place, wave, left);
         else
-            half_p.template request<RAGGED, N - Half::kCopies>(p_other, lds_at + place + Half::kBytes, wave, p_left);
+            half_p.template request<RAGGED, N - Half::kCopies>(p_other, lds_at + place + Half::kBytes, wave, left);
     };
-    auto advance_q = [&]() {
-        ++q_ahead;
+    auto advance = [&]() {
+        ++ahead;
         q_at += q_step;
-        q_left -= kGatedDepth;
-        if constexpr (FORM == kInputGrad)
-            if (q_ahead == half_steps)
-                seek_q();
-    };
-    auto advance_p = [&]() {
-        ++p_ahead;
         p_at += p_step;
         if constexpr (FORM == kForward)
             p_other += p_step;
-        p_left -= kGatedDepth;
+        left -= kGatedDepth;
         if constexpr (FORM == kInputGrad)
-            if (p_ahead == half_steps)
-                seek_p();
+            if (ahead == half_steps)
+                seek(ahead);
     };
-    auto request_all_q = [&](uint32_t place) {
-        if (q_left >= kGatedDepth)
-            each_of<Q::kCopies>([&](auto n) { request_q(std::false_type{}, n, place); });
+    auto request_all = [&](uint32_t q_place, uint32_t p_place) {
+        auto all_of = [&](auto ragged) {
+            each_of<Q::kCopies>([&](auto n) { request_q(ragged, n, q_place); });
+            each_of<P::kCopies>([&](auto n) { request_p(ragged, n, p_place); });
+        };
+        if (left >= kGatedDepth)
+            all_of(std::false_type{});
         else
-            each_of<Q::kCopies>([&](auto n) { request_q(std::true_type{}, n, place); });
-        advance_q();
-    };
-    auto request_all_p = [&](uint32_t place) {
-        if (p_left >= kGatedDepth)
-            each_of<P::kCopies>([&](auto n) { request_p(std::false_type{}, n, place); });
-        else
-            each_of<P::kCopies>([&](auto n) { request_p(std::true_type{}, n, place); });
-        advance_p();
+            all_of(std::true_type{});
+        advance();
     };
     constexpr uint32_t kCopies = Q::kCopies + P::kCopies;
 
@@ -307,8 +291,11 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
         for (int it = 0; it < TILES; ++it)
             acc[jt][it] = gated_f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
-    // The operands of half a step are read into registers while the half before it is multiplied; once everyone has read the second
-    // half, the place in LDS is requested for the step after the next.
+    // The operands of half a step are read into registers while the half before it is multiplied.  Once everyone has read a step's
+    // second half, its places in LDS are free: during its second half the q of the step after the next (RING 2) is requested, during the first
+    // half of the next step its p, which has a place more for that.  A CU takes in 64 bytes a cycle, half of a tile of 256's cycles of
+    // products and all of one of 128's, so the requests are spread over both halves (all in one: input gradient of 2048 tokens without
+    // slices 620 us, 575 so; in tiles of 128, 64 tokens, 252 / 204).
     struct Operands {
         gated_bf16x8_t q[TILES], p[TILES];
     };
@@ -320,30 +307,23 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
         else
             o.p[n] = P::read(lds + place, p_lane, n, h);
     };
-    static_assert(kCopies == 2 * TILES, "two copies to a row of sums");
+    static_assert(Q::kCopies == TILES && P::kCopies == TILES, "a copy to a row of sums");
     // the next step has come, and everyone holds this one in registers; `pass` copies that were requested later may still travel
     auto arrive = [&](auto pass) {
         asm volatile("s_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"v"(lds), "n"(decltype(pass)::value) : "memory");
     };
     constexpr std::integral_constant<uint32_t, 0> kNone{};
-    constexpr std::integral_constant<uint32_t, (kQRing - 2) * kCopies + (kPRing - kQRing) * P::kCopies> kLater{};
-    constexpr std::integral_constant<uint32_t, (kQRing - 1) * Q::kCopies + (kPRing - 1) * P::kCopies> kOthers{};  // than the first step's
+    constexpr std::integral_constant<uint32_t, (kQRing - 2) * kCopies + P::kCopies> kLater{};
+    constexpr std::integral_constant<uint32_t, (kQRing - 1) * kCopies> kOthers{};  // than the first step's
     static_assert(kLater.value < 64 && kOthers.value < 64, "as many as the counter counts");
     // (what is not a product stands by itself between products, in their shadow)
-    auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, uint32_t h,
-                           uint32_t q_to, uint32_t p_to) {
+    auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, auto h,
+                           uint32_t to) {
         constexpr int n = decltype(number)::value, kEach = TILES / 4;
         auto some = [&](int from) {
 #pragma unroll
             for (int it = from * kEach; it < (from + 1) * kEach; ++it)
                 acc[n][it] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(now.p[n], now.q[it], acc[n][it], 0, 0, 0);
-        };
-        auto request = [&](auto copy) {
-            constexpr uint32_t N = decltype(copy)::value;
-            if constexpr (N < Q::kCopies)
-                request_q(std::false_type{}, copy, q_to);
-            else
-                request_p(std::false_type{}, std::integral_constant<uint32_t, N - Q::kCopies>{}, p_to);
         };
         some(0);
         read_q(then, q_place, n, h);
@@ -352,30 +332,28 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
         read_p(then, p_place, n, h);
         __builtin_amdgcn_sched_barrier(0);
         some(2);
-        if constexpr (decltype(requests)::value)
-            request(std::integral_constant<uint32_t, 2 * n>{});
+        if constexpr (decltype(requests)::value && h == 1)
+            request_p(std::false_type{}, number, to);
+        else if constexpr (decltype(requests)::value)
+            request_q(std::false_type{}, number, to);
         __builtin_amdgcn_sched_barrier(0);
         some(3);
-        if constexpr (decltype(requests)::value)
-            request(std::integral_constant<uint32_t, 2 * n + 1>{});
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto half_step = [&](auto requests, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, uint32_t h, uint32_t q_to = 0,
-                         uint32_t p_to = 0) {
-        each_of<TILES>([&](auto n) { row_of_sums(requests, n, now, then, q_place, p_place, h, q_to, p_to); });
+    // h: the half that is read meanwhile
+    auto half_step = [&](auto requests, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, auto h, uint32_t to) {
+        each_of<TILES>([&](auto n) { row_of_sums(requests, n, now, then, q_place, p_place, h, to); });
     };
     if (steps > 0) {
+        constexpr std::integral_constant<uint32_t, 0> kFirstHalf{};
+        constexpr std::integral_constant<uint32_t, 1> kSecondHalf{};
         Operands first, second;
-        uint32_t q_now = 0, p_now = kQEnd;  // the step's places
+        uint32_t q_now = 0, p_now = kQEnd, p_before = kPEnd - P::kBytes;  // the step's places, and the one's before
         auto after = [](uint32_t place, uint32_t bytes, uint32_t begin, uint32_t end) { return place + bytes == end ? begin : place + bytes; };
-        seek_q();
-        seek_p();
-        for (uint32_t r = 0; r < kPRing && r < steps; ++r) {
-            if (r < kQRing)
-                request_all_q(r * Q::kBytes);
-            request_all_p(kQEnd + r * P::kBytes);
-        }
-        if (steps >= kPRing)
+        seek(s_begin);
+        for (uint32_t r = 0; r < kQRing && r < steps; ++r)
+            request_all(r * Q::kBytes, kQEnd + r * P::kBytes);
+        if (steps >= kQRing)
             arrive(kOthers);
         else
             arrive(kNone);
@@ -385,27 +363,26 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
             read_p(first, kQEnd, n, 0);
         }
         for (uint32_t s = 0; s < steps;) {
-            while (s + kPRing < steps && q_left >= kGatedDepth && p_left >= kGatedDepth) {
+            while (s + kQRing < steps && left >= kGatedDepth) {
                 const uint32_t q_next = after(q_now, Q::kBytes, 0, kQEnd), p_next = after(p_now, P::kBytes, kQEnd, kPEnd);
-                half_step(std::false_type{}, first, second, q_now, p_now, 1);
+                half_step(std::true_type{}, first, second, q_now, p_now, kSecondHalf, p_before);
                 arrive(kLater);
-                half_step(std::true_type{}, second, first, q_next, p_next, 0, q_now, p_now);
-                advance_q();
-                advance_p();
+                half_step(std::true_type{}, second, first, q_next, p_next, kFirstHalf, q_now);
+                advance();
                 q_now = q_next;
+                p_before = p_now;
                 p_now = p_next;
                 ++s;
             }
             // one by one: the last, and where half a sum ends
             const uint32_t q_next = after(q_now, Q::kBytes, 0, kQEnd), p_next = after(p_now, P::kBytes, kQEnd, kPEnd);
-            half_step(std::false_type{}, first, second, q_now, p_now, 1);
+            half_step(std::false_type{}, first, second, q_now, p_now, kSecondHalf, 0);
             arrive(kNone);
             if (s + kQRing < steps)
-                request_all_q(q_now);
-            if (s + kPRing < steps)
-                request_all_p(p_now);
-            half_step(std::false_type{}, second, first, q_next, p_next, 0);  // (behind the last step: what nobody uses)
+                request_all(q_now, p_before);
+            half_step(std::false_type{}, second, first, q_next, p_next, kFirstHalf, 0);  // (behind the last step: what nobody uses)
             q_now = q_next;
+            p_before = p_now;
             p_now = p_next;
             ++s;
         }
