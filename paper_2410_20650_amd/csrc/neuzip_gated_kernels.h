@@ -75,6 +75,13 @@ __device__ __forceinline__ void gated_copy(const uint8_t *from)
     asm volatile("global_load_lds_dwordx4 %0, off offset:%1" ::"v"(from), "n"(OFFSET));
 }
 
+// All but the last PASS of the wave's copies have come, and everyone holds in registers what it has read of LDS so far.
+template <uint32_t PASS>
+__device__ __forceinline__ void gated_arrive(const uint8_t *lds)
+{
+    asm volatile("s_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"v"(lds), "n"(PASS) : "memory");
+}
+
 // What lanes read that have no k of their own: zeros.
 __device__ const uint4 kGatedZeros[1] = {};
 
@@ -175,8 +182,16 @@ constexpr uint32_t kGatedWaves = 4, kGatedThreads = kGatedWaves * 64;
 // RING: the steps that LDS holds, of the operand for i; of the one for j one more.  Two and three are all of the 160 KB for a tile of 256,
 // or half of them for one of 128, of which two share a CU.  Where there are fewer of those than CUs, nothing else hides the wait for memory,
 // and four and five are held (two held, 4096 -> 4096, 200 tokens: forward 35.7 us, 29.7 so).
+template <int SIZE, int RING>
+__device__ __forceinline__ uint8_t *gated_lds()
+{
+    __shared__ __align__(16) uint8_t lds[(2 * RING + 1) * SIZE * kGatedDepth * 2];
+    return lds;
+}
+
+// workgroup `index` of `all` that compute FORM
 template <GatedForm FORM, int SIZE, int RING>
-__global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) void gated_kernel(const GatedArgs a)
+__device__ __forceinline__ void gated_workgroup(const GatedArgs &a, const uint32_t index, const uint32_t all)
 {
     constexpr int WAVES = kGatedWaves;
     constexpr bool Q_ALONG = FORM != kWeightGrad, P_ALONG = FORM == kForward;
@@ -186,14 +201,15 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
     typedef GatedOperand<SIZE / 2, WAVES, true> Half;  // kForward: the rows of one weight
     constexpr uint32_t kQRing = RING, kPRing = RING + 1;
     constexpr uint32_t kQEnd = kQRing * Q::kBytes, kPEnd = kQEnd + kPRing * P::kBytes;
-    __shared__ __align__(16) uint8_t lds[kPEnd];
+    uint8_t *const lds = gated_lds<SIZE, RING>();
+    static_assert(kPEnd == (2 * RING + 1) * SIZE * kGatedDepth * 2, "as gated_lds() has it");
 
     const uint32_t lane = threadIdx.x % 64;
     const uint32_t wave = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / 64)));
     // Which tile.  Workgroups go to the 8 XCDs in turn: each XCD takes a run of neighbouring tiles, and in it columns of 8 tiles of
     // i, so that what its L2 holds of both operands is used again.
-    const uint32_t all = gridDim.x, per = all / 8, more = all % 8, xcd = blockIdx.x % 8;
-    uint32_t tile = xcd * per + (xcd < more ? xcd : more) + blockIdx.x / 8;
+    const uint32_t per = all / 8, more = all % 8, xcd = index % 8;
+    uint32_t tile = xcd * per + (xcd < more ? xcd : more) + index / 8;
     const uint32_t per_slice = a.tiles_i * a.tiles_j * (FORM == kWeightGrad ? 2 : 1);
     const uint32_t slice = tile / per_slice;
     tile -= slice * per_slice;
@@ -308,14 +324,10 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
             o.p[n] = P::read(lds + place, p_lane, n, h);
     };
     static_assert(Q::kCopies == TILES && P::kCopies == TILES, "a copy to a row of sums");
-    // the next step has come, and everyone holds this one in registers; `pass` copies that were requested later may still travel
-    auto arrive = [&](auto pass) {
-        asm volatile("s_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"v"(lds), "n"(decltype(pass)::value) : "memory");
-    };
-    constexpr std::integral_constant<uint32_t, 0> kNone{};
-    constexpr std::integral_constant<uint32_t, (kQRing - 2) * kCopies + P::kCopies> kLater{};
-    constexpr std::integral_constant<uint32_t, (kQRing - 1) * kCopies> kOthers{};  // than the first step's
-    static_assert(kLater.value < 64 && kOthers.value < 64, "as many as the counter counts");
+    // how many of the copies requested last may still travel when the next step is read
+    constexpr uint32_t kLater = (kQRing - 2) * kCopies + P::kCopies;
+    constexpr uint32_t kOthers = (kQRing - 1) * kCopies;  // (the first step)
+    static_assert(kLater < 64 && kOthers < 64, "as many as the counter counts");
     // (what is not a product stands by itself between products, in their shadow)
     auto row_of_sums = [&](auto requests, auto number, const Operands &now, Operands &then, uint32_t q_place, uint32_t p_place, auto h,
                            uint32_t to) {
@@ -354,9 +366,9 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
         for (uint32_t r = 0; r < kQRing && r < steps; ++r)
             request_all(r * Q::kBytes, kQEnd + r * P::kBytes);
         if (steps >= kQRing)
-            arrive(kOthers);
+            gated_arrive<kOthers>(lds);
         else
-            arrive(kNone);
+            gated_arrive<0>(lds);
 #pragma unroll
         for (int n = 0; n < TILES; ++n) {
             read_q(first, 0, n, 0);
@@ -366,7 +378,7 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
             while (s + kQRing < steps && left >= kGatedDepth) {
                 const uint32_t q_next = after(q_now, Q::kBytes, 0, kQEnd), p_next = after(p_now, P::kBytes, kQEnd, kPEnd);
                 half_step(std::true_type{}, first, second, q_now, p_now, kSecondHalf, p_before);
-                arrive(kLater);
+                gated_arrive<kLater>(lds);
                 half_step(std::true_type{}, second, first, q_next, p_next, kFirstHalf, q_now);
                 advance();
                 q_now = q_next;
@@ -377,7 +389,7 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
             // one by one: the last, and where half a sum ends
             const uint32_t q_next = after(q_now, Q::kBytes, 0, kQEnd), p_next = after(p_now, P::kBytes, kQEnd, kPEnd);
             half_step(std::false_type{}, first, second, q_now, p_now, kSecondHalf, 0);
-            arrive(kNone);
+            gated_arrive<0>(lds);
             if (s + kQRing < steps)
                 request_all(q_now, p_before);
             half_step(std::false_type{}, second, first, q_next, p_next, kFirstHalf, 0);  // (behind the last step: what nobody uses)
@@ -463,6 +475,21 @@ __global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) vo
             }
         }
     }
+}
+
+template <GatedForm FORM, int SIZE, int RING>
+__global__ __launch_bounds__(kGatedThreads, SIZE == 128 && RING == 2 ? 2 : 1) void gated_kernel(const GatedArgs a)
+{
+    gated_workgroup<FORM, SIZE, RING>(a, blockIdx.x, gridDim.x);
+}
+
+// The input gradient and the weight gradients in one launch.
+__global__ __launch_bounds__(kGatedThreads, 2) void gated_gradients_kernel(const GatedArgs x, const GatedArgs w, const uint32_t x_wgs)
+{
+    if (blockIdx.x < x_wgs)
+        gated_workgroup<kInputGrad, 128, 2>(x, blockIdx.x, x_wgs);
+    else
+        gated_workgroup<kWeightGrad, 128, 2>(w, blockIdx.x - x_wgs, gridDim.x - x_wgs);
 }
 
 // dg = dh * u * act'(g), du = dh * act(g), each rounded to bf16 once (the matrix cores take bf16; with g and u rounded before, the
