@@ -159,14 +159,23 @@ def test_forward(nz, tokens, infeat, outfeat, act):
 
 @pytest.mark.parametrize("act", [0, 1])
 @pytest.mark.parametrize("tokens,infeat,outfeat", SHAPES)
-def test_backward(nz, tokens, infeat, outfeat, act):
+@pytest.mark.parametrize("alone", [False, True])
+def test_backward(nz, tokens, infeat, outfeat, act, alone):
     x, wg, wu = data(tokens, infeat, outfeat, 9300 + tokens, std=1.5 / math.sqrt(infeat))
     gate, up = (inputs.gaussian_f32((tokens, outfeat), 9310 + i, std=1.5, device=DEV) for i in range(2))
     grad_h = inputs.gaussian_bf16((tokens, outfeat), 9320, std=0.1, device=DEV)
     whole_x, grad_x = guarded((tokens, infeat))
     whole_g, grad_g = guarded((outfeat, infeat))
     whole_u, grad_u = guarded((outfeat, infeat))
-    nz.neuzip_gated_backward(x, wg, wu, gate, up, grad_h, act, grad_x, (grad_g, grad_u))
+
+    def backward(grad_x, grad_g, grad_u):
+        if not alone:
+            return nz.neuzip_gated_backward(x, wg, wu, gate, up, grad_h, act, grad_x, (grad_g, grad_u) if grad_g is not None else True)
+        (grad_x, _, _) = nz.neuzip_gated_backward(x, wg, wu, gate, up, grad_h, act, grad_x, False)
+        (_, grad_g, grad_u) = nz.neuzip_gated_backward(x, wg, wu, gate, up, grad_h, act, False, (grad_g, grad_u) if grad_g is not None else True)
+        return grad_x, grad_g, grad_u
+
+    backward(grad_x, grad_g, grad_u)
     torch.cuda.synchronize()
     assert untouched(whole_x, whole_g, whole_u)
     g, u, gh = gate.double(), up.double(), grad_h.double()
@@ -190,7 +199,7 @@ def test_backward(nz, tokens, infeat, outfeat, act):
           torch.matmul(dg.abs(), gs.abs()) + torch.matmul(du.abs(), us.abs()), 2 * outfeat)
     check(grad_g, torch.matmul(dg.t(), xs), torch.matmul(off_dg.t(), xs.abs()), torch.matmul(dg.abs().t(), xs.abs()), tokens)
     check(grad_u, torch.matmul(du.t(), xs), torch.matmul(off_du.t(), xs.abs()), torch.matmul(du.abs().t(), xs.abs()), tokens)
-    again = nz.neuzip_gated_backward(x, wg, wu, gate, up, grad_h, act)
+    again = backward(True, None, None)
     for one, other in zip(again, (grad_x, grad_g, grad_u)):
         assert torch.equal(one, other)      # from run to run the same
 
