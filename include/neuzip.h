@@ -409,8 +409,8 @@ uint64_t neuzip_gated_linear_scratch_bytes(uint64_t out_features, uint64_t in_fe
  *   d_scratch         device buffer of scratch_bytes bytes, at least neuzip_gated_backward_scratch_bytes(), in use until the call's
  *                     work has run.
  * All pointers are aligned to 16 bytes.  Products are exact, sums binary32; h and the three gradients are rounded once, to nearest
- * even, and so are dg and du, which the matrix cores take as bf16.  Results do not change from run to run.  Never allocates, never
- * synchronises.
+ * even, and so are dg and du, which the matrix cores take as bf16.  Results do not change from run to run; the order that dx is summed
+ * in is another where it is asked for alone.  Never allocates, never synchronises.
  */
 int neuzip_gated_forward(const void *d_x, const void *d_gate_weight, const void *d_up_weight, uint64_t tokens, uint64_t out_features,
                          uint64_t in_features, int activation, void *d_h, float *d_gate, float *d_up, void *hip_stream);

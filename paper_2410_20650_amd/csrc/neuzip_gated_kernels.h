@@ -9,6 +9,10 @@
 //   kWeightGrad  dWg = dg^T x and dWu = du^T x, sums over the tokens; half of the tiles are the one's, half the other's
 // The operand that supplies i or j lies with k along its rows (x and the weights in kForward, dg and du in kInputGrad), or with k
 // down its columns (the others).
+//
+// Measured, 2048 tokens, 4096 -> 2 x 14336 (481 * 10^9 operations each): forward with both sums kept 416 us, input gradient 356 and 13 for
+// its slices, weight gradients 414; forward of 1000 tokens 183 = 1284 TFLOP/s.  The matrix cores are busy in 0.56 to 0.72 of the cycles; with
+// operands of zeros, and the clock at 2.4 instead of 2.0 GHz, the same launches take 15 to 25 % less: power is what bounds them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -493,9 +497,9 @@ __global__ __launch_bounds__(kGatedThreads, 2) void gated_gradients_kernel(const
 }
 
 // dg = dh * u * act'(g), du = dh * act(g), each rounded to bf16 once (the matrix cores take bf16; with g and u rounded before, the
-// gradients were off by 3.1e-3 in the mean, 2.4e-3 now, of which the roundings of the results are 1.7e-3), 8 elements to a thread.
+// gradients were off by 3.1e-3 in the mean, 2.3e-3 now, of which the roundings of the results are 1.7e-3), 8 elements to a thread.
 // act'(g) = s + g s (1 - s) z'(g), s = sigmoid(z(g)); z' of the GELU grows with g^2, where s (1 - s) has long been zero.
-// Bound by memory: 14 bytes an element (2048 x 14336: see the figures of the backward pass).
+// Bound by memory: 14 bytes an element, 2048 x 14336 in 77 us = 5.3 TB/s.
 constexpr uint32_t kGatedSlopeThreads = 256;
 __global__ __launch_bounds__(kGatedSlopeThreads) void gated_slope_kernel(const float4 *__restrict__ gate, const float4 *__restrict__ up,
                                                                          const uint4 *__restrict__ grad_h, uint4 *__restrict__ dg,
@@ -528,7 +532,7 @@ __global__ __launch_bounds__(kGatedSlopeThreads) void gated_slope_kernel(const f
     du[at] = make_uint4(dus[0], dus[1], dus[2], dus[3]);
 }
 
-// dx from the sums of the slices of k, in their order, 8 elements to a thread.
+// dx from the sums of the slices of k, in their order, 8 elements to a thread.  Bound by memory: two slices of 2048 x 4096 12.7 us = 6.6 TB/s.
 __global__ __launch_bounds__(kGatedSlopeThreads) void gated_join_kernel(const float4 *__restrict__ partial, uint4 *__restrict__ out,
                                                                         uint64_t pieces, uint32_t slices)
 {
