@@ -36,7 +36,7 @@
 #include "neuzip_host.h"
 #include "neuzip_compress_kernels.h"
 #include "neuzip_decode_kernels.h"
-#include "neuzip_linear_kernels.h"
+#include "neuzip_linear_launch.h"
 
 using namespace nz;
 
@@ -608,13 +608,6 @@ inline LinearForm linear_form(uint32_t tokens, uint64_t in_features, const uint6
     return {32u, false, whole};
 }
 
-// Workgroups up to which the walks step without a branch (see rans_get): at most one per CU, two waves per SIMD (4096 x 4096,
-// 1 token, 15.5 us, with the branch 16.1; 1000 x 1024 17.0 / 17.7; 2048 x 4096, 16 tokens, k = 3, 15.5 / 16.4), while with more
-// (q, k and v of a Llama-3-8B attention block, 8 tokens: 20.9 / 20.0; two of 4096 x 4096, 12 tokens: 20.8 / 19.9) the vector unit has the branch's savings.
-// Not where most of the weights are symbols of 8 or of 4 bits, all alike, whose runs have 256 or 128 bytes, one as long as the
-// other: the lanes of a wave then read one or two LDS banks, at every symbol without the branch (16 exponents of one frequency,
-// 4096 x 4096, 1 token, 21.6 us).
-constexpr uint32_t kLinEager = 256;
 inline bool columns_in_step(const neuzip_blob *const *weights, uint32_t count)
 {
     uint64_t all = 0, in_step = 0;
@@ -626,38 +619,13 @@ inline bool columns_in_step(const neuzip_blob *const *weights, uint32_t count)
     return 2 * in_step > all;
 }
 
-template <int KB, bool NORM>
-void launch_linear(const LinearBatchArgs &batch, uint32_t cols, uint32_t wgs, bool in_step, hipStream_t stream)
-{
-    const dim3 grid(wgs), block(kLinThreads);
-    const uint32_t tokens = batch.t[0].tokens;
-    bool read = true;  // all weights walked whole, with tables to read
-    for (uint32_t i = 0; i < batch.count; ++i)
-        read = read && !batch.t[i].split && holds_table(batch.t[i].n_chunks);
-#define NZ_LINEAR(COLS, MT)                                                                                        \
-    do {                                                                                                           \
-        if (read)                                                                                                  \
-            hipLaunchKernelGGL((linear_batch_kernel<KB, COLS, MT, NORM, true, false>), grid, block, 0, stream, batch);  \
-        else if (wgs <= kLinEager && !in_step)                                                                                 \
-            hipLaunchKernelGGL((linear_batch_kernel<KB, COLS, MT, NORM, false, true>), grid, block, 0, stream, batch);  \
-        else                                                                                                       \
-            hipLaunchKernelGGL((linear_batch_kernel<KB, COLS, MT, NORM, false, false>), grid, block, 0, stream, batch); \
-    } while (0)
-    if (cols == 32) {
-        if (tokens <= 32)
-            NZ_LINEAR(32, 1);
-        else
-            NZ_LINEAR(32, 2);
-        return;
+template <int KB, int COLS, int MT, bool NORM, bool READ, bool EAGER>
+struct LinearBatch {
+    static void launch(const LinearBatchArgs &batch, uint32_t wgs, hipStream_t stream)
+    {
+        hipLaunchKernelGGL((linear_batch_kernel<KB, COLS, MT, NORM, READ, EAGER>), dim3(wgs), dim3(kLinThreads), 0, stream, batch);
     }
-    switch ((tokens + 15) / 16) {
-    case 1: NZ_LINEAR(16, 1); break;
-    case 2: NZ_LINEAR(16, 2); break;
-    case 3: NZ_LINEAR(16, 3); break;
-    default: NZ_LINEAR(16, 4); break;
-    }
-#undef NZ_LINEAR
-}
+};
 
 // An empty tensor: a zeroed table block (a fill kernel, not a memset node, so the call stays safe
 // to record into a graph) and a single zero offset.
@@ -1531,16 +1499,16 @@ int neuzip_linear_batch_scratch(const neuzip_blob *const *weights, const uint64_
                                 uint64_t in_features, const void *d_x, uint32_t tokens, const float *const *d_bias,
                                 float *const *d_y, void *d_scratch, uint64_t scratch_bytes, void *hip_stream)
 {
-    return linear_behind(weights, out_features, count, in_features, d_x, tokens, d_bias, d_y, d_scratch, scratch_bytes, nullptr, nullptr,
+    return linear_with(weights, out_features, count, in_features, d_x, tokens, d_bias, d_y, d_scratch, scratch_bytes, nullptr, nullptr,
                          static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"
 
-// (see neuzip_host.h; without a front, the launch in front is the layer's own)
-int nz::linear_behind(const neuzip_blob *const *weights, const uint64_t *out_features, uint32_t count, uint64_t in_features,
+// (see neuzip_host.h)
+int nz::linear_with(const neuzip_blob *const *weights, const uint64_t *out_features, uint32_t count, uint64_t in_features,
                       const void *d_x, uint32_t tokens, const float *const *d_bias, float *const *d_y, void *d_scratch,
-                      uint64_t scratch_bytes, LinearFront front, const void *context, hipStream_t stream)
+                      uint64_t scratch_bytes, LinearLauncher launch, const void *context, hipStream_t stream)
 {
     if (count == 0)
         return NEUZIP_OK;
@@ -1637,11 +1605,7 @@ int nz::linear_behind(const neuzip_blob *const *weights, const uint64_t *out_fea
         init.row_pieces = static_cast<uint32_t>(in_features / kRun);
         init_wgs += static_cast<uint32_t>((static_cast<uint64_t>(init.row_pieces) * tokens + kLinInitThreads - 1) / kLinInitThreads);
     }
-    if (front) {
-        const int rc = front(init, init_wgs, context, stream);
-        if (rc != NEUZIP_OK)
-            return rc;
-    } else if (init_wgs > 0)
+    if (init_wgs > 0)
         hipLaunchKernelGGL(linear_init_kernel, dim3(init_wgs), dim3(kLinInitThreads), 0, stream, init);
     // the kernel holds the partial sums of at most 64 tokens: larger batches go through in tiles of 64
     // (each tile decodes the weights again: beyond a few tiles decompressing once and a dense product win)
@@ -1672,19 +1636,13 @@ int nz::linear_behind(const neuzip_blob *const *weights, const uint64_t *out_fea
             wgs += (a.n_groups + groups_per_wg - 1) / groups_per_wg;
             batch.wg_end[i] = wgs;
         }
-        if (first->block) {
-            switch (first->k) {
-            case 3: launch_linear<3, true>(batch, cols, wgs, in_step, stream); break;
-            case 1: launch_linear<1, true>(batch, cols, wgs, in_step, stream); break;
-            default: launch_linear<0, true>(batch, cols, wgs, in_step, stream); break;
-            }
+        const LinearLaunch kind = {first->k, first->block != 0, in_step, cols, wgs};
+        if (launch && t0 == 0) {
+            const int rc = launch(batch, kind, context, stream);
+            if (rc != NEUZIP_OK)
+                return rc;
         } else {
-            switch (first->k) {
-            case 7: launch_linear<7, false>(batch, cols, wgs, in_step, stream); break;
-            case 3: launch_linear<3, false>(batch, cols, wgs, in_step, stream); break;
-            case 1: launch_linear<1, false>(batch, cols, wgs, in_step, stream); break;
-            default: launch_linear<0, false>(batch, cols, wgs, in_step, stream); break;
-            }
+            launch_linear<LinearBatch>(batch, kind, stream);
         }
         if (in_pieces) {
             sum.tokens = tile;

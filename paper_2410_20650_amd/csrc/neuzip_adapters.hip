@@ -19,13 +19,23 @@ constexpr uint32_t kAdapterMostTokens = 65535;  // a grid's second dimension
 
 inline uint64_t low_bytes(uint32_t tokens, uint32_t rank) { return pad_to(static_cast<uint64_t>(tokens) * rank * sizeof(float), 256); }
 
-int launch_low(const LinearInitArgs &init, uint32_t wgs, const void *context, hipStream_t stream)
+inline uint64_t low_wgs(const AdapterArgs &g) { return static_cast<uint64_t>((g.rank + kAdapterRows - 1) / kAdapterRows) * g.tokens; }
+
+template <int KB, int COLS, int MT, bool NORM, bool READ, bool EAGER>
+struct LinearAdapters {
+    static void launch(const LinearBatchArgs &batch, uint32_t wgs, hipStream_t stream, const AdapterArgs &g)
+    {
+        hipLaunchKernelGGL((linear_adapters_kernel<KB, COLS, MT, NORM, READ, EAGER>), dim3(wgs + static_cast<uint32_t>(low_wgs(g))), dim3(kLinThreads),
+                           0, stream, batch, g, wgs);
+    }
+};
+
+int launch_adapters(const LinearBatchArgs &batch, const LinearLaunch &kind, const void *context, hipStream_t stream)
 {
     const AdapterArgs &g = *static_cast<const AdapterArgs *>(context);
-    const uint64_t low_wgs = static_cast<uint64_t>((g.rank + kAdapterRows - 1) / kAdapterRows) * g.tokens;
-    if (too_many_wgs(wgs + low_wgs, kAdapterThreads))
+    if (too_many_wgs(kind.wgs + low_wgs(g), kLinThreads))
         return NEUZIP_EUNSUPPORTED;
-    hipLaunchKernelGGL(adapter_low_kernel, dim3(static_cast<uint32_t>(wgs + low_wgs)), dim3(kAdapterThreads), 0, stream, init, wgs, g);
+    launch_linear<LinearAdapters>(batch, kind, stream, g);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
 
@@ -69,9 +79,8 @@ int neuzip_linear_adapters(const neuzip_blob *weight, uint64_t out_features, uin
     g.rank = rank;
     g.in_features = static_cast<uint32_t>(in_features);
     g.out_features = static_cast<uint32_t>(out_features);
-    // (the low products are launched once the layer's own arguments have been found right)
-    const int rc = linear_behind(&weight, &out_features, 1, in_features, d_x, tokens, &d_bias, &d_y, static_cast<uint8_t *>(d_scratch) + own,
-                                 scratch_bytes - own, launch_low, &g, stream);
+    const int rc = linear_with(&weight, &out_features, 1, in_features, d_x, tokens, &d_bias, &d_y, static_cast<uint8_t *>(d_scratch) + own,
+                               scratch_bytes - own, launch_adapters, &g, stream);
     if (rc != NEUZIP_OK)
         return rc;
     hipLaunchKernelGGL(adapter_high_kernel, dim3((g.out_features + kAdapterThreads - 1) / kAdapterThreads, tokens), dim3(kAdapterThreads), 0,

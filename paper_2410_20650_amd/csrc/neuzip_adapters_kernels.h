@@ -1,16 +1,17 @@
 // Low-rank adapters beside a projection for gfx950:  y[t] += s[a] B[a] (A[a] x[t]),  a = id[t].
 //
-// Two launches with the low products, rank floats a token, between them: every row of A is a sum over all input features, and every
-// output wants all of them.  Bound by the adapters' bytes where requests name many (24 of rank 64, 14336 -> 4096, 48 tokens: 13.7 us for the
-// low products, 88 MB read by waves and 52 of them beyond the L2, and 5.8 for the high ones, beside the linear layer's 41), by latency for one token
-// (rank 16, 4096 -> 4096: 3.3 and 3.8 us, the linear layer 16.8).  A token reads its adapter by itself: tokens are not put in the order
-// of their adapters first, which would cost a launch; those of a common one meet in the L2.
+// The low products, rank floats a token, by workgroups behind the linear layer's own in its launch, where a CU has room beside one of
+// those or has run out of them; the high ones in a launch behind it: every row of A is a sum over all input features, and every output
+// wants all of them.  Bound by the linear layer beside them (4096 -> 4096, one token, rank 16: 17.4 us in all, 22.0 with the low
+// products in a launch in front, the layer alone 14.7; 14336 -> 4096, 48 tokens, 24 adapters of rank 64, 88 MB read by waves: 58.5, 64.1 with
+// them beside the setting up of the layer's outputs).  A token reads its adapter by itself: tokens are not put in the order of their
+// adapters first, which would cost a launch; those of a common one meet in the L2.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <cstdint>
 
-#include "neuzip_linear_front.h"
+#include "neuzip_linear_launch.h"
 
 namespace nz {
 
@@ -38,17 +39,11 @@ __device__ __forceinline__ float adapter_dot(const uint4 &p, const uint4 &q, flo
     return sum;
 }
 
-// low[t][r] = s (A[a] x[t])[r]: a wave to a token and a row of A, beside what the linear layer has its outputs and activations set up
-// with (48 tokens, 14336 -> 4096, rank 64: 4.0 and 11.0 us one behind the other).
-constexpr uint32_t kAdapterThreads = 256, kAdapterRows = kAdapterThreads / 64;  // rows of A of a workgroup
-static_assert(kAdapterThreads == kLinInitThreads, "both in one launch");
-__global__ __launch_bounds__(kAdapterThreads) void adapter_low_kernel(const LinearInitArgs init, uint32_t init_wgs, const AdapterArgs g)
+// low[t][r] = s (A[a] x[t])[r]: a wave to a token and a row of A.
+constexpr uint32_t kAdapterRows = kLinThreads / 64;  // rows of A of a workgroup
+__device__ __forceinline__ void adapter_low_workgroup(const AdapterArgs &g, uint32_t wg)
 {
-    if (blockIdx.x < init_wgs) {
-        linear_init_workgroup(init, blockIdx.x);
-        return;
-    }
-    const uint32_t groups = (g.rank + kAdapterRows - 1) / kAdapterRows, wg = blockIdx.x - init_wgs, t = wg / groups;
+    const uint32_t groups = (g.rank + kAdapterRows - 1) / kAdapterRows, t = wg / groups;
     const uint32_t lane = threadIdx.x % 64, r = (wg - t * groups) * kAdapterRows + threadIdx.x / 64;
     const int32_t id = g.ids[t];
     if (r >= g.rank || id < 0 || static_cast<uint32_t>(id) >= g.adapters)
@@ -78,7 +73,18 @@ __global__ __launch_bounds__(kAdapterThreads) void adapter_low_kernel(const Line
         g.low[static_cast<uint64_t>(t) * g.rank + r] = g.scales ? g.scales[id] * sum : sum;
 }
 
+// The linear layer's workgroups, and behind them those of the low products.
+template <int KB, int COLS, int MT, bool NORM, bool READ, bool EAGER>
+__global__ __launch_bounds__(kLinThreads, 4) void linear_adapters_kernel(const LinearBatchArgs b, const AdapterArgs g, const uint32_t wgs)
+{
+    if (blockIdx.x < wgs)
+        linear_batch_workgroup<KB, COLS, MT, NORM, READ, EAGER>(b);
+    else
+        adapter_low_workgroup(g, blockIdx.x - wgs);
+}
+
 // y[t][o] += B[a][o] . low[t]: a thread to an output.
+constexpr uint32_t kAdapterThreads = 256;
 __global__ __launch_bounds__(kAdapterThreads) void adapter_high_kernel(const AdapterArgs g)
 {
     const uint32_t o = blockIdx.x * kAdapterThreads + threadIdx.x, t = blockIdx.y;

@@ -15,7 +15,7 @@ namespace nz {
 // ------------------------------------------------------------------------------------------
 // Small helpers
 // ------------------------------------------------------------------------------------------
-__global__ void fill_u32_kernel(uint32_t *p, uint32_t value, uint32_t count)
+inline __global__ void fill_u32_kernel(uint32_t *p, uint32_t value, uint32_t count)
 {
     uint32_t i = blockIdx.x * blockDim.x + threadIdx.x;
     if (i < count)
@@ -609,7 +609,7 @@ __device__ __forceinline__ uint32_t update_word(uint32_t w, uint32_t g, float lr
 
 // The weight step alone, in place: w <- w - lr * g over n bf16 words (for the rare tensor whose
 // kept table did not serve after a fused step that was asked not to write the new weight back).
-__global__ __launch_bounds__(256) void sgd_update_kernel(uint16_t *__restrict__ w, const uint16_t *__restrict__ g,
+inline __global__ __launch_bounds__(256) void sgd_update_kernel(uint16_t *__restrict__ w, const uint16_t *__restrict__ g,
                                                          uint64_t n, float lr)
 {
     const uint64_t n_vec = n / 8;
@@ -1181,7 +1181,7 @@ __global__ __launch_bounds__(kEncThreads) __attribute__((amdgpu_waves_per_eu(1, 
 // ------------------------------------------------------------------------------------------
 constexpr uint32_t kCompactThreads = 256;
 
-__global__ __launch_bounds__(kCompactThreads) void compact_kernel(const CompressBatch b,
+inline __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const CompressBatch b,
                                                                  const uint16_t *__restrict__ slots_all,
                                                                  const uint32_t *__restrict__ chunk_words_all,
                                                                  const uint32_t *__restrict__ group_words_all,

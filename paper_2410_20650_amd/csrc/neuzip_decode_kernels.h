@@ -947,7 +947,7 @@ __device__ __forceinline__ void walk_to_entry(const uint32_t *__restrict__ lut, 
     }
 }
 
-__global__ __launch_bounds__(kEntryThreads) void entry_points_kernel(const DecodeArgs a, uint32_t *__restrict__ mid_states,
+inline __global__ __launch_bounds__(kEntryThreads) void entry_points_kernel(const DecodeArgs a, uint32_t *__restrict__ mid_states,
                                                                      uint8_t *__restrict__ mid_lens)
 {
     __shared__ __align__(16) uint32_t lut[kM];

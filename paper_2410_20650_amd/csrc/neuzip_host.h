@@ -139,12 +139,13 @@ inline bool on_current_device(const neuzip_blob *b)
 int follow(const neuzip_blob *const *blobs, uint32_t count, hipStream_t stream);
 inline int follow(const neuzip_blob *blob, hipStream_t stream) { return follow(&blob, 1, stream); }
 
-// neuzip_linear_batch_scratch with another's work in the launch in front of the layer's own.  front: launches the `wgs` workgroups of
-// `init` (linear_init_workgroup; there may be none), and whatever else can go beside them, on the stream.
-struct LinearInitArgs;
-typedef int (*LinearFront)(const LinearInitArgs &init, uint32_t wgs, const void *context, hipStream_t stream);
-int linear_behind(const neuzip_blob *const *weights, const uint64_t *out_features, uint32_t count, uint64_t in_features,
-                  const void *d_x, uint32_t tokens, const float *const *d_bias, float *const *d_y, void *d_scratch,
-                  uint64_t scratch_bytes, LinearFront front, const void *context, hipStream_t stream);
+// neuzip_linear_batch_scratch with another's work beside the layer's own.  launch, if there is one: launches the layer's kernel for the
+// first tile of tokens (launch_linear), and whatever else can go beside it, on the stream.
+struct LinearBatchArgs;
+struct LinearLaunch;
+typedef int (*LinearLauncher)(const LinearBatchArgs &batch, const LinearLaunch &kind, const void *context, hipStream_t stream);
+int linear_with(const neuzip_blob *const *weights, const uint64_t *out_features, uint32_t count, uint64_t in_features,
+                const void *d_x, uint32_t tokens, const float *const *d_bias, float *const *d_y, void *d_scratch,
+                uint64_t scratch_bytes, LinearLauncher launch, const void *context, hipStream_t stream);
 
 }  // namespace nz

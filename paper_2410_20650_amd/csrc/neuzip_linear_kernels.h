@@ -126,7 +126,7 @@ struct LinearBatchArgs {
     uint32_t count;                 // (for the host)
     LinearArgs t[kLinBatchMax];
 };
-__global__ void linear_init_kernel(const LinearInitArgs b) { linear_init_workgroup(b, blockIdx.x); }
+inline __global__ void linear_init_kernel(const LinearInitArgs b) { linear_init_workgroup(b, blockIdx.x); }
 
 // Behind the kernel below, where the sums of pieces are added up: y[t][r] = bias[r] + the pieces of row r.  A workgroup takes 64
 // rows; a piece's tokens are read 16 bytes per lane and turned in LDS, so that y is written a row of outputs at a time.
@@ -141,7 +141,7 @@ struct LinearSumArgs {
     uint64_t in_features;
     uint32_t tokens, piece_tokens, count;
 };
-__global__ __launch_bounds__(kLinSumThreads) void linear_sum_kernel(const LinearSumArgs b)
+inline __global__ __launch_bounds__(kLinSumThreads) void linear_sum_kernel(const LinearSumArgs b)
 {
     __shared__ float sums[kLinSumRows][kLinMaxTokens + 1];
     uint32_t i = 0, first = 0;
@@ -603,10 +603,8 @@ __device__ __forceinline__ void linear_workgroup(const LinearArgs &a, uint32_t w
                                                                        split && row_turns == kTurns, true, row_live, row, at.unit);
 }
 
-// (Two workgroups of 8 waves share a CU if a lane has at most 128 registers; with the 138 the compiler took
-// for 64 tokens it held one.)
 template <int KB, int COLS, int MT, bool NORM, bool READ, bool EAGER>
-__global__ __launch_bounds__(kLinThreads, 4) void linear_batch_kernel(const LinearBatchArgs b)
+__device__ __forceinline__ void linear_batch_workgroup(const LinearBatchArgs &b)
 {
     __shared__ __align__(16) struct {
         uint8_t stage[kLinStageBytes];  // first: a direct copy's LDS address has 16 bits
@@ -625,6 +623,14 @@ __global__ __launch_bounds__(kLinThreads, 4) void linear_batch_kernel(const Line
         }
     }
     linear_workgroup<KB, COLS, MT, NORM, READ, EAGER>(b.t[i], blockIdx.x - first, lds.lut, lds.steps, lds.stage, lds.area);
+}
+
+// (Two workgroups of 8 waves share a CU if a lane has at most 128 registers; with the 138 the compiler took
+// for 64 tokens it held one.)
+template <int KB, int COLS, int MT, bool NORM, bool READ, bool EAGER>
+__global__ __launch_bounds__(kLinThreads, 4) void linear_batch_kernel(const LinearBatchArgs b)
+{
+    linear_batch_workgroup<KB, COLS, MT, NORM, READ, EAGER>(b);
 }
 
 }  // namespace nz
