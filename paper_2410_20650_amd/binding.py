@@ -490,6 +490,8 @@ def _own_scratch(size, scratch, device, stream):
         if not (scratch.is_cuda and scratch.is_contiguous()):
             raise TypeError("expected a contiguous CUDA tensor as scratch memory")
         return scratch
+    if size == 0:
+        return None
     if stream is not None and isinstance(stream, torch.cuda.Stream):
         with torch.cuda.stream(stream):
             return _own_scratch(size, None, device, None)
@@ -500,7 +502,7 @@ def _own_scratch(size, scratch, device, stream):
 
 
 def _bytes_of(t):
-    return t.numel() * t.element_size()
+    return t.numel() * t.element_size() if t is not None else 0
 
 
 def neuzip_embedding(table: Blob, rows: int, features: int, tokens: torch.Tensor, scale: float = 1.0, out: torch.Tensor = None,

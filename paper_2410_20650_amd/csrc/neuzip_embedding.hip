@@ -20,6 +20,27 @@ inline bool valid_table(uint64_t rows, uint64_t features)
            rows * features < (1ull << 32);
 }
 
+// Gradient: up to which tokens one launch does it all, with any table (us, three launches / one: 64 tokens, 5003 x 520 7.9 / 4.2, 50257 x 768
+// 15.3 / 13.1, 128256 x 4096 158.6 / 151.7; all of one row, 5003 x 520, 9.8 / 9.0), and with one of at most 8 MB, whose zeros then leave at a quarter of
+// the rate (333 tokens, 2048 x 512 12.0 / 5.9, 5003 x 520 12.6 / 8.1, 1040 x 3648, 7.6 MB, 13.7 / 11.8, but 12936 x 856, 22 MB, 13.7 / 18.6; 512 of one
+// row, 5003 x 520, 14.7 / 15.7).
+constexpr uint32_t kFewTokens = 64, kSomeTokens = 512;
+constexpr uint64_t kSomePieces = 1ull << 19;
+
+// how many parts the tokens are looked over in, 0: not in one launch
+inline uint32_t few_parts(uint64_t count, uint64_t rows, uint64_t features)
+{
+    return count == 0 ? 0u : count <= kFewTokens ? 1u : count <= kSomeTokens && rows * features / kRun <= kSomePieces ? 4u : 0u;
+}
+
+template <int PARTS>
+void launch_few(const EmbeddingGradArgs &a, hipStream_t stream)
+{
+    constexpr uint32_t kWide = kGradThreads / PARTS;
+    const uint32_t pieces = a.rows * a.row_pieces.by;
+    hipLaunchKernelGGL(embedding_few_kernel<PARTS>, dim3((pieces + kWide - 1) / kWide), dim3(kGradThreads), 0, stream, a);
+}
+
 template <int KB, bool NORM>
 void launch_embedding(const EmbeddingArgs &a, hipStream_t stream)
 {
@@ -98,7 +119,7 @@ int neuzip_embedding(const neuzip_blob *table, uint64_t rows, uint64_t features,
 
 uint64_t neuzip_embedding_grad_scratch_bytes(uint64_t count, uint64_t rows, uint64_t features)
 {
-    if (!valid_table(rows, features) || count >= (1ull << 31))
+    if (!valid_table(rows, features) || count >= (1ull << 31) || few_parts(count, rows, features))
         return 0;
     const uint64_t runs = (count + kSortRun - 1) / kSortRun;
     return runs * sizeof(SortedRun) + (count > kBlockTokens ? runs * kPieces * features * sizeof(float) : 0);
@@ -111,9 +132,10 @@ int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d
         return NEUZIP_EINVAL;
     if (count >= (1ull << 31))
         return NEUZIP_EUNSUPPORTED;
-    if (count > 0 && (!d_tokens || !d_grad_out || !d_scratch || (reinterpret_cast<uintptr_t>(d_tokens) & 7u) ||
-                      (reinterpret_cast<uintptr_t>(d_grad_out) & 15u) || (reinterpret_cast<uintptr_t>(d_scratch) & 15u) ||
-                      scratch_bytes < neuzip_embedding_grad_scratch_bytes(count, rows, features)))
+    if (count > 0 && (!d_tokens || !d_grad_out || (reinterpret_cast<uintptr_t>(d_tokens) & 7u) || (reinterpret_cast<uintptr_t>(d_grad_out) & 15u)))
+        return NEUZIP_EINVAL;
+    const uint64_t needed = neuzip_embedding_grad_scratch_bytes(count, rows, features);
+    if (needed > 0 && (!d_scratch || (reinterpret_cast<uintptr_t>(d_scratch) & 15u) || scratch_bytes < needed))
         return NEUZIP_EINVAL;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     EmbeddingGradArgs a;
@@ -139,6 +161,13 @@ int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d
     const uint32_t strips = (a.row_pieces.by + kGradThreads - 1) / kGradThreads;
     if (strips > 65535)
         return NEUZIP_EUNSUPPORTED;
+    if (const uint32_t parts = few_parts(count, rows, features)) {
+        if (parts == 1)
+            launch_few<1>(a, stream);
+        else
+            launch_few<4>(a, stream);
+        return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
+    }
     hipLaunchKernelGGL(embedding_sort_kernel, dim3(static_cast<uint32_t>(static_cast<uint64_t>(a.sort_wgs) * a.n_runs + fill_wgs)), dim3(kSortThreads), 0,
                        stream, a);
     if (count > kBlockTokens)

@@ -242,7 +242,7 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
 // ------------------------------------------------------------------------------------------
 // Gradient:  grad[r] = bf16(scale * sum of g[t] over the tokens t with token[t] = r, in their order), every row of the table.
 //
-// Three launches, and nothing that depends on the order in which atomics arrive.
+// Three launches (few tokens: one, see embedding_few_kernel), and nothing that depends on the order in which atomics arrive.
 //   sort      the tokens in runs of 4096, by token and then position: an element's place is the number of those that come before it,
 //             which is counted, 32 elements to a workgroup, so that a run is sorted by many CUs in one go (one workgroup with a
 //             bitonic network in LDS took 45 us for 4096 tokens).  Counted the same way: where the rows of each of 2048 ranges begin
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
 // Most of the work for a large table is zeros: the first launch's other workgroups fill the gradient with them meanwhile (4096
 // tokens, 128256 x 4096: 159 us, in which the sort is done after 17; three quarters of the zeros beside the second launch gave nothing).
 // Bound by memory there, 1.05 GB at 6.5 TB/s, the pieces' 12 and the rows' 20 us behind it: 193 us; 333 tokens, 5003 x 520: 5.7, 3.0 and
-// 3.6 us, launches and latency.
+// 3.6 us, launches and latency, which is why few tokens go another way.
 // ------------------------------------------------------------------------------------------
 constexpr uint32_t kSortRun = 4096, kSortThreads = 256, kSortRanges = 2048, kSortQueries = 32;
 constexpr uint32_t kBlockTokens = 64, kBlocks = kSortRun / kBlockTokens;
@@ -434,6 +434,15 @@ __device__ __forceinline__ void places_of(const SortedRun &run, uint32_t row, ui
     upto = low;
 }
 
+__device__ __forceinline__ void leave_row(const EmbeddingGradArgs &a, uint32_t row, uint32_t piece, const float (&sum)[8])
+{
+    uint32_t d[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+        d[p] = bf16_of(sum[2 * p] * a.scale) | (bf16_of(sum[2 * p + 1] * a.scale) << 16);
+    reinterpret_cast<uint4 *>(a.grad)[static_cast<uint64_t>(row) * a.row_pieces.by + piece] = make_uint4(d[0], d[1], d[2], d[3]);
+}
+
 __global__ __launch_bounds__(kGradThreads) void embedding_rows_kernel(const EmbeddingGradArgs a)
 {
     const uint32_t own = blockIdx.y, place = blockIdx.x, lane = threadIdx.x % 64;
@@ -504,13 +513,84 @@ __global__ __launch_bounds__(kGradThreads) void embedding_rows_kernel(const Embe
             }
         }
     }
-    if (live) {
-        uint32_t d[4];
+    if (live)
+        leave_row(a, row, piece, sum);
+}
+
+// Few tokens in one launch: a thread to 16 bytes of the gradient.  Every wave looks its tokens over, a lane to each; those of the workgroup's
+// rows are added in their order, several requested at a time, by the threads whose row they name.
+//   PARTS 1   up to 64 tokens, all of them every wave's
+//   PARTS 4   up to 512: a workgroup holds a quarter as much of the gradient, its waves have a quarter of the tokens each, and the first adds
+//             their sums up in order
+template <int PARTS>
+__global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const EmbeddingGradArgs a)
+{
+    constexpr uint32_t kWide = kGradThreads / PARTS, kChunks = PARTS == 1 ? 1 : 2, kAtOnce = PARTS == 1 ? 8 : 16;
+    const uint32_t tid = threadIdx.x, lane = tid % 64, row_pieces = a.row_pieces.by;
+    const uint32_t part = PARTS == 1 ? 0u : tid / 64, at = PARTS == 1 ? tid : lane;
+    const uint32_t flat0 = blockIdx.x * kWide, flat = flat0 + at;  // (fewer than 2^29 pieces)
+    const uint32_t first = a.row_pieces.quotient(flat0), own_rows = a.row_pieces.quotient(flat0 + kWide - 1) - first + 1;
+    const uint32_t row = a.row_pieces.quotient(flat), own = row - first, piece = flat - row * row_pieces;
+    const bool live = row < a.rows;
+    const uint32_t count = static_cast<uint32_t>(a.count), each = (count + PARTS - 1) / PARTS, begin = part * each;
+    uint64_t off[kChunks];
 #pragma unroll
-        for (int p = 0; p < 4; ++p)
-            d[p] = bf16_of(sum[2 * p] * a.scale) | (bf16_of(sum[2 * p + 1] * a.scale) << 16);
-        reinterpret_cast<uint4 *>(a.grad)[static_cast<uint64_t>(row) * a.row_pieces.by + piece] = make_uint4(d[0], d[1], d[2], d[3]);
+    for (uint32_t c = 0; c < kChunks; ++c) {
+        const uint32_t in_part = c * 64 + lane;
+        const int64_t token = in_part < each && begin + in_part < count ? a.tokens[begin + in_part] : -1;
+        off[c] = token < static_cast<int64_t>(a.rows) ? static_cast<uint64_t>(token) - first : ~0ull;  // (a token below them is far behind)
     }
+    float sum[8] = {};
+    bool any = false;
+#pragma unroll
+    for (uint32_t c = 0; c < kChunks; ++c) {
+        uint64_t left = __ballot(off[c] < own_rows);
+        any = any || left;
+        while (left) {
+            uint4 v[kAtOnce];
+#pragma unroll
+            for (uint32_t n = 0; n < kAtOnce; ++n) {
+                const uint32_t l = left ? static_cast<uint32_t>(__builtin_ctzll(left)) : 0u;
+                const uint32_t of = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(off[c])), static_cast<int>(l)));
+                v[n] = make_uint4(0, 0, 0, 0);
+                if (live && left && of == own)
+                    v[n] = reinterpret_cast<const uint4 *>(a.grad_out)[static_cast<uint64_t>(begin + c * 64 + l) * row_pieces + piece];
+                left &= left - 1;  // (of none: none)
+            }
+#pragma unroll
+            for (uint32_t n = 0; n < kAtOnce; ++n)
+                add_eight(sum, v[n]);
+        }
+    }
+    if constexpr (PARTS > 1) {
+        __shared__ float4 sums[PARTS][2][64];
+        __shared__ uint32_t has[PARTS];
+        if (any) {
+            sums[part][0][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            sums[part][1][lane] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        }
+        if (lane == 0)
+            has[part] = any;
+        __syncthreads();
+        if (part > 0)
+            return;
+#pragma unroll
+        for (uint32_t p = 1; p < PARTS; ++p) {
+            if (!has[p])
+                continue;
+            const float4 u = sums[p][0][lane], v = sums[p][1][lane];
+            sum[0] += u.x;
+            sum[1] += u.y;
+            sum[2] += u.z;
+            sum[3] += u.w;
+            sum[4] += v.x;
+            sum[5] += v.y;
+            sum[6] += v.z;
+            sum[7] += v.w;
+        }
+    }
+    if (live)
+        leave_row(a, row, piece, sum);
 }
 
 }  // namespace nz

@@ -226,6 +226,15 @@ def test_gradient_of_the_table(nz, rows, features, count):
     check_grad(nz, some_tokens(rows, count, count + 1), g, rows, 0.3)
 
 
+# tables up to 8 MB and beyond, rows that divide a workgroup's 256 pieces of 16 bytes (or 64) and rows that do not, wider ones
+@pytest.mark.parametrize("rows,features", [(1, 8), (11, 24), (3000, 1416), (2900, 1416), (1030, 4104), (70000, 64), (65536, 64), (300, 2048)])
+@pytest.mark.parametrize("count", [1, 5, 64, 65, 200, 257, 512, 513])
+def test_gradient_of_few_tokens(nz, rows, features, count):
+    g = inputs.gaussian_bf16((count, features), 8850 + count, std=0.01, device=DEV)
+    check_grad(nz, some_tokens(rows, count, count), g, rows, 1.0)
+    check_grad(nz, torch.full((count,), rows - 1, dtype=torch.int64, device=DEV), g, rows, 0.3)
+
+
 @pytest.mark.parametrize("count", [1, 64, 65, 4096, 13000])
 @pytest.mark.parametrize("kind", ["same", "none", "distinct", "halves"])
 def test_tokens_of_one_kind(nz, count, kind):
@@ -312,6 +321,6 @@ def test_refusals(nz):
         nz.neuzip_embedding_grad(tok, g.float(), 64)
     with pytest.raises(ValueError):
         nz.neuzip_embedding_grad(tok[:4], g, 64)
-    assert code(lambda: nz.neuzip_embedding_grad(tok, g, 64, scratch=torch.empty(16, dtype=torch.uint8, device=DEV))) == nz.EINVAL
+    assert code(lambda: nz.neuzip_embedding_grad(tok.repeat(130), g.repeat(130, 1), 64, scratch=torch.empty(16, dtype=torch.uint8, device=DEV))) == nz.EINVAL
     assert code(lambda: nz.neuzip_embedding_grad(tok, g[:, :4].contiguous(), 64)) == nz.EINVAL
     assert code(lambda: nz.neuzip_embedding_grad(tok, odd.view(5, 256), 64)) == nz.EINVAL

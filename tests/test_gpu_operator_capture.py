@@ -27,7 +27,7 @@ def calls(nz):
     layer's sums come in any order."""
     x, gate, up = bf(TOKENS, IN, seed=1), bf(OUT, IN, seed=2), bf(OUT, IN, seed=3)
     blobs = [nz.neuzip_compress(w, 7) for w in (gate, up)]
-    tokens = (torch.arange(TOKENS, device=DEV) * 7) % ROWS
+    tokens, grad_out = (torch.arange(600, device=DEV) * 7) % ROWS, bf(600, IN, seed=10)
     ids = (torch.arange(TOKENS, device=DEV) % ADAPTERS).to(torch.int32)
     a, b = bf(ADAPTERS, RANK, IN, seed=4), bf(ADAPTERS, OUT, RANK, seed=5)
     g, u = bf(TOKENS, OUT, seed=6).float(), bf(TOKENS, OUT, seed=7).float()
@@ -40,7 +40,7 @@ def calls(nz):
     of_h = 1.2 * of_gate * um + of_up * gm + 2.0 ** -7 * gm * um        # (the activation's slope; a rounding to bf16 each)
     low = sum((xm @ a[i].float().abs().t()) @ b[i].float().abs().t() for i in range(ADAPTERS)).max().item()
     return {
-        "embedding_grad": (lambda **kw: nz.neuzip_embedding_grad(tokens, x, ROWS, 1.0, grad, **kw), [grad], 0.0),
+        "embedding_grad": (lambda **kw: nz.neuzip_embedding_grad(tokens, grad_out, ROWS, 1.0, grad, **kw), [grad], 0.0),
         "gated_linear": (lambda **kw: nz.neuzip_gated_linear(*blobs, OUT, IN, x, nz.SILU, h, **kw), [h], of_h),
         "gated_backward": (lambda **kw: nz.neuzip_gated_backward(x, gate, up, g, u, gh, nz.SILU, gx, gw, **kw), [gx, *gw], 0.0),
         "linear_adapters": (lambda **kw: nz.neuzip_linear_adapters(blobs[0], OUT, IN, x, a, b, None, ids, None, y, **kw), [y], of_gate + 2.0 * sums * low),

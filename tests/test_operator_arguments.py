@@ -138,11 +138,12 @@ def test_the_library_refuses_before_any_device_work():
                  (some,) * 6 + (3, 40, 256, 0, odd, some, some, some, room)):
         assert backward(*args, None) == nz.EINVAL, args
     grad = lib.neuzip_embedding_grad
-    room = lib.neuzip_embedding_grad_scratch_bytes(100, 50, 256)
-    for args in ((some, 100, some, 50, 250, 1.0, some, some, room + 4096), (some, 100, some, 0, 256, 1.0, some, some, room),
-                 (some, 100, some, 50, 256, 1.0, null, some, room), (some, 100, some, 50, 256, 1.0, odd, some, room),
-                 (null, 100, some, 50, 256, 1.0, some, some, room), (some, 100, some, 50, 256, 1.0, some, some, room - 1),
-                 (some, 100, some, 1 << 24, 256, 1.0, some, some, room)):
+    room = lib.neuzip_embedding_grad_scratch_bytes(600, 50, 256)
+    assert room > 0
+    for args in ((some, 600, some, 50, 250, 1.0, some, some, room + 4096), (some, 600, some, 0, 256, 1.0, some, some, room),
+                 (some, 600, some, 50, 256, 1.0, null, some, room), (some, 600, some, 50, 256, 1.0, odd, some, room),
+                 (null, 600, some, 50, 256, 1.0, some, some, room), (some, 600, some, 50, 256, 1.0, some, some, room - 1),
+                 (some, 600, some, 1 << 24, 256, 1.0, some, some, room)):
         assert grad(*args, None) == nz.EINVAL, args
     assert grad(some, 1 << 31, some, 50, 256, 1.0, some, some, room, None) == nz.EUNSUPPORTED
     # something that is not a blob
@@ -154,5 +155,7 @@ def test_the_library_refuses_before_any_device_work():
 
 
 def test_scratch_memory_of_odd_shapes_is_none():
+    assert nz.neuzip_embedding_grad_scratch_bytes(512, 50, 256) == 0 and nz.neuzip_embedding_grad_scratch_bytes(64, 128256, 4096) == 0   # (in one launch)
+    assert nz.neuzip_embedding_grad_scratch_bytes(513, 50, 256) > 0 and nz.neuzip_embedding_grad_scratch_bytes(65, 128256, 4096) > 0
     assert nz.neuzip_embedding_grad_scratch_bytes(0, 50, 256) == 0 and nz.neuzip_embedding_grad_scratch_bytes(10, 50, 250) == 0
     assert nz.neuzip_gated_backward_scratch_bytes(0, 40, 256) == 0 and nz.neuzip_gated_backward_scratch_bytes(3, 41, 256) == 0
