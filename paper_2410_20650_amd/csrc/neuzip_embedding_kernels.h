@@ -299,13 +299,19 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const Embe
     const uint64_t base = static_cast<uint64_t>(of_run) * kSortRun;
     const uint32_t here = a.count - base < kSortRun ? static_cast<uint32_t>(a.count - base) : kSortRun;
     const uint32_t padded = (here + 4 * kParts - 1) / (4 * kParts) * (4 * kParts), each = padded / kParts;
-    for (uint32_t i = tid; i < padded; i += kSortThreads) {
-        uint32_t row = ~0u;  // of no row: behind them all
-        if (i < here) {
-            const int64_t token = a.tokens[base + i];
-            row = token >= 0 && token < static_cast<int64_t>(a.rows) ? static_cast<uint32_t>(token) : ~0u;
-        }
-        rows[i] = row;
+    // (all of a thread's tokens requested together)
+    constexpr uint32_t kEach = kSortRun / kSortThreads;
+    int64_t tokens[kEach];
+#pragma unroll
+    for (uint32_t r = 0; r < kEach; ++r) {
+        const uint32_t i = r * kSortThreads + tid;
+        tokens[r] = i < here ? a.tokens[base + i] : -1;
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < kEach; ++r) {
+        const uint32_t i = r * kSortThreads + tid;
+        if (i < padded)  // (of no row: behind them all)
+            rows[i] = tokens[r] >= 0 && tokens[r] < static_cast<int64_t>(a.rows) ? static_cast<uint32_t>(tokens[r]) : ~0u;
     }
     if (tid < kSortQueries)
         before[tid] = 0;
