@@ -481,19 +481,33 @@ __global__ __launch_bounds__(kGradThreads) void embedding_rows_kernel(const Embe
     float sum[8] = {};
     // the sums of the pieces that the places from `from` on are in, in order
     auto add_pieces = [&](uint32_t r, uint32_t from, uint32_t ends) {
-        for (uint32_t k = 0; k <= ends; ++k) {
-            const uint32_t number = 2 * (from / kBlockTokens + k) + (k == 0 ? 1 : 0);
-            const float4 *v = reinterpret_cast<const float4 *>(a.partial + (static_cast<uint64_t>(r) * kPieces + number) * a.features) + 2 * piece;
-            const float4 p = v[0], q = v[1];
-            sum[0] += p.x;
-            sum[1] += p.y;
-            sum[2] += p.z;
-            sum[3] += p.w;
-            sum[4] += q.x;
-            sum[5] += q.y;
-            sum[6] += q.z;
-            sum[7] += q.w;
-        }
+        auto take = [&](auto pieces, uint32_t k) {
+            constexpr uint32_t N = decltype(pieces)::value;
+            float4 p[N], q[N];
+#pragma unroll
+            for (uint32_t n = 0; n < N; ++n) {
+                const uint32_t number = 2 * (from / kBlockTokens + k + n) + (k + n == 0 ? 1 : 0);
+                const float4 *v = reinterpret_cast<const float4 *>(a.partial + (static_cast<uint64_t>(r) * kPieces + number) * a.features) + 2 * piece;
+                p[n] = v[0];
+                q[n] = v[1];
+            }
+#pragma unroll
+            for (uint32_t n = 0; n < N; ++n) {
+                sum[0] += p[n].x;
+                sum[1] += p[n].y;
+                sum[2] += p[n].z;
+                sum[3] += p[n].w;
+                sum[4] += q[n].x;
+                sum[5] += q[n].y;
+                sum[6] += q[n].z;
+                sum[7] += q[n].w;
+            }
+        };
+        uint32_t k = 0;
+        for (; k + 8 <= ends + 1; k += 8)
+            take(std::integral_constant<uint32_t, 8>{}, k);
+        for (; k <= ends; ++k)
+            take(std::integral_constant<uint32_t, 1>{}, k);
     };
     if (live) {
         if (passes)
