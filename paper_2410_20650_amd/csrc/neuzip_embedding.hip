@@ -27,6 +27,17 @@ inline bool valid_table(uint64_t rows, uint64_t features)
 constexpr uint32_t kFewTokens = 64, kSomeTokens = 512;
 constexpr uint64_t kSomePieces = 1ull << 19;
 
+// Tables up to which the sort has workgroups of 1024 threads, which count a run sooner; the zeros of larger ones, which hide it, leave
+// faster from smaller ones (us, 256 / 1024 threads: 4096 tokens, 5003 x 520, 11.4 / 7.2; 2048, 32000 x 2048, 18.3 / 18.4; 4096, 128256 x 4096, 155 / 171).
+constexpr uint64_t kSortWidePieces = 1ull << 23;
+template <uint32_t THREADS>
+void launch_sort(const EmbeddingGradArgs &a, hipStream_t stream)
+{
+    const uint64_t fill_wgs = (static_cast<uint64_t>(a.rows) * a.row_pieces.by + THREADS - 1) / THREADS;
+    hipLaunchKernelGGL(embedding_sort_kernel<THREADS>, dim3(static_cast<uint32_t>(static_cast<uint64_t>(a.sort_wgs) * a.n_runs + fill_wgs)), dim3(THREADS), 0,
+                       stream, a);
+}
+
 // how many parts the tokens are looked over in, 0: not in one launch
 inline uint32_t few_parts(uint64_t count, uint64_t rows, uint64_t features)
 {
@@ -157,7 +168,6 @@ int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d
         return NEUZIP_EUNSUPPORTED;
     const uint32_t most = count < kSortRun ? static_cast<uint32_t>(count) : kSortRun;  // tokens of a run
     a.sort_wgs = count > 0 ? (most + kSortRanges + kSortQueries) / kSortQueries : 0u;
-    const uint64_t fill_wgs = (rows * a.row_pieces.by + kSortThreads - 1) / kSortThreads;
     const uint32_t strips = (a.row_pieces.by + kGradThreads - 1) / kGradThreads;
     if (strips > 65535)
         return NEUZIP_EUNSUPPORTED;
@@ -168,8 +178,10 @@ int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d
             launch_few<4>(a, stream);
         return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
     }
-    hipLaunchKernelGGL(embedding_sort_kernel, dim3(static_cast<uint32_t>(static_cast<uint64_t>(a.sort_wgs) * a.n_runs + fill_wgs)), dim3(kSortThreads), 0,
-                       stream, a);
+    if (rows * a.row_pieces.by <= kSortWidePieces && a.n_runs <= 64)  // (more runs have every CU at work anyway, and a launch fewer than 2^32 threads)
+        launch_sort<1024>(a, stream);
+    else
+        launch_sort<256>(a, stream);
     if (count > kBlockTokens)
         hipLaunchKernelGGL(embedding_pieces_kernel, dim3(kPieces, a.n_runs, strips), dim3(kGradThreads), 0, stream, a);
     if (count > 0)

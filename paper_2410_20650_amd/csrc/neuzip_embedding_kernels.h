@@ -251,11 +251,11 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
 //             binary32, so that a token that is very frequent is no workgroup's work alone
 //   rows      a workgroup to a row with tokens, at the first of them, adds its tokens up, or its pieces, and stores it.
 // Most of the work for a large table is zeros: the first launch's other workgroups fill the gradient with them meanwhile (4096
-// tokens, 128256 x 4096: 159 us, in which the sort is done after 17; three quarters of the zeros beside the second launch gave nothing).
-// Bound by memory there, 1.05 GB at 6.5 TB/s, the pieces' 12 and the rows' 20 us behind it: 193 us; 333 tokens, 5003 x 520: 5.7, 3.0 and
-// 3.6 us, launches and latency, which is why few tokens go another way.
+// tokens, 128256 x 4096: 159 us, in which the sort is done after 11; three quarters of the zeros beside the second launch gave nothing).
+// Bound by memory there, 1.05 GB at 6.5 TB/s, the pieces' 12 and the rows' 20 us behind it: 186 to 193 us; by latency and launches with
+// small tables (5003 x 520: 7.2, 6.5 and 5.0 us), which is why few tokens go another way.
 // ------------------------------------------------------------------------------------------
-constexpr uint32_t kSortRun = 4096, kSortThreads = 256, kSortRanges = 2048, kSortQueries = 32;
+constexpr uint32_t kSortRun = 4096, kSortRanges = 2048, kSortQueries = 32;
 constexpr uint32_t kBlockTokens = 64, kBlocks = kSortRun / kBlockTokens;
 constexpr uint32_t kPieces = 2 * kBlocks;  // of a run: of a row that began before the block; of one that begins in it and passes its end
 struct SortedRun {
@@ -279,12 +279,13 @@ struct EmbeddingGradArgs {
     float scale;
 };
 
-__global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const EmbeddingGradArgs a)
+template <uint32_t THREADS>
+__global__ __launch_bounds__(THREADS) void embedding_sort_kernel(const EmbeddingGradArgs a)
 {
     const uint32_t sorting = a.sort_wgs * a.n_runs;
     if (blockIdx.x >= sorting) {
         // Zeros, 16 bytes to a thread: 1.05 GB take 155 us, with four or sixteen times as much 177 and 191.  (Fewer than 2^29 pieces.)
-        const uint32_t piece = (blockIdx.x - sorting) * kSortThreads + threadIdx.x;
+        const uint32_t piece = (blockIdx.x - sorting) * THREADS + threadIdx.x;
         if (piece < a.rows * a.row_pieces.by)
             reinterpret_cast<uint4 *>(a.grad)[piece] = make_uint4(0, 0, 0, 0);
         return;
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const Embe
     const uint32_t of_run = a.sort_wgs == 0 ? 0u : blockIdx.x / a.sort_wgs, group = blockIdx.x - of_run * a.sort_wgs;
     // Queries are the run's elements, then the ranges' first rows.  A wave's lanes hold the 32 queries twice, for two halves of
     // the wave's quarter of the run.
-    constexpr uint32_t kParts = kSortThreads / kSortQueries;
+    constexpr uint32_t kParts = THREADS / kSortQueries;
     __shared__ __align__(16) uint32_t rows[kSortRun];
     __shared__ uint32_t before[kSortQueries];
     const uint32_t tid = threadIdx.x, query = tid % kSortQueries, part = tid / kSortQueries;
@@ -300,16 +301,16 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const Embe
     const uint32_t here = a.count - base < kSortRun ? static_cast<uint32_t>(a.count - base) : kSortRun;
     const uint32_t padded = (here + 4 * kParts - 1) / (4 * kParts) * (4 * kParts), each = padded / kParts;
     // (all of a thread's tokens requested together)
-    constexpr uint32_t kEach = kSortRun / kSortThreads;
+    constexpr uint32_t kEach = kSortRun / THREADS;
     int64_t tokens[kEach];
 #pragma unroll
     for (uint32_t r = 0; r < kEach; ++r) {
-        const uint32_t i = r * kSortThreads + tid;
+        const uint32_t i = r * THREADS + tid;
         tokens[r] = i < here ? a.tokens[base + i] : -1;
     }
 #pragma unroll
     for (uint32_t r = 0; r < kEach; ++r) {
-        const uint32_t i = r * kSortThreads + tid;
+        const uint32_t i = r * THREADS + tid;
         if (i < padded)  // (of no row: behind them all)
             rows[i] = tokens[r] >= 0 && tokens[r] < static_cast<int64_t>(a.rows) ? static_cast<uint32_t>(tokens[r]) : ~0u;
     }
@@ -325,7 +326,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const Embe
     const uint32_t not_above = is_element ? (row == ~0u ? row : row + 1) : row;
     const uint32_t p0 = group * kSortQueries;
     uint32_t count = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (uint32_t j = part * each; j < (part + 1) * each; j += 4) {
         const uint4 v = *reinterpret_cast<const uint4 *>(rows + j);
         const uint32_t limit = j < p0 ? not_above : row;
@@ -335,9 +336,16 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const Embe
         count += v.w < limit;
     }
     // ... of the workgroup's own, those in front (the equal ones have not been counted)
-    if (part == 0 && is_element)
-        for (uint32_t j = p0; j < number; ++j)
-            count += rows[j] == row;
+    if (part == 0 && is_element) {
+#pragma unroll
+        for (uint32_t j = 0; j < kSortQueries; j += 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(rows + p0 + j);
+            count += v.x == row && j < query;
+            count += v.y == row && j + 1 < query;
+            count += v.z == row && j + 2 < query;
+            count += v.w == row && j + 3 < query;
+        }
+    }
     atomicAdd(&before[query], count);
     __syncthreads();
     if (tid >= kSortQueries)
