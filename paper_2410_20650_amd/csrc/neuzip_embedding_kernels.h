@@ -448,12 +448,12 @@ __device__ __forceinline__ void places_of(const SortedRun &run, uint32_t row, ui
     upto = low;
 }
 
-__device__ __forceinline__ void leave_row(const EmbeddingGradArgs &a, uint32_t row, uint32_t piece, const float (&sum)[8])
+__device__ __forceinline__ void leave_row(const EmbeddingGradArgs &a, uint32_t row, uint32_t piece, const float (&sum)[8], float scale)
 {
     uint32_t d[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p)
-        d[p] = bf16_of(sum[2 * p] * a.scale) | (bf16_of(sum[2 * p + 1] * a.scale) << 16);
+        d[p] = bf16_of(sum[2 * p] * scale) | (bf16_of(sum[2 * p + 1] * scale) << 16);
     reinterpret_cast<uint4 *>(a.grad)[static_cast<uint64_t>(row) * a.row_pieces.by + piece] = make_uint4(d[0], d[1], d[2], d[3]);
 }
 
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(kGradThreads) void embedding_rows_kernel(const Embe
         }
     }
     if (live)
-        leave_row(a, row, piece, sum);
+        leave_row(a, row, piece, sum, a.scale);
 }
 
 // Few tokens in one launch: a thread to 16 bytes of the gradient.  Every wave looks its tokens over, a lane to each; those of the workgroup's
@@ -550,6 +550,7 @@ __global__ __launch_bounds__(kGradThreads) void embedding_rows_kernel(const Embe
 //   PARTS 1   up to 64 tokens, all of them every wave's
 //   PARTS 4   up to 512: a workgroup holds a quarter as much of the gradient, its waves have a quarter of the tokens each, and the first adds
 //             their sums up in order
+// A row without tokens is left as zeros, whatever the factor: a negative one would make them -0, an infinity or a NaN a NaN.
 template <int PARTS>
 __global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const EmbeddingGradArgs a)
 {
@@ -569,11 +570,10 @@ __global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const Embed
         off[c] = token < static_cast<int64_t>(a.rows) ? static_cast<uint64_t>(token) - first : ~0ull;  // (a token below them is far behind)
     }
     float sum[8] = {};
-    bool any = false;
+    bool mine = false;  // a token names the thread's row
 #pragma unroll
     for (uint32_t c = 0; c < kChunks; ++c) {
         uint64_t left = __ballot(off[c] < own_rows);
-        any = any || left;
         while (left) {
             uint4 v[kAtOnce];
 #pragma unroll
@@ -581,7 +581,9 @@ __global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const Embed
                 const uint32_t l = left ? static_cast<uint32_t>(__builtin_ctzll(left)) : 0u;
                 const uint32_t of = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(static_cast<uint32_t>(off[c])), static_cast<int>(l)));
                 v[n] = make_uint4(0, 0, 0, 0);
-                if (live && left && of == own)
+                const bool here = live && left && of == own;
+                mine = mine || here;
+                if (here)
                     v[n] = reinterpret_cast<const uint4 *>(a.grad_out)[static_cast<uint64_t>(begin + c * 64 + l) * row_pieces + piece];
                 left &= left - 1;  // (of none: none)
             }
@@ -592,13 +594,14 @@ __global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const Embed
     }
     if constexpr (PARTS > 1) {
         __shared__ float4 sums[PARTS][2][64];
-        __shared__ uint32_t has[PARTS];
-        if (any) {
+        __shared__ uint64_t has[PARTS];  // the lanes with a token in that part
+        const uint64_t lanes = __ballot(mine);
+        if (lanes) {
             sums[part][0][lane] = make_float4(sum[0], sum[1], sum[2], sum[3]);
             sums[part][1][lane] = make_float4(sum[4], sum[5], sum[6], sum[7]);
         }
         if (lane == 0)
-            has[part] = any;
+            has[part] = lanes;
         __syncthreads();
         if (part > 0)
             return;
@@ -606,6 +609,7 @@ __global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const Embed
         for (uint32_t p = 1; p < PARTS; ++p) {
             if (!has[p])
                 continue;
+            mine = mine || (has[p] >> lane & 1u);
             const float4 u = sums[p][0][lane], v = sums[p][1][lane];
             sum[0] += u.x;
             sum[1] += u.y;
@@ -618,7 +622,7 @@ __global__ __launch_bounds__(kGradThreads) void embedding_few_kernel(const Embed
         }
     }
     if (live)
-        leave_row(a, row, piece, sum);
+        leave_row(a, row, piece, sum, mine ? a.scale : 0.0f);
 }
 
 }  // namespace nz
