@@ -483,6 +483,14 @@ def _expect(t, dtype, shape, what):
     return t
 
 
+def _memory_of(stream):
+    """Tensors made in here are of this stream's memory.  (Any object with a handle will do as a call's stream.)"""
+    if not isinstance(stream, torch.cuda.Stream):
+        # (an external stream of handle 0 would be a new one)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream) if stream.cuda_stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 def _own_scratch(size, scratch, device, stream):
     """The caller's scratch memory, or the call's own: of the stream's that its work runs on, so that it is not handed out to
     another one's while it is in use."""
@@ -492,8 +500,8 @@ def _own_scratch(size, scratch, device, stream):
         return scratch
     if size == 0:
         return None
-    if stream is not None and isinstance(stream, torch.cuda.Stream):
-        with torch.cuda.stream(stream):
+    if stream is not None:
+        with _memory_of(stream):
             return _own_scratch(size, None, device, None)
     if torch.cuda.is_current_stream_capturing():
         return torch.empty(size, dtype=torch.uint8, device=device)
