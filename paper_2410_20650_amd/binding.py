@@ -389,6 +389,31 @@ class _OutsideOfCaptures:
         _lib.hipThreadExchangeStreamCaptureMode(ctypes.byref(self.mode))
 
 
+def _memory_of(stream):
+    """Tensors made in here are of this stream's memory.  (Any object with a handle will do as a call's stream.)"""
+    if not isinstance(stream, torch.cuda.Stream):
+        # (an external stream of handle 0 would be a new one)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream) if stream.cuda_stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
+def _made_apart(shape, dtype, device):
+    """A tensor of the current stream's memory, whose making leaves another thread's capture alone."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _OutsideOfCaptures():
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _empty(shape, dtype, device, stream):
+    """A result that the caller has not brought along, of the stream's memory that the call's work runs on: that of another may
+    still be read by work of that one, and would be handed on to it, once the result is dropped, while it is written."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _memory_of(stream):
+        return _made_apart(shape, dtype, device)
+
+
 def _linear_scratch(outs, in_features, tokens, device, stream):
     """Scratch memory for the linear calls below, of the stream's that the call's work runs on, or None where it needs none,
     there is none to be had, or the stream is being captured (by whom is not known here, and an allocation could end it)."""
@@ -440,7 +465,7 @@ def neuzip_linear(weight: Blob, out_features: int, in_features: int, x: torch.Te
     if x.numel() != tokens * in_features:
         raise ValueError("activations must be tokens x in_features")
     if y is None:
-        y = torch.empty((tokens, out_features), dtype=torch.float32, device=x.device)
+        y = _empty((tokens, out_features), torch.float32, x.device, stream)
     if not (y.is_cuda and y.dtype == torch.float32 and y.is_contiguous() and y.numel() == tokens * out_features):
         raise TypeError("expected a contiguous float32 CUDA tensor of tokens x out_features")
     if bias is not None and not (bias.is_cuda and bias.dtype == torch.float32 and bias.is_contiguous()
@@ -464,7 +489,7 @@ def neuzip_linear_batch(weights, out_features, in_features: int, x: torch.Tensor
     _check_tensor(x)
     if ys is None:
         tokens = x.numel() // in_features if in_features else 0
-        ys = [torch.empty((tokens, o), dtype=torch.float32, device=x.device) for o in out_features]
+        ys = [_empty((tokens, o), torch.float32, x.device, stream) for o in out_features]
     tokens = _check_linear(weights, out_features, in_features, x, biases, ys)
     _linear_call(weights, out_features, in_features, x, tokens, biases, ys, stream, "neuzip_linear_batch")
     return ys
@@ -483,14 +508,6 @@ def _expect(t, dtype, shape, what):
     return t
 
 
-def _memory_of(stream):
-    """Tensors made in here are of this stream's memory.  (Any object with a handle will do as a call's stream.)"""
-    if not isinstance(stream, torch.cuda.Stream):
-        # (an external stream of handle 0 would be a new one)
-        stream = torch.cuda.ExternalStream(stream.cuda_stream) if stream.cuda_stream else torch.cuda.default_stream()
-    return torch.cuda.stream(stream)
-
-
 def _own_scratch(size, scratch, device, stream):
     """The caller's scratch memory, or the call's own: of the stream's that its work runs on, so that it is not handed out to
     another one's while it is in use."""
@@ -500,13 +517,9 @@ def _own_scratch(size, scratch, device, stream):
         return scratch
     if size == 0:
         return None
-    if stream is not None:
-        with _memory_of(stream):
-            return _own_scratch(size, None, device, None)
-    if torch.cuda.is_current_stream_capturing():
-        return torch.empty(size, dtype=torch.uint8, device=device)
-    with _OutsideOfCaptures():
-        return torch.empty(size, dtype=torch.uint8, device=device)
+    if stream is None:
+        return _made_apart(size, torch.uint8, device)
+    return _empty(size, torch.uint8, device, stream)
 
 
 def _bytes_of(t):
@@ -519,7 +532,7 @@ def neuzip_embedding(table: Blob, rows: int, features: int, tokens: torch.Tensor
     bf16; a number outside 0 .. rows - 1 names none and yields zeros."""
     _expect(tokens, torch.int64, tokens.shape, "tokens")
     if out is None:
-        out = torch.empty((*tokens.shape, features), dtype=torch.bfloat16, device=tokens.device)
+        out = _empty((*tokens.shape, features), torch.bfloat16, tokens.device, stream)
     _expect(out, torch.bfloat16, (tokens.numel(), features), "out")
     rc = _lib.neuzip_embedding(table.handle, rows, features, _pointer(tokens), tokens.numel(), scale, _pointer(out), _stream_handle(stream))
     if rc != OK:
@@ -538,7 +551,7 @@ def neuzip_embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, rows: in
     features = grad_out.shape[-1] if grad_out.dim() else 0
     _expect(grad_out, torch.bfloat16, (tokens.numel(), features), "grad_out")
     if grad is None:
-        grad = torch.empty((rows, features), dtype=torch.bfloat16, device=grad_out.device)
+        grad = _empty((rows, features), torch.bfloat16, grad_out.device, stream)
     _expect(grad, torch.bfloat16, (rows, features), "grad")
     scratch = _own_scratch(neuzip_embedding_grad_scratch_bytes(tokens.numel(), rows, features), scratch, grad_out.device, stream)
     rc = _lib.neuzip_embedding_grad(_pointer(tokens), tokens.numel(), _pointer(grad_out), rows, features, scale, _pointer(grad),
@@ -565,7 +578,7 @@ def neuzip_gated_linear(gate: Blob, up: Blob, out_features: int, in_features: in
     """h = act(x W_gate^T) * (x W_up^T), bf16, straight from the two compressed weights."""
     tokens = _tokens_of(x, in_features)
     if h is None:
-        h = torch.empty((tokens, out_features), dtype=torch.bfloat16, device=x.device)
+        h = _empty((tokens, out_features), torch.bfloat16, x.device, stream)
     _expect(h, torch.bfloat16, (tokens, out_features), "h")
     scratch = _own_scratch(neuzip_gated_linear_scratch_bytes(out_features, in_features, tokens), scratch, x.device, stream)
     rc = _lib.neuzip_gated_linear(gate.handle, up.handle, out_features, in_features, _pointer(x), tokens, activation, _pointer(h),
@@ -591,11 +604,11 @@ def neuzip_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tens
     tokens, out_features, in_features = _gated_shape(x, w_gate, w_up)
     shape = (tokens, out_features)
     if h is None:
-        h = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+        h = _empty(shape, torch.bfloat16, x.device, stream)
     _expect(h, torch.bfloat16, shape, "h")
     gate = up = None
     if keep is True:
-        gate, up = (torch.empty(shape, dtype=torch.float32, device=x.device) for _ in range(2))
+        gate, up = (_empty(shape, torch.float32, x.device, stream) for _ in range(2))
     elif keep:
         gate, up = keep
         _expect(gate, torch.float32, shape, "gate")
@@ -619,11 +632,11 @@ def neuzip_gated_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Ten
     for t, dtype, what in ((gate, torch.float32, "gate"), (up, torch.float32, "up"), (grad_h, torch.bfloat16, "grad_h")):
         _expect(t, dtype, (tokens, out_features), what)
     if grad_x is True:
-        grad_x = torch.empty((tokens, in_features), dtype=torch.bfloat16, device=x.device)
+        grad_x = _empty((tokens, in_features), torch.bfloat16, x.device, stream)
     elif grad_x is False:
         grad_x = None
     if grad_weights is True:
-        grad_weights = (torch.empty_like(w_gate), torch.empty_like(w_up))
+        grad_weights = tuple(_empty((out_features, in_features), torch.bfloat16, x.device, stream) for _ in range(2))
     elif grad_weights is False:
         grad_weights = (None, None)
     if grad_x is not None:
@@ -661,7 +674,7 @@ def neuzip_linear_adapters(weight: Blob, out_features: int, in_features: int, x:
     if bias is not None:
         _expect(bias, torch.float32, (out_features,), "bias")
     if y is None:
-        y = torch.empty((tokens, out_features), dtype=torch.float32, device=x.device)
+        y = _empty((tokens, out_features), torch.float32, x.device, stream)
     _expect(y, torch.float32, (tokens, out_features), "y")
     scratch = _own_scratch(neuzip_linear_adapters_scratch_bytes(out_features, in_features, tokens, rank), scratch, x.device, stream)
     rc = _lib.neuzip_linear_adapters(weight.handle, out_features, in_features, _pointer(x), tokens, _pointer(bias), _pointer(a),

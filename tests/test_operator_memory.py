@@ -65,6 +65,7 @@ def made(monkeypatch):
 STREAMS = [None, Stream(0x22), Handle(0x33), Handle(0)]
 X, H, SUMS = Stub((TOKENS, IN)), Stub((TOKENS, OUT)), Stub((TOKENS, OUT), F32)
 W = Stub((OUT, IN))
+MANY = Stub((64, IN))     # (as many tokens as the linear layer takes scratch memory for)
 ADAPTED = (Stub((ADAPTERS, RANK, IN)), Stub((ADAPTERS, OUT, RANK)), None, Stub((TOKENS,), I32), None)
 WITH_SCRATCH = {
     "embedding_grad": lambda s: nz.neuzip_embedding_grad(Stub((TOKENS,), I64), X, ROWS, 1.0, Stub((ROWS, IN)), stream=s),
@@ -83,3 +84,33 @@ def expected(stream):
 def test_scratch_memory(made, name, stream):
     WITH_SCRATCH[name](stream)
     assert made == [expected(stream)]
+
+
+# results that the caller has not brought along, and how many tensors with the scratch memory
+OF_ITS_OWN = {
+    "embedding": (1, lambda s: nz.neuzip_embedding(BLOB, ROWS, IN, Stub((TOKENS,), I64), stream=s)),
+    "embedding_grad": (2, lambda s: nz.neuzip_embedding_grad(Stub((TOKENS,), I64), X, ROWS, stream=s)),
+    "gated_linear": (2, lambda s: nz.neuzip_gated_linear(BLOB, BLOB, OUT, IN, X, stream=s)),
+    "gated_forward": (1, lambda s: nz.neuzip_gated_forward(X, W, W, stream=s)),
+    "gated_forward_kept": (3, lambda s: nz.neuzip_gated_forward(X, W, W, keep=True, stream=s)),
+    "gated_backward": (4, lambda s: nz.neuzip_gated_backward(X, W, W, SUMS, SUMS, H, stream=s)),
+    "linear_adapters": (2, lambda s: nz.neuzip_linear_adapters(BLOB, OUT, IN, X, *ADAPTED, stream=s)),
+    "linear": (1, lambda s: nz.neuzip_linear(BLOB, OUT, IN, X, stream=s)),
+    "linear_batch": (2, lambda s: nz.neuzip_linear_batch([BLOB, BLOB], [OUT, OUT], IN, X, stream=s)),
+}
+
+
+@pytest.mark.parametrize("stream", STREAMS)
+@pytest.mark.parametrize("name", OF_ITS_OWN)
+def test_results(made, name, stream):
+    count, call = OF_ITS_OWN[name]
+    call(stream)
+    assert made == [expected(stream)] * count
+
+
+@pytest.mark.parametrize("stream", STREAMS)
+def test_results_beside_the_linear_layers_scratch_memory(made, stream):
+    # (which does without, where all it has of a stream is the handle)
+    nz.neuzip_linear(BLOB, OUT, IN, MANY, stream=stream)
+    nz.neuzip_linear_batch([BLOB, BLOB], [OUT, OUT], IN, MANY, stream=stream)
+    assert made == [expected(stream)] * (3 if type(stream) is Handle else 5)
