@@ -499,11 +499,23 @@ def _pointer(t):
     return ctypes.c_void_p(t.data_ptr() if t is not None else None)
 
 
+def _laid_out_as(t, shape):
+    """Whether t's elements, which are as many as the shape's, lie as the shape has them: dimensions may be taken together (all of them,
+    say) or apart (batch x sequence for tokens, heads for features); others, a transposed matrix's, are another order."""
+    if t.dim() <= 1 or len(shape) <= 1 or tuple(t.shape) == tuple(shape) or t.numel() == 0:
+        return True
+
+    def rows(sizes):    # of how many elements, of every dimension
+        return {math.prod(sizes[i:]) for i in range(len(sizes))} - {1, t.numel()}
+
+    return rows(t.shape) >= rows(shape) or rows(t.shape) <= rows(shape)
+
+
 def _expect(t, dtype, shape, what):
-    """t, a contiguous CUDA tensor of that type and of as many elements as the shape has (its own shape is the caller's affair)."""
+    """t, a contiguous CUDA tensor of that type that holds what a tensor of that shape holds."""
     if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype):
         raise TypeError(f"expected a contiguous {dtype} CUDA tensor: {what}")
-    if t.numel() != math.prod(shape):
+    if t.numel() != math.prod(shape) or not _laid_out_as(t, shape):
         raise ValueError(f"{what} must be {' x '.join(str(s) for s in shape)}")
     return t
 
@@ -564,7 +576,7 @@ def neuzip_embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, rows: in
 def _tokens_of(x, in_features):
     _check_tensor(x)
     tokens = x.numel() // in_features if in_features else 0
-    if x.numel() != tokens * in_features:
+    if x.numel() != tokens * in_features or not _laid_out_as(x, (tokens, in_features)):
         raise ValueError("activations must be tokens x in_features")
     return tokens
 
