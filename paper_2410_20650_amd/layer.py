@@ -112,8 +112,9 @@ class CompressedGatedBlock:
         return pair
 
     def forward(self, x: torch.Tensor, space: torch.Tensor) -> torch.Tensor:
-        """x: tokens x in_features, bf16.  Returns bf16 tokens x out_features.  space: room for both weights."""
-        if x.shape[0] <= 64 and self.in_features % 128 == 0:
+        """x: tokens x in_features, bf16 (batch x sequence for the tokens: the same).  Returns bf16 tokens x out_features.  space: room
+        for both weights."""
+        if x.numel() // self.in_features <= 64 and self.in_features % 128 == 0:
             return nz.neuzip_gated_linear(*self.blobs, self.out_features, self.in_features, x.contiguous(), self.activation)
         return nz.neuzip_gated_forward(x.contiguous(), *self.weights_into(space), self.activation)
 
