@@ -114,7 +114,7 @@ class CompressedGatedBlock:
     def forward(self, x: torch.Tensor, space: torch.Tensor) -> torch.Tensor:
         """x: tokens x in_features, bf16 (batch x sequence for the tokens: the same).  Returns bf16 tokens x out_features.  space: room
         for both weights."""
-        if x.numel() // self.in_features <= 64 and self.in_features % 128 == 0:
+        if 0 < x.numel() // self.in_features <= 64 and self.in_features % 128 == 0:     # (no tokens: nothing to serve)
             return nz.neuzip_gated_linear(*self.blobs, self.out_features, self.in_features, x.contiguous(), self.activation)
         return nz.neuzip_gated_forward(x.contiguous(), *self.weights_into(space), self.activation)
 

@@ -1,4 +1,4 @@
-"""Which path CompressedGatedBlock.forward takes: up to 64 tokens from the blobs, more from temporary space, however x has its
+"""Which path CompressedGatedBlock.forward takes: up to 64 tokens from the blobs, more (or none) from temporary space, however x has its
 tokens.  No GPU: the library's calls are noted, not made.
 """
 import types
@@ -22,8 +22,8 @@ def block(monkeypatch):
     return block, taken
 
 
-@pytest.mark.parametrize("shape,path", [((1, IN), "blobs"), ((64, IN), "blobs"), ((65, IN), "space"), ((4, 1024, IN), "space"),
-                                        ((1, 65, IN), "space"), ((65, 1, IN), "space"), ((4, 16, IN), "blobs"), ((IN,), "blobs")])
+@pytest.mark.parametrize("shape,path", [((1, IN), "blobs"), ((64, IN), "blobs"), ((65, IN), "space"), ((0, IN), "space"), ((4, 1024, IN), "space"),
+                                        ((1, 65, IN), "space"), ((65, 1, IN), "space"), ((100, 0, IN), "space"), ((4, 16, IN), "blobs"), ((IN,), "blobs")])
 def test_tokens_are_counted(block, shape, path):
     block, taken = block
     block.forward(torch.zeros(shape, dtype=torch.bfloat16), torch.zeros(2 * OUT * IN, dtype=torch.bfloat16))
