@@ -137,8 +137,13 @@ def library():
 
 
 def _stream_handle(stream):
-    if stream is None:  # (torch.cuda.current_stream() makes an object of it first: 3 us of the host's 8 for a small call)
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    if stream is None:
+        # (torch.cuda.current_stream() makes an object of it first: 3 us of the host's 8 for a small call; the other is torch's own affair
+        # and may be gone from one version to the next)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return ctypes.c_void_p(raw(torch.cuda.current_device()))
+        stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
 
