@@ -19,9 +19,9 @@
 #include <cstdint>
 #include <type_traits>
 
-namespace nz {
+#include "neuzip_gated_shape.h"
 
-enum GatedForm { kForward, kInputGrad, kWeightGrad };
+namespace nz {
 
 struct GatedArgs {
     const uint16_t *q[2];   // kForward: x, x;  kInputGrad: dg, du;  kWeightGrad: dg, du
@@ -103,7 +103,6 @@ __device__ __forceinline__ void each_of(const F &f)
 // Along k: a row of the tile is 64 k, 128 bytes, 8 pieces of 16 bytes, piece p of row r in place p ^ (r / 2 % 8).
 // Across k: a row is one k and its R values, in units of 16 values; unit u of row k in place u ^ f(k), f = k % 4 + 4 * (k / 8 % 2):
 // the eight rows that half a wave reads a unit of at a time then lie in different banks.
-constexpr uint32_t kGatedDepth = 64;
 template <int R, int WAVES, bool ALONG>
 struct GatedOperand {
     static constexpr uint32_t kBytes = R * kGatedDepth * 2;
