@@ -27,6 +27,13 @@ template <GatedForm FORM>
 inline GatedShape gated_shape(uint64_t rows, uint64_t cols, uint64_t depth)
 {
     const double steps = static_cast<double>(tiles_of(depth, kGatedDepth)) * (FORM == kInputGrad ? 2 : 1);
+    // Sums of fewer than four steps fill no ring of four, and tiles of 256 are then all beginning and end: 128, two held, without a look at
+    // the figures above, which are of longer sums (128 with two held / with four / 256, us: weight gradients of 8 to 192 tokens, 256 -> 640
+    // 6.5-7.5 / 6.4-8.3 / 10.9-13.3, 1160 -> 2808 9.2-12.3 / 11.2-15.3 / 11.5-16.1, 4096 -> 14336 60-87 / 96-138 / 71-98; forward of 64 to 192
+    // features, 64 to 2048 tokens, 4096 outputs 4.1-13.6 / 4.1-19.7 / 9.1-14.1; input gradient of 32 and 64 outputs, 4096 features,
+    // 6.1-10.3 / 6.3-12.7 / 10.1-14.6.  By those figures few tiles would have four held: 7.7 -> 8.3, 4.8 -> 5.1.)
+    if (steps < 4)
+        return {128, 2, 1};
     GatedShape best = {128, 2, 1};
     double least = 0;
     for (uint32_t size = 128; size <= 256; size += 128) {
