@@ -13,7 +13,7 @@ SOURCES = [os.path.join(HERE, "csrc", name) for name in ("neuzip.hip", "neuzip_e
 HEADERS = [os.path.join(ROOT, "include", "neuzip.h")] + [
     os.path.join(HERE, "csrc", name)
     for name in ("neuzip_format.h", "neuzip_host.h", "neuzip_walk.h", "neuzip_compress_kernels.h", "neuzip_decode_kernels.h",
-                 "neuzip_linear_front.h", "neuzip_linear_kernels.h", "neuzip_linear_launch.h", "neuzip_embedding_kernels.h",
+                 "neuzip_linear_kernels.h", "neuzip_linear_launch.h", "neuzip_embedding_kernels.h",
                  "neuzip_gated_shape.h", "neuzip_gated_kernels.h", "neuzip_adapters_kernels.h")]
 
 HIPCC_FLAGS = [
