@@ -133,7 +133,7 @@ uint64_t neuzip_embedding_grad_scratch_bytes(uint64_t count, uint64_t rows, uint
     if (!valid_table(rows, features) || count >= (1ull << 31) || few_parts(count, rows, features))
         return 0;
     const uint64_t runs = (count + kSortRun - 1) / kSortRun;
-    return runs * sizeof(SortedRun) + (count > kBlockTokens ? runs * kPieces * features * sizeof(float) : 0);
+    return runs * (sizeof(SortedRun) + kPieces * features * sizeof(float));
 }
 
 int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d_grad_out, uint64_t rows, uint64_t features, float scale,
@@ -182,10 +182,10 @@ int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d
         launch_sort<1024>(a, stream);
     else
         launch_sort<256>(a, stream);
-    if (count > kBlockTokens)
+    if (count > 0) {
         hipLaunchKernelGGL(embedding_pieces_kernel, dim3(kPieces, a.n_runs, strips), dim3(kGradThreads), 0, stream, a);
-    if (count > 0)
         hipLaunchKernelGGL(embedding_rows_kernel, dim3(most, a.n_runs, strips), dim3(kGradThreads), 0, stream, a);
+    }
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
 

@@ -247,7 +247,7 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
 //             which is counted, 32 elements to a workgroup, so that a run is sorted by many CUs in one go (one workgroup with a
 //             bitonic network in LDS took 45 us for 4096 tokens).  Counted the same way: where the rows of each of 2048 ranges begin
 //             in the run.
-//   pieces    (more than 64 tokens) a row whose tokens pass the end of a block of 64 sorted places is summed block by block, in
+//   pieces    a row whose tokens pass the end of a block of 64 sorted places is summed block by block, in
 //             binary32, so that a token that is very frequent is no workgroup's work alone
 //   rows      a workgroup to a row with tokens, at the first of them, adds its tokens up, or its pieces, and stores it.
 // Most of the work for a large table is zeros: the first launch's other workgroups fill the gradient with them meanwhile (4096
