@@ -367,7 +367,8 @@ int neuzip_embedding(const neuzip_blob *table, uint64_t rows, uint64_t features,
  *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_embedding_grad_scratch_bytes(), 16-byte aligned, in use until
  *               the call's work has run (NULL where that is 0).
  * The sums are held in binary32 and formed in an order that depends on the tokens alone, so that a call's result is the same every
- * time; scaled and rounded once.  Never allocates, never synchronises.
+ * time; scaled and rounded once.  Never allocates, never synchronises.  More than 268431360 tokens (65535 runs of 4096) or rows of more
+ * than 134215680 features -> EUNSUPPORTED.
  */
 int neuzip_embedding_grad(const int64_t *d_tokens, uint64_t count, const void *d_grad_out, uint64_t rows, uint64_t features, float scale,
                           void *d_grad, void *d_scratch, uint64_t scratch_bytes, void *hip_stream);
