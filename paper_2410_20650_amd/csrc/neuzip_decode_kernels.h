@@ -859,14 +859,14 @@ __device__ __forceinline__ void decode_from_entries(const DecodeArgs &a, uint32_
         atomicOr(a.status, 1u);
 }
 
-// The LDS of a workgroup.  The words come first: a direct copy's LDS address has 16 bits.
+// The LDS of a workgroup.  The words come first: on 16 bytes, as direct copies need it.
 template <int KB, bool MADE>
 struct DecodeLds {
     uint8_t stage[kStageBytesOf<KB>];
     uint32_t lut[kM];
     uint2 spread[kSpreadEntries<KB>];
     uint32_t steps[MADE ? kSteps : 2];
-    static_assert(kStageBytesOf<KB> <= 65536 && kStageBytesOf<KB> % 16 == 0, "within reach, and the table behind it aligned");
+    static_assert(kStageBytesOf<KB> % 16 == 0, "the table behind it is aligned");
 };
 
 template <int KB, bool NORM, int MODE, bool SPLIT>

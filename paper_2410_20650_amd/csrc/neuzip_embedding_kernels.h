@@ -109,7 +109,7 @@ __global__ __launch_bounds__(THREADS) void embedding_kernel(const EmbeddingArgs 
 {
     constexpr uint32_t kWaves = THREADS / 64;
     __shared__ __align__(16) struct {
-        uint8_t stage[kWaves * kEmbWindow];  // first: a direct copy's LDS address has 16 bits
+        uint8_t stage[kWaves * kEmbWindow];  // first: on 16 bytes, as direct copies need it
         uint32_t lut[kM];
         uint32_t steps[kSteps];
     } lds;
@@ -291,8 +291,8 @@ __global__ __launch_bounds__(THREADS) void embedding_sort_kernel(const Embedding
         return;
     }
     const uint32_t of_run = a.sort_wgs == 0 ? 0u : blockIdx.x / a.sort_wgs, group = blockIdx.x - of_run * a.sort_wgs;
-    // Queries are the run's elements, then the ranges' first rows.  A wave's lanes hold the 32 queries twice, for two halves of
-    // the wave's quarter of the run.
+    // Queries are the run's elements, then the ranges' first rows.  A wave's lanes hold the 32 queries twice, for the two parts of the run
+    // that are the wave's (of 8 parts in a workgroup of 256 threads, of 32 in one of 1024).
     constexpr uint32_t kParts = THREADS / kSortQueries;
     __shared__ __align__(16) uint32_t rows[kSortRun];
     __shared__ uint32_t before[kSortQueries];

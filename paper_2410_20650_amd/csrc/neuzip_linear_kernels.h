@@ -672,7 +672,7 @@ template <int KB, int COLS, int MT, bool NORM, bool READ, bool EAGER>
 __device__ __forceinline__ void linear_batch_workgroup(const LinearBatchArgs &b)
 {
     __shared__ __align__(16) struct {
-        uint8_t stage[kLinStageBytes];  // first: a direct copy's LDS address has 16 bits
+        uint8_t stage[kLinStageBytes];  // first: on 16 bytes, as direct copies need it
         uint32_t lut[kM];
         float area[kLinAreaBytes / 4];
         uint32_t steps[READ ? 4 : kSteps];
