@@ -507,7 +507,7 @@ def _pointer(t):
 def _laid_out_as(t, shape):
     """Whether t's elements, which are as many as the shape's, lie as the shape has them: dimensions may be taken together (all of them,
     say) or apart (batch x sequence for tokens, heads for features); others, a transposed matrix's, are another order."""
-    if t.dim() <= 1 or len(shape) <= 1 or tuple(t.shape) == tuple(shape) or t.numel() == 0:
+    if t.dim() <= 1 or len(shape) <= 1 or t.numel() == 0:
         return True
 
     def rows(sizes):    # of how many elements, of every dimension
@@ -520,7 +520,7 @@ def _expect(t, dtype, shape, what):
     """t, a contiguous CUDA tensor of that type that holds what a tensor of that shape holds."""
     if not (t.is_cuda and t.is_contiguous() and t.dtype == dtype):
         raise TypeError(f"expected a contiguous {dtype} CUDA tensor: {what}")
-    if t.numel() != math.prod(shape) or not _laid_out_as(t, shape):
+    if t.shape != shape and (t.numel() != math.prod(shape) or not _laid_out_as(t, shape)):
         raise ValueError(f"{what} must be {' x '.join(str(s) for s in shape)}")
     return t
 
@@ -581,7 +581,8 @@ def neuzip_embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, rows: in
 def _tokens_of(x, in_features):
     _check_tensor(x)
     tokens = x.numel() // in_features if in_features else 0
-    if x.numel() != tokens * in_features or not _laid_out_as(x, (tokens, in_features)):
+    shape = (tokens, in_features)
+    if x.shape != shape and (x.numel() != tokens * in_features or not _laid_out_as(x, shape)):
         raise ValueError("activations must be tokens x in_features")
     return tokens
 
