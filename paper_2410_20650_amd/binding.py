@@ -550,7 +550,8 @@ def neuzip_embedding(table: Blob, rows: int, features: int, tokens: torch.Tensor
     _expect(tokens, torch.int64, tokens.shape, "tokens")
     if out is None:
         out = _empty((*tokens.shape, features), torch.bfloat16, tokens.device, stream)
-    _expect(out, torch.bfloat16, (tokens.numel(), features), "out")
+    else:
+        _expect(out, torch.bfloat16, (tokens.numel(), features), "out")
     rc = _lib.neuzip_embedding(table.handle, rows, features, _pointer(tokens), tokens.numel(), scale, _pointer(out), _stream_handle(stream))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_embedding")
@@ -569,7 +570,8 @@ def neuzip_embedding_grad(tokens: torch.Tensor, grad_out: torch.Tensor, rows: in
     _expect(grad_out, torch.bfloat16, (tokens.numel(), features), "grad_out")
     if grad is None:
         grad = _empty((rows, features), torch.bfloat16, grad_out.device, stream)
-    _expect(grad, torch.bfloat16, (rows, features), "grad")
+    else:
+        _expect(grad, torch.bfloat16, (rows, features), "grad")
     scratch = _own_scratch(neuzip_embedding_grad_scratch_bytes(tokens.numel(), rows, features), scratch, grad_out.device, stream)
     rc = _lib.neuzip_embedding_grad(_pointer(tokens), tokens.numel(), _pointer(grad_out), rows, features, scale, _pointer(grad),
                                     _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
@@ -597,7 +599,8 @@ def neuzip_gated_linear(gate: Blob, up: Blob, out_features: int, in_features: in
     tokens = _tokens_of(x, in_features)
     if h is None:
         h = _empty((tokens, out_features), torch.bfloat16, x.device, stream)
-    _expect(h, torch.bfloat16, (tokens, out_features), "h")
+    else:
+        _expect(h, torch.bfloat16, (tokens, out_features), "h")
     scratch = _own_scratch(neuzip_gated_linear_scratch_bytes(out_features, in_features, tokens), scratch, x.device, stream)
     rc = _lib.neuzip_gated_linear(gate.handle, up.handle, out_features, in_features, _pointer(x), tokens, activation, _pointer(h),
                                   _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
@@ -623,7 +626,8 @@ def neuzip_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tens
     shape = (tokens, out_features)
     if h is None:
         h = _empty(shape, torch.bfloat16, x.device, stream)
-    _expect(h, torch.bfloat16, shape, "h")
+    else:
+        _expect(h, torch.bfloat16, shape, "h")
     gate = up = None
     if keep is True:
         gate, up = (_empty(shape, torch.float32, x.device, stream) for _ in range(2))
@@ -653,15 +657,16 @@ def neuzip_gated_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Ten
         grad_x = _empty((tokens, in_features), torch.bfloat16, x.device, stream)
     elif grad_x is False:
         grad_x = None
+    elif grad_x is not None:
+        _expect(grad_x, torch.bfloat16, (tokens, in_features), "grad_x")
     if grad_weights is True:
-        grad_weights = tuple(_empty((out_features, in_features), torch.bfloat16, x.device, stream) for _ in range(2))
+        grad_weights = [_empty((out_features, in_features), torch.bfloat16, x.device, stream) for _ in range(2)]
     elif grad_weights is False:
         grad_weights = (None, None)
-    if grad_x is not None:
-        _expect(grad_x, torch.bfloat16, (tokens, in_features), "grad_x")
-    for t in grad_weights:
-        if t is not None:
-            _expect(t, torch.bfloat16, (out_features, in_features), "grad_weights")
+    else:
+        for t in grad_weights:
+            if t is not None:
+                _expect(t, torch.bfloat16, (out_features, in_features), "grad_weights")
     scratch = _own_scratch(neuzip_gated_backward_scratch_bytes(tokens, out_features, in_features), scratch, x.device, stream)
     rc = _lib.neuzip_gated_backward(_pointer(x), _pointer(w_gate), _pointer(w_up), _pointer(gate), _pointer(up), _pointer(grad_h),
                                     tokens, out_features, in_features, activation, _pointer(grad_x), _pointer(grad_weights[0]),
@@ -693,7 +698,8 @@ def neuzip_linear_adapters(weight: Blob, out_features: int, in_features: int, x:
         _expect(bias, torch.float32, (out_features,), "bias")
     if y is None:
         y = _empty((tokens, out_features), torch.float32, x.device, stream)
-    _expect(y, torch.float32, (tokens, out_features), "y")
+    else:
+        _expect(y, torch.float32, (tokens, out_features), "y")
     scratch = _own_scratch(neuzip_linear_adapters_scratch_bytes(out_features, in_features, tokens, rank), scratch, x.device, stream)
     rc = _lib.neuzip_linear_adapters(weight.handle, out_features, in_features, _pointer(x), tokens, _pointer(bias), _pointer(a),
                                      _pointer(b), rank, adapters, _pointer(scales), _pointer(ids), _pointer(y), _pointer(scratch),
