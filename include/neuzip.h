@@ -386,7 +386,8 @@ enum { NEUZIP_SILU = 0, NEUZIP_GELU_TANH = 1 };
  *   d_h         tokens x out_features bf16 words, row-major; overwritten.
  *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_gated_linear_scratch_bytes(), 16-byte aligned, in use until
  *               the call's work has run.
- * The two sums, the activation and the product are binary32; h is rounded once.  Never allocates, never synchronises.
+ * The two sums, the activation and the product are binary32; h is rounded once.  The sums are neuzip_linear's, whose last bits can
+ * differ from run to run.  Never allocates, never synchronises.
  */
 int neuzip_gated_linear(const neuzip_blob *gate, const neuzip_blob *up, uint64_t out_features, uint64_t in_features, const void *d_x,
                         uint32_t tokens, int activation, void *d_h, void *d_scratch, uint64_t scratch_bytes, void *hip_stream);
@@ -433,7 +434,8 @@ uint64_t neuzip_gated_backward_scratch_bytes(uint64_t tokens, uint64_t out_featu
  *   d_ids       the adapter of each token, 32-bit integers; outside 0 .. adapters - 1: the token has none.
  *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_linear_adapters_scratch_bytes(), 16-byte aligned, in use until
  *               the call's work has run.
- * The low products A x and all sums are binary32.  Never allocates, never synchronises.
+ * The low products A x and all sums are binary32; W_hat x is neuzip_linear's, whose last bits can differ from run to run.  As there, more
+ * than 64 tokens decode the weight once for every 64.  Never allocates, never synchronises.
  */
 int neuzip_linear_adapters(const neuzip_blob *weight, uint64_t out_features, uint64_t in_features, const void *d_x, uint32_t tokens,
                            const float *d_bias, const void *d_a, const void *d_b, uint32_t rank, uint32_t adapters,

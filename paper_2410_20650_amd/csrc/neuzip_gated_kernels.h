@@ -10,8 +10,8 @@
 // The operand that supplies i or j lies with k along its rows (x and the weights in kForward, dg and du in kInputGrad), or with k
 // down its columns (the others).
 //
-// Measured, 2048 tokens, 4096 -> 2 x 14336 (481 * 10^9 operations each): forward with both sums kept 416 us, input gradient 356 and 13 for
-// its slices, weight gradients 414; forward of 1000 tokens 183 = 1284 TFLOP/s.  The matrix cores are busy in 0.56 to 0.72 of the cycles; with
+// Measured, 2048 tokens, 4096 -> 2 x 14336 (481 * 10^9 operations each): forward with both sums kept 398 to 416 us, input gradient 334 to 356
+// and 13 for its slices, weight gradients 387 to 414; forward of 1000 tokens 184 = 1277 TFLOP/s.  The matrix cores are busy in 0.56 to 0.72 of the cycles; with
 // operands of zeros, and the clock at 2.4 instead of 2.0 GHz, the same launches take 15 to 25 % less: power is what bounds them.
 #pragma once
 
