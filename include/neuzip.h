@@ -443,6 +443,146 @@ int neuzip_linear_adapters(const neuzip_blob *weight, uint64_t out_features, uin
                            void *hip_stream);
 uint64_t neuzip_linear_adapters_scratch_bytes(uint64_t out_features, uint64_t in_features, uint32_t tokens, uint32_t rank);
 
+/*
+ * neuzip_norm -- what stands between two layers of a model: the layer's result is added to the stream, and the next layer takes the
+ * stream's rows divided by their root mean square.
+ *     total <- T(x + residual),   y <- bf16(total / sqrt(mean(total^2) + eps) * weight)
+ *
+ *   d_x         tokens x width values of x_type (NEUZIP_BF16, or NEUZIP_F32: what neuzip_linear leaves), row-major.
+ *   d_residual, d_total   the stream before and after, tokens x width values of total_type (T); d_total may be d_residual.  Both NULL:
+ *               there is no stream yet, total is x itself (and total_type is x_type).
+ *   d_weight    width floats.
+ *   width       a multiple of 8, at most 16384 (else EINVAL).  eps at least 0.
+ *   d_y         tokens x width bf16 words, what the linear layers take; overwritten.
+ * The sum x + residual is rounded once, to T, and the norm is that of the rounded values, which the backward pass is given; squares,
+ * sums and products are binary32, y is rounded once.  All pointers aligned to 16 bytes.  tokens = 0 does nothing; 2^24 tokens and more ->
+ * EUNSUPPORTED.  Results do not change from run to run.  Never allocates, never synchronises.
+ */
+int neuzip_norm(const void *d_x, int x_type, const void *d_residual, void *d_total, int total_type, const float *d_weight, uint64_t tokens,
+                uint64_t width, float eps, void *d_y, void *hip_stream);
+
+/*
+ * neuzip_norm_backward -- its gradients.  With n = 1 / sqrt(mean(total^2) + eps) of a token and g = grad_y * weight:
+ *     grad_x <- bf16(grad_total + n * (g - total * n^2 * mean(g * total))),   grad_weight <- sum over the tokens of grad_y * total * n
+ *
+ *   d_total, total_type   the stream as neuzip_norm left it (its x, where there was no stream).
+ *   d_grad_y    tokens x width bf16 words.
+ *   d_grad_total   tokens x width bf16 words, the gradient that comes back along the stream; NULL: none does.
+ *   d_grad_x    tokens x width bf16 words, the gradient of x and of residual, which is one; may be d_grad_y or d_grad_total; NULL: not wanted.
+ *   d_grad_weight   width floats; overwritten (no tokens: zeros); NULL: not wanted.
+ *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_norm_backward_scratch_bytes(), 16-byte aligned, in use until the
+ *               call's work has run; only where d_grad_weight is wanted (else NULL will do).
+ * Otherwise as neuzip_norm.  The sums over the tokens are formed in an order that depends on tokens and width alone.
+ */
+int neuzip_norm_backward(const void *d_total, int total_type, const float *d_weight, const void *d_grad_y, const void *d_grad_total,
+                         uint64_t tokens, uint64_t width, float eps, void *d_grad_x, float *d_grad_weight, void *d_scratch,
+                         uint64_t scratch_bytes, void *hip_stream);
+uint64_t neuzip_norm_backward_scratch_bytes(uint64_t tokens, uint64_t width);
+
+/*
+ * The cache of the keys and values that attention looks back at, in 8 bits: pages of page_tokens tokens, a scale for each page and head.
+ * Element types and order are what the attention kernels read without rearranging: keys token by token, values feature by feature.
+ *
+ *   d_k         pages x heads x page_tokens x head_dim bytes in e4m3 (4 bits of exponent, 3 of mantissa, largest 448, no infinity).
+ *   d_v         pages x heads x head_dim x page_tokens bytes, likewise.
+ *   d_k_scales, d_v_scales   pages x heads floats, powers of two: a byte stands for its value times its page's and head's scale.
+ *   heads, head_dim, page_tokens   head_dim 64 or 128, page_tokens 16, 32, 64 or 128 (else EINVAL).
+ * d_k and d_v are aligned to 16 bytes.  A new cache needs no filling: what no token was put to is not read for its value.
+ */
+typedef struct {
+    void *d_k, *d_v;
+    float *d_k_scales, *d_v_scales;
+    uint32_t pages, heads, head_dim, page_tokens;
+} neuzip_cache;
+
+/*
+ * The sequences of a call, ragged: sequence s has the rows d_starts[s] .. d_starts[s + 1] - 1 of the call's tensors, its newest tokens, and with
+ * them d_lengths[s] tokens in all; token p of it is in page d_table[s * table_width + p / page_tokens] of the cache, at p % page_tokens.
+ *
+ *   d_starts    count + 1 32-bit integers, ascending.  Rows from d_starts[count] on belong to nobody (a padded batch): they are not
+ *               read, and what they are in an output stays as it is.
+ *   d_lengths   count 32-bit integers.  A sequence with fewer tokens than rows, or with more than table_width * page_tokens, is left out: nothing
+ *               of it is appended, its rows of an attention's output are zeros.
+ *   d_table     count x table_width 32-bit integers.  A number outside 0 .. pages - 1 names no page: nothing is put there, and its tokens
+ *               are not seen.  (With a window, pages that no token sees any more may be given back.)
+ * All three are read on the device when the call's work runs, so that a captured graph follows them.  Several sequences may share pages that
+ * are only read.
+ */
+typedef struct {
+    const int32_t *d_starts, *d_lengths, *d_table;
+    uint32_t count, table_width;
+} neuzip_sequences;
+
+/*
+ * neuzip_cache_append -- the newest tokens' keys and values, as the projections left them, into the cache; the queries made ready on the way.
+ *     k' <- rotate(k, p),  e <- the least integer from -100 on with |k'| <= 448 * 2^e for the new tokens of the page and head,
+ *     byte <- e4m3(k' * 2^-e),  scale <- 2^e           and so with v, which is not rotated;  q_out <- bf16(rotate(q, p))
+ *     rotate(x, p)[i] = x[i] cos - x[i + D/2] sin,  rotate(x, p)[i + D/2] = x[i + D/2] cos + x[i] sin   for i < D/2, D = head_dim
+ *
+ * A page whose first tokens were there before keeps its scale if it is the larger one; if not, their bytes are rounded to the new one.
+ * (By powers of two: only values that become subnormal change.)  Roundings are to nearest even; the angles' products and sums binary32,
+ * each rounded.  Infinities become +-448 times the scale, NaN stays NaN; neither counts for a scale.
+ *
+ *   type        of k, v and q: NEUZIP_F32 or NEUZIP_BF16.
+ *   d_k, d_v    rows x heads x head_dim; from one row to the next k_row, v_row elements (at least heads * head_dim; parts of a projection's
+ *               result), multiples of 16 bytes.
+ *   d_q, q_row, q_heads, d_q_out   likewise, q_heads heads; d_q_out rows x q_heads x head_dim bf16 words without gaps.  Both NULL: no queries.
+ *   d_rotary    rotary_rows x head_dim floats: of position p the head_dim / 2 cosines, then the sines; rotary_rows at least table_width * page_tokens
+ *               (else EINVAL).  NULL (and 0): nothing is rotated.
+ *   rows        of the tensors.
+ * A page that is appended to belongs to one sequence, and to no other call at that time.  All pointers to values are aligned to 16 bytes.
+ * Never allocates, never synchronises; results do not change from run to run.
+ */
+int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *sequences, int type, const void *d_k, uint64_t k_row,
+                        const void *d_v, uint64_t v_row, const void *d_q, uint64_t q_row, uint32_t q_heads, void *d_q_out,
+                        const float *d_rotary, uint64_t rotary_rows, uint32_t rows, void *hip_stream);
+
+/*
+ * neuzip_cache_attention -- attention of the newest tokens over their sequences' cache, causal: the token at position p sees the keys
+ * at positions j <= p, with a window those at j > p - window.
+ *     out <- bf16(sum_j softmax_j(scale * q . k_j) v_j);   a token that sees no key: zeros
+ *
+ *   d_q, q_row  rows x q_heads x head_dim bf16 words, q_row elements from one row to the next (a multiple of 8).  q_heads is a multiple of the cache's heads;
+ *               query head h reads the cache's head h / (q_heads / heads).
+ *   window      0: none.
+ *   longest     no sequence has more tokens; 0: table_width * page_tokens.  (It decides how the work is split, so it may be too high, not too low:
+ *               results are the same but for the order of sums.)
+ *   d_out       rows x q_heads x head_dim bf16 words.
+ *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_cache_attention_scratch_bytes(), 16-byte aligned, in use until the call's
+ *               work has run (NULL where that is 0).
+ * Keys and values are taken as the cache holds them; scores, maxima, sums and the output's sums are binary32, the weights of the softmax are
+ * rounded to bf16 for the matrix cores (relative error 2^-9 each), out is rounded once.  A key that a token does not see has no influence, whatever
+ * it holds.  rows * q_heads up to 2^27 - 1 (else EUNSUPPORTED).  Never allocates, never synchronises; results do not change from run to run.
+ */
+int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *sequences, const void *d_q, uint64_t q_row, uint32_t q_heads,
+                           uint32_t rows, float scale, uint32_t window, uint64_t longest, void *d_out, void *d_scratch,
+                           uint64_t scratch_bytes, void *hip_stream);
+uint64_t neuzip_cache_attention_scratch_bytes(const neuzip_cache *cache, const neuzip_sequences *sequences, uint32_t q_heads, uint32_t rows,
+                                              uint64_t longest);
+
+/*
+ * neuzip_logits -- what is done to the output projection's result before a token is taken from it, row by row.  With c = how often a token
+ * occurs in the row's history, for each of them in this order:
+ *     c > 0:  x <- x > 0 ? x / repetition : x * repetition;   x <- x - frequency * c;   c > 0:  x <- x - presence;
+ *     x <- x + its bias;   not allowed by the row's mask:  x <- -infinity
+ *
+ *   d_logits, d_out   rows x vocab floats, row-major; d_out may be d_logits.
+ *   history     d_tokens[d_starts[r]] .. d_tokens[d_starts[r + 1] - 1] is row r's, 64-bit integers (a number outside 0 .. vocab - 1 counts for
+ *               nothing).  d_starts: rows + 1 32-bit integers, ascending.  history_tokens = 0: no history.
+ *   d_repetition, d_frequency, d_presence   a float for each row; NULL: 1, 0, 0.
+ *   biases      d_bias_tokens, d_bias_starts as the history's, d_bias_values a float for each entry; of entries for one token in one row the last
+ *               counts.  bias_entries = 0: none.
+ *   d_masks     masks x ceil(vocab / 32) 32-bit words: token v is allowed if bit v % 32 of word v / 32 is set.  d_mask_ids: the mask of each row,
+ *               32-bit integers; outside 0 .. masks - 1: everything is allowed.  Both NULL: no masks.  (A mask that allows nothing leaves a row of -infinity.)
+ *   history_tokens, bias_entries   how many tokens and entries there are: starts beyond them are taken as them.
+ * Each operation is rounded to binary32 by itself.  vocab below 2^31, rows up to 65535 (else EUNSUPPORTED); pointers aligned to their elements.
+ * Never allocates, never synchronises; results do not change from run to run.
+ */
+int neuzip_logits(const float *d_logits, uint32_t rows, uint64_t vocab, const int64_t *d_history, uint64_t history_tokens,
+                  const int32_t *d_history_starts, const float *d_repetition, const float *d_frequency, const float *d_presence,
+                  const int64_t *d_bias_tokens, const float *d_bias_values, uint64_t bias_entries, const int32_t *d_bias_starts,
+                  const int32_t *d_masks, uint32_t masks, const int32_t *d_mask_ids, float *d_out, void *hip_stream);
+
 /* Releases the blob and its device memory.  NULL is a no-op. */
 void neuzip_free(neuzip_blob *blob);
 

@@ -27,6 +27,18 @@ class NeuzipError(RuntimeError):
         self.code = code
 
 
+class _Cache(ctypes.Structure):
+    """neuzip_cache"""
+    _fields_ = [("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_k_scales", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p),
+                ("pages", ctypes.c_uint32), ("heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("page_tokens", ctypes.c_uint32)]
+
+
+class _Sequences(ctypes.Structure):
+    """neuzip_sequences"""
+    _fields_ = [("d_starts", ctypes.c_void_p), ("d_lengths", ctypes.c_void_p), ("d_table", ctypes.c_void_p),
+                ("count", ctypes.c_uint32), ("table_width", ctypes.c_uint32)]
+
+
 def _load():
     if not os.path.exists(_build.LIB):
         _build.build()
@@ -105,10 +117,20 @@ def _load():
     lib.neuzip_gated_backward_scratch_bytes.argtypes = [u64, u64, u64]
     lib.neuzip_linear_adapters.argtypes = [vp, u64, u64, vp, u32, vp, vp, vp, u32, u32, vp, vp, vp, vp, u64, vp]
     lib.neuzip_linear_adapters_scratch_bytes.argtypes = [u64, u64, u32, u32]
+    cache, sequences = ctypes.POINTER(_Cache), ctypes.POINTER(_Sequences)
+    lib.neuzip_norm.argtypes = [vp, i32, vp, vp, i32, vp, u64, u64, f32, vp, vp]
+    lib.neuzip_norm_backward.argtypes = [vp, i32, vp, vp, vp, u64, u64, f32, vp, vp, vp, u64, vp]
+    lib.neuzip_norm_backward_scratch_bytes.argtypes = [u64, u64]
+    lib.neuzip_cache_append.argtypes = [cache, sequences, i32, vp, u64, vp, u64, vp, u64, u32, vp, vp, u64, u32, vp]
+    lib.neuzip_cache_attention.argtypes = [cache, sequences, vp, u64, u32, u32, f32, u32, u64, vp, vp, u64, vp]
+    lib.neuzip_cache_attention_scratch_bytes.argtypes = [cache, sequences, u32, u32, u64]
+    lib.neuzip_logits.argtypes = [vp, u32, u64, vp, u64, vp, vp, vp, vp, vp, vp, u64, vp, vp, u32, vp, vp, vp]
     for name in ("neuzip_embedding", "neuzip_embedding_grad", "neuzip_gated_linear", "neuzip_gated_forward", "neuzip_gated_backward",
-                 "neuzip_linear_adapters"):
+                 "neuzip_linear_adapters", "neuzip_norm", "neuzip_norm_backward", "neuzip_cache_append", "neuzip_cache_attention",
+                 "neuzip_logits"):
         getattr(lib, name).restype = i32
-    for name in ("neuzip_embedding_grad", "neuzip_gated_linear", "neuzip_gated_backward", "neuzip_linear_adapters"):
+    for name in ("neuzip_embedding_grad", "neuzip_gated_linear", "neuzip_gated_backward", "neuzip_linear_adapters", "neuzip_norm_backward",
+                 "neuzip_cache_attention"):
         getattr(lib, name + "_scratch_bytes").restype = u64
     lib.neuzip_strerror.argtypes = [i32]
     lib.neuzip_strerror.restype = ctypes.c_char_p
@@ -126,6 +148,8 @@ EXPORTED = ["neuzip_compress", "neuzip_compress_noalloc", "neuzip_compress_block
             "neuzip_embedding", "neuzip_embedding_grad", "neuzip_embedding_grad_scratch_bytes",
             "neuzip_gated_linear", "neuzip_gated_linear_scratch_bytes", "neuzip_gated_forward", "neuzip_gated_backward",
             "neuzip_gated_backward_scratch_bytes", "neuzip_linear_adapters", "neuzip_linear_adapters_scratch_bytes",
+            "neuzip_norm", "neuzip_norm_backward", "neuzip_norm_backward_scratch_bytes", "neuzip_cache_append", "neuzip_cache_attention",
+            "neuzip_cache_attention_scratch_bytes", "neuzip_logits",
             "neuzip_block_size", "neuzip_decompress", "neuzip_decompress_sequence", "neuzip_decompress_batch", "neuzip_free",
             "neuzip_compressed_bytes", "neuzip_device_bytes", "neuzip_elems", "neuzip_mantissa_bits", "neuzip_dtype",
             "neuzip_export", "neuzip_import", "neuzip_histogram", "neuzip_frequencies", "neuzip_check", "neuzip_stream_probe",
@@ -707,6 +731,281 @@ def neuzip_linear_adapters(weight: Blob, out_features: int, in_features: int, x:
     if rc != OK:
         raise NeuzipError(rc, "neuzip_linear_adapters")
     return y
+
+
+def _here(*tensors):
+    """The tensors that are there are on the current device, where the call's kernels run."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError(f"expected tensors on the current device, cuda:{device}, not {t.device}")
+
+
+_STREAM_TYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _type_of(t, what):
+    if t.dtype not in _STREAM_TYPES:
+        raise TypeError(f"expected a contiguous bf16 or float32 CUDA tensor: {what}")
+    return _STREAM_TYPES[t.dtype]
+
+
+def neuzip_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor = None, y: torch.Tensor = None,
+                total: torch.Tensor = None, stream=None):
+    """total = x + residual in the residual's type, y = total / rms(total) * weight in bf16.  x, residual: tokens x width (bf16 or float32, each its
+    own); weight: float32.  Returns (y, total); without a residual y alone, the norm of x.  total may be the residual."""
+    width = weight.numel()
+    _expect(weight, torch.float32, (width,), "weight")
+    x_type = _type_of(x, "x")
+    tokens = x.numel() // width if width else 0
+    shape = (tokens, width)
+    _expect(x, x.dtype, shape, "x")
+    total_type = x_type
+    if residual is not None:
+        total_type = _type_of(residual, "residual")
+        _expect(residual, residual.dtype, shape, "residual")
+        if total is None:
+            total = _empty(residual.shape, residual.dtype, x.device, stream)
+        else:
+            _expect(total, residual.dtype, shape, "total")
+    elif total is not None:
+        raise ValueError("total is x where there is no residual")
+    if y is None:
+        y = _empty(x.shape, torch.bfloat16, x.device, stream)
+    else:
+        _expect(y, torch.bfloat16, shape, "y")
+    _here(x, weight, residual, total, y)
+    rc = _lib.neuzip_norm(_pointer(x), x_type, _pointer(residual), _pointer(total), total_type, _pointer(weight), tokens, width, eps,
+                          _pointer(y), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_norm")
+    return y if residual is None else (y, total)
+
+
+def neuzip_norm_backward_scratch_bytes(tokens: int, width: int) -> int:
+    return int(_lib.neuzip_norm_backward_scratch_bytes(tokens, width))
+
+
+def neuzip_norm_backward(total: torch.Tensor, weight: torch.Tensor, grad_y: torch.Tensor, eps: float, grad_total: torch.Tensor = None,
+                         grad_x=True, grad_weight=True, scratch=None, stream=None):
+    """(grad_x, grad_weight): the gradient (bf16) of x, which is the residual's too, and that of the weight (float32).  total: the stream that
+    neuzip_norm left (x, where there was none); grad_total: the gradient that comes back along it (bf16), or None.  grad_x and grad_weight: True,
+    False (not wanted: None), or the tensors that receive them; grad_x may be grad_y or grad_total."""
+    width = weight.numel()
+    _expect(weight, torch.float32, (width,), "weight")
+    total_type = _type_of(total, "total")
+    tokens = total.numel() // width if width else 0
+    shape = (tokens, width)
+    _expect(total, total.dtype, shape, "total")
+    _expect(grad_y, torch.bfloat16, shape, "grad_y")
+    if grad_total is not None:
+        _expect(grad_total, torch.bfloat16, shape, "grad_total")
+    if grad_x is True:
+        grad_x = _empty(grad_y.shape, torch.bfloat16, total.device, stream)
+    elif grad_x is False:
+        grad_x = None
+    elif grad_x is not None:
+        _expect(grad_x, torch.bfloat16, shape, "grad_x")
+    if grad_weight is True:
+        grad_weight = _empty((width,), torch.float32, total.device, stream)
+    elif grad_weight is False:
+        grad_weight = None
+    elif grad_weight is not None:
+        _expect(grad_weight, torch.float32, (width,), "grad_weight")
+    if grad_weight is not None:
+        scratch = _own_scratch(neuzip_norm_backward_scratch_bytes(tokens, width), scratch, total.device, stream)
+    _here(total, weight, grad_y, grad_total, grad_x, grad_weight, scratch)
+    rc = _lib.neuzip_norm_backward(_pointer(total), total_type, _pointer(weight), _pointer(grad_y), _pointer(grad_total), tokens, width, eps,
+                                   _pointer(grad_x), _pointer(grad_weight), _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_norm_backward")
+    return grad_x, grad_weight
+
+
+class KeyValueCache:
+    """The keys and values of tokens so far, in 8 bits (neuzip_cache).  k: pages x heads x page_tokens x head_dim, v: pages x heads x head_dim x
+    page_tokens (torch.float8_e4m3fn), k_scales, v_scales: pages x heads (float32, powers of two)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
+        if k.dim() != 4:
+            raise ValueError("k must be pages x heads x page_tokens x head_dim")
+        pages, heads, page, dim = k.shape
+        if dim not in (64, 128) or page not in (16, 32, 64, 128):
+            raise ValueError("heads of 64 or 128 features, pages of 16, 32, 64 or 128 tokens")
+        _expect(k, torch.float8_e4m3fn, (pages, heads, page, dim), "k")
+        if v.shape != (pages, heads, dim, page):
+            raise ValueError("v must be pages x heads x head_dim x page_tokens")
+        _expect(v, torch.float8_e4m3fn, (pages, heads, dim, page), "v")
+        _expect(k_scales, torch.float32, (pages, heads), "k_scales")
+        _expect(v_scales, torch.float32, (pages, heads), "v_scales")
+        if not (k.device == v.device == k_scales.device == v_scales.device):
+            raise ValueError("the tensors of a cache are on one device")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.pages, self.heads, self.page_tokens, self.head_dim = pages, heads, page, dim
+        self._struct = _Cache(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), pages, heads, dim, page)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, head_dim: int, page_tokens: int = 64, device="cuda"):
+        """A new cache.  Its memory is not filled: pages that nothing was put to are not read for their values."""
+        return cls(torch.empty((pages, heads, page_tokens, head_dim), dtype=torch.float8_e4m3fn, device=device),
+                   torch.empty((pages, heads, head_dim, page_tokens), dtype=torch.float8_e4m3fn, device=device),
+                   *(torch.empty((pages, heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+class Sequences:
+    """The ragged sequences of a call (neuzip_sequences), int32: starts (sequences + 1: whose rows are whose), lengths (tokens of each, with the rows'),
+    table (sequences x pages of each, in order).  The tensors may change between calls; they are read when a call's work runs."""
+
+    def __init__(self, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
+        if table.dim() != 2:
+            raise ValueError("table must be sequences x pages")
+        count, width = table.shape
+        _expect(table, torch.int32, (count, width), "table")
+        _expect(starts, torch.int32, (count + 1,), "starts")
+        _expect(lengths, torch.int32, (count,), "lengths")
+        if not (starts.device == lengths.device == table.device):
+            raise ValueError("the tensors of a call's sequences are on one device")
+        self.starts, self.lengths, self.table = starts, lengths, table
+        self._struct = _Sequences(starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), count, width)
+
+
+def _rows_of(t, heads, dim, dtype, what):
+    """t as rows x heads x dim whose rows may lie apart (parts of a projection's result).  Returns (rows, elements from row to row)."""
+    if not t.is_cuda or t.dtype != dtype:
+        raise TypeError(f"expected a {dtype} CUDA tensor: {what}")
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 3 and shape[1] == heads and shape[2] == dim:
+        flat = strides[2] == 1 and (heads == 1 or strides[1] == dim)
+    elif len(shape) == 2 and shape[1] == heads * dim:
+        flat = strides[1] == 1
+    else:
+        raise ValueError(f"{what} must be rows x {heads} x {dim}")
+    row = strides[0] if shape[0] > 1 else heads * dim
+    if not flat or row < heads * dim or row * t.element_size() % 16:
+        raise ValueError(f"{what}: rows without gaps, from one to the next a multiple of 16 bytes")
+    return shape[0], row
+
+
+def neuzip_cache_append(cache: KeyValueCache, sequences: Sequences, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor = None,
+                        rotary: torch.Tensor = None, q_out: torch.Tensor = None, stream=None):
+    """Puts the newest tokens' keys and values (rows x heads x head_dim, bf16 or float32; parts of one tensor's rows will do) into the cache, the keys
+    rotated to their positions by `rotary` (positions x head_dim, float32: the cosines of head_dim / 2 angles, then the sines; None: not).  With
+    queries (rows x query heads x head_dim): returns them rotated, in bf16, as neuzip_cache_attention takes them."""
+    kind = _type_of(k, "k")
+    heads, dim = cache.heads, cache.head_dim
+    rows, k_row = _rows_of(k, heads, dim, k.dtype, "k")
+    v_rows, v_row = _rows_of(v, heads, dim, k.dtype, "v")
+    if v_rows != rows:
+        raise ValueError("k and v have the same rows")
+    q_heads = q_row = 0
+    if q is not None:
+        q_heads = q.shape[-2] if q.dim() == 3 else q.shape[-1] // dim
+        q_rows, q_row = _rows_of(q, q_heads, dim, k.dtype, "q")
+        if q_rows != rows or q_heads == 0:
+            raise ValueError("q has the rows of k")
+        if q_out is None:
+            q_out = _empty((rows, q_heads, dim), torch.bfloat16, k.device, stream)
+        else:
+            _expect(q_out, torch.bfloat16, (rows, q_heads, dim), "q_out")
+    elif q_out is not None:
+        raise ValueError("no queries, no q_out")
+    rotary_rows = 0
+    if rotary is not None:
+        rotary_rows = rotary.shape[0]
+        _expect(rotary, torch.float32, (rotary_rows, dim), "rotary")
+        if rotary_rows < sequences._struct.table_width * cache.page_tokens:
+            raise ValueError("rotary must have a row for each position that the table has room for")
+    _here(cache.k, sequences.starts, k, v, q, rotary, q_out)
+    rc = _lib.neuzip_cache_append(cache._struct, sequences._struct, kind, _pointer(k), k_row, _pointer(v), v_row, _pointer(q), q_row, q_heads,
+                                  _pointer(q_out), _pointer(rotary), rotary_rows, rows, _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_cache_append")
+    return q_out
+
+
+def neuzip_cache_attention_scratch_bytes(cache: KeyValueCache, sequences: Sequences, q_heads: int, rows: int, longest: int = 0) -> int:
+    return int(_lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, longest))
+
+
+def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.Tensor, scale: float = None, window: int = 0,
+                           longest: int = 0, out: torch.Tensor = None, scratch=None, stream=None) -> torch.Tensor:
+    """Causal attention of the newest tokens' queries (rows x query heads x head_dim, bf16) over the cache; bf16, in q's shape.  scale: 1 / sqrt(head_dim)
+    if None; window: how many keys a token sees at most, its own among them (0: all before it); longest: no sequence has more tokens (0: as
+    many as the table has room for)."""
+    dim = cache.head_dim
+    q_heads = q.shape[-2] if q.dim() == 3 else q.shape[-1] // dim if q.dim() else 0
+    rows, q_row = _rows_of(q, q_heads, dim, torch.bfloat16, "q")
+    if q_heads == 0 or q_heads % cache.heads:
+        raise ValueError("the query heads are a multiple of the cache's heads")
+    if out is None:
+        out = _empty(q.shape, torch.bfloat16, q.device, stream)
+    else:
+        _expect(out, torch.bfloat16, (rows, q_heads, dim), "out")
+    if scale is None:
+        scale = 1.0 / math.sqrt(dim)
+    scratch = _own_scratch(neuzip_cache_attention_scratch_bytes(cache, sequences, q_heads, rows, longest), scratch, q.device, stream)
+    _here(cache.k, sequences.starts, q, out, scratch)
+    rc = _lib.neuzip_cache_attention(cache._struct, sequences._struct, _pointer(q), q_row, q_heads, rows, scale, window, longest, _pointer(out),
+                                     _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_cache_attention")
+    return out
+
+
+def _entries(tokens, starts, rows, what):
+    if tokens is None:
+        if starts is not None:
+            raise ValueError(f"{what} and its starts come together")
+        return 0
+    count = tokens.numel()
+    _expect(tokens, torch.int64, (count,), what)
+    if starts is None:
+        raise ValueError(f"{what} and its starts come together")
+    _expect(starts, torch.int32, (rows + 1,), what + "_starts")
+    return count
+
+
+def neuzip_logits(logits: torch.Tensor, history: torch.Tensor = None, history_starts: torch.Tensor = None, repetition: torch.Tensor = None,
+                  frequency: torch.Tensor = None, presence: torch.Tensor = None, bias: torch.Tensor = None, bias_values: torch.Tensor = None,
+                  bias_starts: torch.Tensor = None, masks: torch.Tensor = None, mask_ids: torch.Tensor = None, out: torch.Tensor = None,
+                  stream=None) -> torch.Tensor:
+    """Penalties for tokens of the rows' histories, biases, and grammars' masks on logits (rows x vocab, float32).  history: int64, the rows' one behind the
+    other, history_starts: int32, rows + 1; repetition, frequency, presence: float32, one for each row (None: 1, 0, 0).  bias: int64 tokens,
+    bias_values: float32, bias_starts as history_starts; of two entries for a token the later one counts.  masks: masks x ceil(vocab / 32) int32, bit v % 32 of
+    word v / 32 allows token v; mask_ids: int32, the mask of each row, outside 0 .. masks - 1 none.  out may be logits."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be rows x vocab")
+    rows, vocab = logits.shape
+    _expect(logits, torch.float32, (rows, vocab), "logits")
+    history_tokens = _entries(history, history_starts, rows, "history")
+    entries = _entries(bias, bias_starts, rows, "bias")
+    if (bias is None) != (bias_values is None):
+        raise ValueError("bias and bias_values come together")
+    if bias_values is not None:
+        _expect(bias_values, torch.float32, (entries,), "bias_values")
+    for t, what in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence")):
+        if t is not None:
+            _expect(t, torch.float32, (rows,), what)
+    count = 0
+    if (masks is None) != (mask_ids is None):
+        raise ValueError("masks and mask_ids come together")
+    if masks is not None:
+        count = masks.shape[0] if masks.dim() else 0
+        _expect(masks, torch.int32, (count, (vocab + 31) // 32), "masks")
+        _expect(mask_ids, torch.int32, (rows,), "mask_ids")
+        if count == 0:
+            masks = mask_ids = None
+    if out is None:
+        out = _empty(logits.shape, torch.float32, logits.device, stream)
+    else:
+        _expect(out, torch.float32, (rows, vocab), "out")
+    _here(logits, history, history_starts, repetition, frequency, presence, bias, bias_values, bias_starts, masks, mask_ids, out)
+    rc = _lib.neuzip_logits(_pointer(logits), rows, vocab, _pointer(history), history_tokens, _pointer(history_starts), _pointer(repetition),
+                            _pointer(frequency), _pointer(presence), _pointer(bias), _pointer(bias_values), entries, _pointer(bias_starts),
+                            _pointer(masks), count, _pointer(mask_ids), _pointer(out), _stream_handle(stream))
+    if rc != OK:
+        raise NeuzipError(rc, "neuzip_logits")
+    return out
 
 
 def neuzip_free(blob: Blob) -> None:

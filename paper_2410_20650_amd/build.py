@@ -9,12 +9,14 @@ ROOT = os.path.dirname(HERE)
 LIB = os.environ.get("NEUZIP_LIBRARY") or os.path.join(HERE, "libneuzip.so")
 BUILT_LIB = os.path.join(HERE, "libneuzip.so")
 # (the codec's translation unit first: it is the one whose kernels' metadata the tests read)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("neuzip.hip", "neuzip_embedding.hip", "neuzip_gated.hip", "neuzip_adapters.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("neuzip.hip", "neuzip_embedding.hip", "neuzip_gated.hip", "neuzip_adapters.hip",
+                                                   "neuzip_norm.hip", "neuzip_cache.hip", "neuzip_logits.hip")]
 HEADERS = [os.path.join(ROOT, "include", "neuzip.h")] + [
     os.path.join(HERE, "csrc", name)
     for name in ("neuzip_format.h", "neuzip_host.h", "neuzip_walk.h", "neuzip_compress_kernels.h", "neuzip_decode_kernels.h",
                  "neuzip_linear_kernels.h", "neuzip_linear_launch.h", "neuzip_embedding_kernels.h",
-                 "neuzip_gated_shape.h", "neuzip_gated_kernels.h", "neuzip_adapters_kernels.h")]
+                 "neuzip_gated_shape.h", "neuzip_gated_kernels.h", "neuzip_adapters_kernels.h", "neuzip_norm_kernels.h",
+                 "neuzip_cache_kernels.h", "neuzip_attention_kernels.h", "neuzip_logits_kernels.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
