@@ -733,12 +733,27 @@ def neuzip_linear_adapters(weight: Blob, out_features: int, in_features: int, x:
     return y
 
 
-def _here(*tensors):
-    """The tensors that are there are on the current device, where the call's kernels run."""
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != device:
-            raise ValueError(f"expected tensors on the current device, cuda:{device}, not {t.device}")
+def _here(t, dtype, shape, what, device):
+    """_expect of a tensor on the current device, where the call's kernels run.  (Most are as they should be: one look at each thing.)"""
+    if not (t.shape == shape and t.dtype == dtype and t.get_device() == device and t.is_contiguous()):
+        _expect(t, dtype, shape, what)
+        if t.get_device() != device:
+            raise ValueError(f"{what} must be on the current device, cuda:{device}")
+    return t
+
+
+def _scratch_here(size, scratch, t, device, stream):
+    scratch = _own_scratch(size, scratch, t.device, stream)
+    if scratch is not None and scratch.get_device() != device:
+        raise ValueError(f"scratch memory must be on the current device, cuda:{device}")
+    return scratch
+
+
+def _empty_like(t, dtype, stream):
+    """_empty of t's shape and device."""
+    if stream is None:
+        return torch.empty_like(t, dtype=dtype)
+    return _empty(t.shape, dtype, t.device, stream)
 
 
 _STREAM_TYPES = {torch.bfloat16: BF16, torch.float32: F32}
@@ -754,29 +769,28 @@ def neuzip_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: tor
                 total: torch.Tensor = None, stream=None):
     """total = x + residual in the residual's type, y = total / rms(total) * weight in bf16.  x, residual: tokens x width (bf16 or float32, each its
     own); weight: float32.  Returns (y, total); without a residual y alone, the norm of x.  total may be the residual."""
+    device = torch.cuda.current_device()
     width = weight.numel()
-    _expect(weight, torch.float32, (width,), "weight")
-    x_type = _type_of(x, "x")
+    _here(weight, torch.float32, (width,), "weight", device)
+    x_type = total_type = _type_of(x, "x")
     tokens = x.numel() // width if width else 0
     shape = (tokens, width)
-    _expect(x, x.dtype, shape, "x")
-    total_type = x_type
+    _here(x, x.dtype, shape, "x", device)
     if residual is not None:
         total_type = _type_of(residual, "residual")
-        _expect(residual, residual.dtype, shape, "residual")
+        _here(residual, residual.dtype, shape, "residual", device)
         if total is None:
-            total = _empty(residual.shape, residual.dtype, x.device, stream)
-        else:
-            _expect(total, residual.dtype, shape, "total")
+            total = _empty_like(residual, residual.dtype, stream)
+        elif total is not residual:
+            _here(total, residual.dtype, shape, "total", device)
     elif total is not None:
         raise ValueError("total is x where there is no residual")
     if y is None:
-        y = _empty(x.shape, torch.bfloat16, x.device, stream)
+        y = _empty_like(x, torch.bfloat16, stream)
     else:
-        _expect(y, torch.bfloat16, shape, "y")
-    _here(x, weight, residual, total, y)
-    rc = _lib.neuzip_norm(_pointer(x), x_type, _pointer(residual), _pointer(total), total_type, _pointer(weight), tokens, width, eps,
-                          _pointer(y), _stream_handle(stream))
+        _here(y, torch.bfloat16, shape, "y", device)
+    rc = _lib.neuzip_norm(x.data_ptr(), x_type, _pointer(residual), _pointer(total), total_type, weight.data_ptr(), tokens, width, eps,
+                          y.data_ptr(), _stream_handle(stream))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_norm")
     return y if residual is None else (y, total)
@@ -791,31 +805,31 @@ def neuzip_norm_backward(total: torch.Tensor, weight: torch.Tensor, grad_y: torc
     """(grad_x, grad_weight): the gradient (bf16) of x, which is the residual's too, and that of the weight (float32).  total: the stream that
     neuzip_norm left (x, where there was none); grad_total: the gradient that comes back along it (bf16), or None.  grad_x and grad_weight: True,
     False (not wanted: None), or the tensors that receive them; grad_x may be grad_y or grad_total."""
+    device = torch.cuda.current_device()
     width = weight.numel()
-    _expect(weight, torch.float32, (width,), "weight")
+    _here(weight, torch.float32, (width,), "weight", device)
     total_type = _type_of(total, "total")
     tokens = total.numel() // width if width else 0
     shape = (tokens, width)
-    _expect(total, total.dtype, shape, "total")
-    _expect(grad_y, torch.bfloat16, shape, "grad_y")
+    _here(total, total.dtype, shape, "total", device)
+    _here(grad_y, torch.bfloat16, shape, "grad_y", device)
     if grad_total is not None:
-        _expect(grad_total, torch.bfloat16, shape, "grad_total")
+        _here(grad_total, torch.bfloat16, shape, "grad_total", device)
     if grad_x is True:
-        grad_x = _empty(grad_y.shape, torch.bfloat16, total.device, stream)
+        grad_x = _empty_like(grad_y, torch.bfloat16, stream)
     elif grad_x is False:
         grad_x = None
     elif grad_x is not None:
-        _expect(grad_x, torch.bfloat16, shape, "grad_x")
+        _here(grad_x, torch.bfloat16, shape, "grad_x", device)
     if grad_weight is True:
-        grad_weight = _empty((width,), torch.float32, total.device, stream)
+        grad_weight = _empty_like(weight, torch.float32, stream)
     elif grad_weight is False:
         grad_weight = None
     elif grad_weight is not None:
-        _expect(grad_weight, torch.float32, (width,), "grad_weight")
+        _here(grad_weight, torch.float32, (width,), "grad_weight", device)
     if grad_weight is not None:
-        scratch = _own_scratch(neuzip_norm_backward_scratch_bytes(tokens, width), scratch, total.device, stream)
-    _here(total, weight, grad_y, grad_total, grad_x, grad_weight, scratch)
-    rc = _lib.neuzip_norm_backward(_pointer(total), total_type, _pointer(weight), _pointer(grad_y), _pointer(grad_total), tokens, width, eps,
+        scratch = _scratch_here(_lib.neuzip_norm_backward_scratch_bytes(tokens, width), scratch, total, device, stream)
+    rc = _lib.neuzip_norm_backward(total.data_ptr(), total_type, weight.data_ptr(), grad_y.data_ptr(), _pointer(grad_total), tokens, width, eps,
                                    _pointer(grad_x), _pointer(grad_weight), _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_norm_backward")
@@ -838,10 +852,11 @@ class KeyValueCache:
         _expect(v, torch.float8_e4m3fn, (pages, heads, dim, page), "v")
         _expect(k_scales, torch.float32, (pages, heads), "k_scales")
         _expect(v_scales, torch.float32, (pages, heads), "v_scales")
-        if not (k.device == v.device == k_scales.device == v_scales.device):
+        if not k.get_device() == v.get_device() == k_scales.get_device() == v_scales.get_device():
             raise ValueError("the tensors of a cache are on one device")
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
         self.pages, self.heads, self.page_tokens, self.head_dim = pages, heads, page, dim
+        self.device = k.get_device()
         self._struct = _Cache(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), pages, heads, dim, page)
 
     @classmethod
@@ -863,16 +878,19 @@ class Sequences:
         _expect(table, torch.int32, (count, width), "table")
         _expect(starts, torch.int32, (count + 1,), "starts")
         _expect(lengths, torch.int32, (count,), "lengths")
-        if not (starts.device == lengths.device == table.device):
+        if not starts.get_device() == lengths.get_device() == table.get_device():
             raise ValueError("the tensors of a call's sequences are on one device")
         self.starts, self.lengths, self.table = starts, lengths, table
+        self.device = table.get_device()
         self._struct = _Sequences(starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), count, width)
 
 
-def _rows_of(t, heads, dim, dtype, what):
+def _rows_of(t, heads, dim, dtype, what, device):
     """t as rows x heads x dim whose rows may lie apart (parts of a projection's result).  Returns (rows, elements from row to row)."""
     if not t.is_cuda or t.dtype != dtype:
         raise TypeError(f"expected a {dtype} CUDA tensor: {what}")
+    if t.get_device() != device:
+        raise ValueError(f"{what} must be on the current device, cuda:{device}")
     shape, strides = t.shape, t.stride()
     if len(shape) == 3 and shape[1] == heads and shape[2] == dim:
         flat = strides[2] == 1 and (heads == 1 or strides[1] == dim)
@@ -886,37 +904,45 @@ def _rows_of(t, heads, dim, dtype, what):
     return shape[0], row
 
 
+def _cached_on(cache, sequences):
+    """The current device, which a cache and a call's sequences are on."""
+    device = torch.cuda.current_device()
+    if cache.device != device or sequences.device != device:
+        raise ValueError(f"the cache and the sequences must be on the current device, cuda:{device}")
+    return device
+
+
 def neuzip_cache_append(cache: KeyValueCache, sequences: Sequences, k: torch.Tensor, v: torch.Tensor, q: torch.Tensor = None,
                         rotary: torch.Tensor = None, q_out: torch.Tensor = None, stream=None):
     """Puts the newest tokens' keys and values (rows x heads x head_dim, bf16 or float32; parts of one tensor's rows will do) into the cache, the keys
     rotated to their positions by `rotary` (positions x head_dim, float32: the cosines of head_dim / 2 angles, then the sines; None: not).  With
     queries (rows x query heads x head_dim): returns them rotated, in bf16, as neuzip_cache_attention takes them."""
+    device = _cached_on(cache, sequences)
     kind = _type_of(k, "k")
     heads, dim = cache.heads, cache.head_dim
-    rows, k_row = _rows_of(k, heads, dim, k.dtype, "k")
-    v_rows, v_row = _rows_of(v, heads, dim, k.dtype, "v")
+    rows, k_row = _rows_of(k, heads, dim, k.dtype, "k", device)
+    v_rows, v_row = _rows_of(v, heads, dim, k.dtype, "v", device)
     if v_rows != rows:
         raise ValueError("k and v have the same rows")
     q_heads = q_row = 0
     if q is not None:
         q_heads = q.shape[-2] if q.dim() == 3 else q.shape[-1] // dim
-        q_rows, q_row = _rows_of(q, q_heads, dim, k.dtype, "q")
+        q_rows, q_row = _rows_of(q, q_heads, dim, k.dtype, "q", device)
         if q_rows != rows or q_heads == 0:
             raise ValueError("q has the rows of k")
         if q_out is None:
             q_out = _empty((rows, q_heads, dim), torch.bfloat16, k.device, stream)
         else:
-            _expect(q_out, torch.bfloat16, (rows, q_heads, dim), "q_out")
+            _here(q_out, torch.bfloat16, (rows, q_heads, dim), "q_out", device)
     elif q_out is not None:
         raise ValueError("no queries, no q_out")
     rotary_rows = 0
     if rotary is not None:
         rotary_rows = rotary.shape[0]
-        _expect(rotary, torch.float32, (rotary_rows, dim), "rotary")
+        _here(rotary, torch.float32, (rotary_rows, dim), "rotary", device)
         if rotary_rows < sequences._struct.table_width * cache.page_tokens:
             raise ValueError("rotary must have a row for each position that the table has room for")
-    _here(cache.k, sequences.starts, k, v, q, rotary, q_out)
-    rc = _lib.neuzip_cache_append(cache._struct, sequences._struct, kind, _pointer(k), k_row, _pointer(v), v_row, _pointer(q), q_row, q_heads,
+    rc = _lib.neuzip_cache_append(cache._struct, sequences._struct, kind, k.data_ptr(), k_row, v.data_ptr(), v_row, _pointer(q), q_row, q_heads,
                                   _pointer(q_out), _pointer(rotary), rotary_rows, rows, _stream_handle(stream))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_cache_append")
@@ -932,36 +958,36 @@ def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.
     """Causal attention of the newest tokens' queries (rows x query heads x head_dim, bf16) over the cache; bf16, in q's shape.  scale: 1 / sqrt(head_dim)
     if None; window: how many keys a token sees at most, its own among them (0: all before it); longest: no sequence has more tokens (0: as
     many as the table has room for)."""
+    device = _cached_on(cache, sequences)
     dim = cache.head_dim
     q_heads = q.shape[-2] if q.dim() == 3 else q.shape[-1] // dim if q.dim() else 0
-    rows, q_row = _rows_of(q, q_heads, dim, torch.bfloat16, "q")
+    rows, q_row = _rows_of(q, q_heads, dim, torch.bfloat16, "q", device)
     if q_heads == 0 or q_heads % cache.heads:
         raise ValueError("the query heads are a multiple of the cache's heads")
     if out is None:
         out = _empty(q.shape, torch.bfloat16, q.device, stream)
     else:
-        _expect(out, torch.bfloat16, (rows, q_heads, dim), "out")
+        _here(out, torch.bfloat16, (rows, q_heads, dim), "out", device)
     if scale is None:
         scale = 1.0 / math.sqrt(dim)
-    scratch = _own_scratch(neuzip_cache_attention_scratch_bytes(cache, sequences, q_heads, rows, longest), scratch, q.device, stream)
-    _here(cache.k, sequences.starts, q, out, scratch)
-    rc = _lib.neuzip_cache_attention(cache._struct, sequences._struct, _pointer(q), q_row, q_heads, rows, scale, window, longest, _pointer(out),
+    scratch = _scratch_here(_lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, longest), scratch, q, device, stream)
+    rc = _lib.neuzip_cache_attention(cache._struct, sequences._struct, q.data_ptr(), q_row, q_heads, rows, scale, window, longest, out.data_ptr(),
                                      _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_cache_attention")
     return out
 
 
-def _entries(tokens, starts, rows, what):
+def _entries(tokens, starts, rows, what, device):
     if tokens is None:
         if starts is not None:
             raise ValueError(f"{what} and its starts come together")
         return 0
     count = tokens.numel()
-    _expect(tokens, torch.int64, (count,), what)
+    _here(tokens, torch.int64, (count,), what, device)
     if starts is None:
         raise ValueError(f"{what} and its starts come together")
-    _expect(starts, torch.int32, (rows + 1,), what + "_starts")
+    _here(starts, torch.int32, (rows + 1,), what + "_starts", device)
     return count
 
 
@@ -973,36 +999,36 @@ def neuzip_logits(logits: torch.Tensor, history: torch.Tensor = None, history_st
     other, history_starts: int32, rows + 1; repetition, frequency, presence: float32, one for each row (None: 1, 0, 0).  bias: int64 tokens,
     bias_values: float32, bias_starts as history_starts; of two entries for a token the later one counts.  masks: masks x ceil(vocab / 32) int32, bit v % 32 of
     word v / 32 allows token v; mask_ids: int32, the mask of each row, outside 0 .. masks - 1 none.  out may be logits."""
+    device = torch.cuda.current_device()
     if logits.dim() != 2:
         raise ValueError("logits must be rows x vocab")
     rows, vocab = logits.shape
-    _expect(logits, torch.float32, (rows, vocab), "logits")
-    history_tokens = _entries(history, history_starts, rows, "history")
-    entries = _entries(bias, bias_starts, rows, "bias")
+    _here(logits, torch.float32, (rows, vocab), "logits", device)
+    history_tokens = _entries(history, history_starts, rows, "history", device)
+    entries = _entries(bias, bias_starts, rows, "bias", device)
     if (bias is None) != (bias_values is None):
         raise ValueError("bias and bias_values come together")
     if bias_values is not None:
-        _expect(bias_values, torch.float32, (entries,), "bias_values")
+        _here(bias_values, torch.float32, (entries,), "bias_values", device)
     for t, what in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence")):
         if t is not None:
-            _expect(t, torch.float32, (rows,), what)
+            _here(t, torch.float32, (rows,), what, device)
     count = 0
     if (masks is None) != (mask_ids is None):
         raise ValueError("masks and mask_ids come together")
     if masks is not None:
         count = masks.shape[0] if masks.dim() else 0
-        _expect(masks, torch.int32, (count, (vocab + 31) // 32), "masks")
-        _expect(mask_ids, torch.int32, (rows,), "mask_ids")
+        _here(masks, torch.int32, (count, (vocab + 31) // 32), "masks", device)
+        _here(mask_ids, torch.int32, (rows,), "mask_ids", device)
         if count == 0:
             masks = mask_ids = None
     if out is None:
-        out = _empty(logits.shape, torch.float32, logits.device, stream)
-    else:
-        _expect(out, torch.float32, (rows, vocab), "out")
-    _here(logits, history, history_starts, repetition, frequency, presence, bias, bias_values, bias_starts, masks, mask_ids, out)
-    rc = _lib.neuzip_logits(_pointer(logits), rows, vocab, _pointer(history), history_tokens, _pointer(history_starts), _pointer(repetition),
+        out = _empty_like(logits, torch.float32, stream)
+    elif out is not logits:
+        _here(out, torch.float32, (rows, vocab), "out", device)
+    rc = _lib.neuzip_logits(logits.data_ptr(), rows, vocab, _pointer(history), history_tokens, _pointer(history_starts), _pointer(repetition),
                             _pointer(frequency), _pointer(presence), _pointer(bias), _pointer(bias_values), entries, _pointer(bias_starts),
-                            _pointer(masks), count, _pointer(mask_ids), _pointer(out), _stream_handle(stream))
+                            _pointer(masks), count, _pointer(mask_ids), out.data_ptr(), _stream_handle(stream))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_logits")
     return out

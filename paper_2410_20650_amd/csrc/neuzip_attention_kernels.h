@@ -35,7 +35,7 @@ struct AttendArgs {
     float2 *stats;      // ... and the rows' maximum and sum
     uint32_t q_heads, group;
     uint32_t window;
-    uint32_t splits;
+    uint32_t splits, tiles;
     float scale;        // times log2(e)
 };
 
@@ -294,6 +294,261 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
         const attend_f32x4_t v = {sum[d] * once, sum[d + 1] * once, sum[d + 2] * once, sum[d + 3] * once};
         *reinterpret_cast<bf16x4_t *>(a.out + to * DIM + at + d) = __builtin_convertvector(v, bf16x4_t);
     }
+}
+
+// ---- many rows: a workgroup has 128, a wave 32 of them.  A step's keys and values are widened once, by all four waves, into LDS, from where every wave
+// reads them as operands; the next step's bytes are on their way meanwhile, and the pages of the one behind it.  Here the lane (row c = l % 32, half
+// h = l / 32) has of every 32 keys the ones 16 h .. 16 h + 15.
+// In LDS: row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4, its pieces of 16 bytes (8 features) in places p ^ c % kPieces;
+// the values' row is a feature, 64 keys in 8 pieces, in places p ^ feature % 8: what 8 lanes read together lies in different banks.
+constexpr uint32_t kAttendManyRows = 128;
+constexpr float kAttendSlack = 6.0f;  // by so much (a factor of 64) a row's weights may exceed 1 before its sums are scaled down to a new maximum
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float attend_f32x16_t;
+
+__device__ __forceinline__ float attend_max_of_halves(float v)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    const uint32_t low = both[0], high = both[1];  // (a bit cast of both[1] itself is taken for both[0]'s)
+    return fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
+}
+
+template <uint32_t DIM>
+struct alignas(16) AttendStep {  // of 64 keys in LDS
+    uint8_t k[kAttendStep * DIM * 2];
+    uint8_t v[DIM * kAttendStep * 2];
+    uint32_t nans[4];   // by the waves that filled it: NaN among the values
+    uint32_t there;     // bit i: keys 16 i .. 16 i + 15 have a page and are seen by some row
+};
+
+template <uint32_t DIM>
+__global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const AttendArgs a)
+{
+    constexpr uint32_t kPieces = DIM / 8, kItems = DIM / 64;  // items: 16 bytes of the cache, of keys and of values, to a thread
+    __shared__ AttendStep<DIM> steps[2];
+    const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
+    const TileNumbers numbers = {kAttendManyRows, a.group, 1};
+    const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
+    if (s >= a.s.count)
+        return;
+    const NewTokens n = new_tokens(a.s, s);
+    const uint64_t row0_wide = (tile - first_tile(numbers, a.s.starts[s], s)) * kAttendManyRows;
+    const uint32_t rows = n.count * a.group;
+    if (row0_wide >= rows)
+        return;
+    const uint32_t row0 = static_cast<uint32_t>(row0_wide), row_end = rows - row0 < kAttendManyRows ? rows : row0 + kAttendManyRows;
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 32, h = lane / 32;
+    const AttendRange range = attend_range(n, row0 / a.group, (row_end - 1) / a.group, a.window);
+    uint32_t step, last;
+    attend_split(range, split, a.splits, step, last);
+
+    // the wave's rows, and the lane's
+    const uint32_t wave0 = row0 + wave * 32 < row_end ? row0 + wave * 32 : row_end - 1, wave_end = wave0 + 32 < row_end ? wave0 + 32 : row_end;
+    const AttendRange of_wave = attend_range(n, wave0 / a.group, (wave_end - 1) / a.group, a.window);
+    const bool mine = row0 + wave * 32 + c < row_end;
+    const uint32_t row = mine ? row0 + wave * 32 + c : row_end - 1, position = n.first + row / a.group;
+    const uint32_t my_high = mine ? position + 1 : 0, my_low = a.window && position + 1 > a.window ? position + 1 - a.window : 0;
+    attend_bf16x8_t q[DIM / 16];
+    const uint16_t *q_at = a.q + (n.begin + row / a.group) * a.q_row + (head * a.group + row % a.group) * DIM + h * 8;
+#pragma unroll
+    for (uint32_t j = 0; j < DIM / 16; ++j)
+        q[j] = *reinterpret_cast<const attend_bf16x8_t *>(q_at + j * 16);
+
+    // the thread's items of a step: a key's 16 features (keys 32 apart where there are two), a feature's 16 keys
+    const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
+    const uint32_t k_key = threadIdx.x / (DIM / 16), k_part = threadIdx.x % (DIM / 16), v_feature = threadIdx.x / 4, v_part = threadIdx.x % 4;
+    uint32_t k_page[kItems], v_page;
+    const auto find_pages = [&](uint32_t at) {
+        const uint32_t k0 = at * kAttendStep;
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i)
+            k_page[i] = at < last ? page_of(a.s, s, (k0 + k_key + i * 32) >> shift) : kNoPage;
+        v_page = at < last && k0 + v_part * 16 < range.high && k0 + v_part * 16 + 16 > range.low ? page_of(a.s, s, (k0 + v_part * 16) >> shift) : kNoPage;
+    };
+    uint4 k_item[kItems], v_item[kItems];
+    float k_scale[kItems], v_scale;
+    bool v_there;
+    const auto request = [&](uint32_t at) {
+        const uint32_t k0 = at * kAttendStep;
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i) {
+            const uint64_t page = static_cast<uint64_t>(k_page[i] != kNoPage ? k_page[i] : 0) * a.c.heads + head;  // (read, and not used)
+            k_scale[i] = a.c.k_scales[page];
+            k_item[i] = *reinterpret_cast<const uint4 *>(a.c.k + ((page << shift) + ((k0 + k_key + i * 32) & inside)) * DIM + k_part * 16);
+        }
+        v_there = v_page != kNoPage;
+        const uint64_t page = static_cast<uint64_t>(v_there ? v_page : 0) * a.c.heads + head;
+        v_scale = v_there ? a.c.v_scales[page] : 1.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i)
+            v_item[i] = *reinterpret_cast<const uint4 *>(a.c.v + ((page * DIM + v_feature + i * 64) << shift) + ((k0 + v_part * 16) & inside));
+    };
+    const auto put = [&](uint32_t at, AttendStep<DIM> &to) {
+        const uint32_t k0 = at * kAttendStep;
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i) {
+            const uint32_t key = k_key + i * 32, x = key % 32, r = key / 32 * 32 + x / 4 % 4 * 8 + x / 16 * 4 + x % 4;
+            uint8_t *line = to.k + r * DIM * 2;
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2) ^ (r % kPieces)) * 16) = attend_widen(k_item[i].x, k_item[i].y, k_scale[i]);
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2 + 1) ^ (r % kPieces)) * 16) = attend_widen(k_item[i].z, k_item[i].w, k_scale[i]);
+        }
+        const bool edge = k0 < range.low_all || k0 + kAttendStep > range.high_all || __any(!v_there);
+        uint32_t nans = 0;
+        if (edge) {
+            const uint32_t v0 = k0 + v_part * 16;
+            const int32_t from = v_there ? static_cast<int32_t>(range.low - v0) : 16, upto = v_there ? static_cast<int32_t>(range.high - v0) : 0;
+#pragma unroll
+            for (uint32_t i = 0; i < kItems; ++i) {
+                v_item[i].x &= attend_bytes(from, upto, 0), v_item[i].y &= attend_bytes(from, upto, 1);
+                v_item[i].z &= attend_bytes(from, upto, 2), v_item[i].w &= attend_bytes(from, upto, 3);
+                nans |= attend_nan_bytes(v_item[i].x) | attend_nan_bytes(v_item[i].y) | attend_nan_bytes(v_item[i].z) | attend_nan_bytes(v_item[i].w);
+            }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kItems; ++i) {
+            const uint32_t feature = v_feature + i * 64;
+            uint8_t *line = to.v + feature * kAttendStep * 2;
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2) ^ (feature % 8)) * 16) = attend_widen(v_item[i].x, v_item[i].y, v_scale);
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2 + 1) ^ (feature % 8)) * 16) = attend_widen(v_item[i].z, v_item[i].w, v_scale);
+        }
+        const bool any = __any(nans != 0);
+        const uint32_t parts = static_cast<uint32_t>(__ballot(v_there)) & 15u;
+        if (lane == 0) {
+            to.nans[wave] = any;
+            if (wave == 0)
+                to.there = parts;
+        }
+    };
+
+    attend_f32x16_t o[DIM / 32] = {};
+    float top = -__builtin_inff(), total = 0.0f;
+    if (step < last) {
+        find_pages(step);
+        request(step);
+        find_pages(step + 1);
+        put(step, steps[0]);
+    }
+    for (uint32_t turn = 0; step < last; ++step, turn ^= 1) {
+        const AttendStep<DIM> &now = steps[turn];
+        __syncthreads();
+        const bool more = step + 1 < last;
+        if (more) {
+            request(step + 1);
+            find_pages(step + 2);
+        }
+        const uint32_t k0 = step * kAttendStep;
+        if (k0 < of_wave.high && k0 + kAttendStep > of_wave.low) {
+            attend_f32x16_t score[2] = {};
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half)
+#pragma unroll
+                for (uint32_t j = 0; j < DIM / 16; ++j) {
+                    const attend_bf16x8_t keys = *reinterpret_cast<const attend_bf16x8_t *>(now.k + (half * 32 + c) * DIM * 2 + ((j * 2 + h) ^ (c % kPieces)) * 16);
+                    score[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys, q[j], score[half], 0, 0, 0);
+                }
+            const uint32_t there = now.there;
+            const bool edge = k0 < of_wave.low_all || k0 + kAttendStep > of_wave.high_all || there != 15u;
+            if (edge) {
+#pragma unroll
+                for (uint32_t half = 0; half < 2; ++half)
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e) {
+                        const uint32_t key = k0 + half * 32 + h * 16 + e;
+                        if (!(key >= my_low && key < my_high && (there >> (half * 2 + h) & 1u)))
+                            score[half][e] = -__builtin_inff();
+                    }
+            }
+            float most = -__builtin_inff();
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half)
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e)
+                    most = fmaxf(most, score[half][e]);
+            most = attend_max_of_halves(most) * a.scale;
+            if (__any(most > top + kAttendSlack)) {
+                const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+                top = higher;
+                total *= less;
+#pragma unroll
+                for (uint32_t f = 0; f < DIM / 32; ++f)
+                    o[f] *= less;
+            }
+            const float base = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half)
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e) {
+                    score[half][e] = attend_exp2(score[half][e] * a.scale - base);
+                    total += score[half][e];
+                }
+            const bool nans = edge && (now.nans[0] | now.nans[1] | now.nans[2] | now.nans[3]);
+            if (nans) {
+                // NaN among values that some rows see and others do not: the rows that see it have it
+#pragma unroll
+                for (uint32_t f = 0; f < DIM / 32; ++f) {
+                    attend_f32x16_t seen = {};
+#pragma unroll
+                    for (uint32_t u = 0; u < 4; ++u) {
+                        attend_bf16x8_t is = *reinterpret_cast<const attend_bf16x8_t *>(now.v + (f * 32 + c) * kAttendStep * 2 + ((u / 2 * 4 + h * 2 + u % 2) ^ (c % 8)) * 16);
+                        attend_bf16x8_t sees;
+#pragma unroll
+                        for (uint32_t e = 0; e < 8; ++e) {
+                            const uint32_t key = k0 + u / 2 * 32 + h * 16 + u % 2 * 8 + e;
+                            is[e] = is[e] != is[e] ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
+                            sees[e] = key >= my_low && key < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
+                        }
+                        seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (uint32_t e = 0; e < 16; ++e)
+                        o[f][e] = seen[e] > 0.0f ? __builtin_nanf("") : o[f][e];
+                }
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+                const attend_f32x16_t &w = score[u / 2];
+                const uint32_t e = u % 2 * 8;
+                const attend_bf16x8_t p = attend_round(w[e], w[e + 1], w[e + 2], w[e + 3], w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
+#pragma unroll
+                for (uint32_t f = 0; f < DIM / 32; ++f) {
+                    attend_bf16x8_t values = *reinterpret_cast<const attend_bf16x8_t *>(now.v + (f * 32 + c) * kAttendStep * 2 + ((u / 2 * 4 + h * 2 + u % 2) ^ (c % 8)) * 16);
+                    if (nans) {
+#pragma unroll
+                        for (uint32_t i = 0; i < 8; ++i)
+                            values[i] = values[i] != values[i] ? static_cast<__bf16>(0.0f) : values[i];
+                    }
+                    o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values, p, o[f], 0, 0, 0);
+                }
+            }
+        }
+        if (more)
+            put(step + 1, steps[turn ^ 1]);
+    }
+    total += __shfl_xor(total, 32);
+    if (!mine)
+        return;
+    const uint64_t to = attend_row(a, n, head, row);
+    if (a.splits > 1) {
+        const uint64_t place = static_cast<uint64_t>(split) * a.s.rows * a.q_heads + to;
+        if (h == 0)
+            a.stats[place] = make_float2(top, total);
+#pragma unroll
+        for (uint32_t f = 0; f < DIM / 32; ++f)
+#pragma unroll
+            for (uint32_t e = 0; e < 16; e += 4)
+                *reinterpret_cast<float4 *>(a.partial + place * DIM + f * 32 + e * 2 + h * 4) = make_float4(o[f][e], o[f][e + 1], o[f][e + 2], o[f][e + 3]);
+        return;
+    }
+    const float once = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+    for (uint32_t f = 0; f < DIM / 32; ++f)
+#pragma unroll
+        for (uint32_t e = 0; e < 16; e += 4) {
+            typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
+            const attend_f32x4_t v = {o[f][e] * once, o[f][e + 1] * once, o[f][e + 2] * once, o[f][e + 3] * once};
+            *reinterpret_cast<bf16x4_t *>(a.out + to * DIM + f * 32 + e * 2 + h * 4) = __builtin_convertvector(v, bf16x4_t);
+        }
 }
 
 // The splits of a row together; four features to a lane.

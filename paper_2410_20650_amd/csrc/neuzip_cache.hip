@@ -62,6 +62,7 @@ void launch_append(const AppendArgs &a, uint32_t wgs, hipStream_t stream)
 }
 
 struct AttendShape {
+    bool many;  // rows to a workgroup
     uint64_t tiles;
     uint32_t splits;
     uint64_t sums, bytes;  // of scratch memory: the partial sums, and with the rows' statistics
@@ -74,7 +75,8 @@ AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint3
         longest = room;
     const uint32_t group = q_heads / c->heads;
     AttendShape shape;
-    shape.tiles = tile_count({kAttendFewRows, group, 1}, rows, s->count);
+    shape.many = static_cast<uint64_t>(rows) * group > static_cast<uint64_t>(s->count) * kAttendFewRows;
+    shape.tiles = tile_count({shape.many ? kAttendManyRows : kAttendFewRows, group, 1}, rows, s->count);
     const uint64_t wgs = shape.tiles * c->heads;
     uint64_t splits = (kAttendWgs + wgs - 1) / wgs;
     const uint64_t most = (longest + kAttendStep * kAttendLeastSteps - 1) / (kAttendStep * kAttendLeastSteps);
@@ -89,9 +91,12 @@ AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint3
 inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_heads > 0 && q_heads % c->heads == 0; }
 
 template <uint32_t DIM>
-int launch_attend(const AttendArgs &a, uint32_t wgs, hipStream_t stream)
+int launch_attend(const AttendArgs &a, bool many, uint32_t wgs, hipStream_t stream)
 {
-    hipLaunchKernelGGL((attend_few_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    if (many)
+        hipLaunchKernelGGL((attend_many_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((attend_few_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
     if (!hip_ok(hipGetLastError()))
         return NEUZIP_EHIP;
     if (a.splits > 1) {
@@ -197,10 +202,11 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
     a.group = q_heads / cache->heads;
     a.window = window;
     a.splits = shape.splits;
+    a.tiles = static_cast<uint32_t>(shape.tiles);
     a.scale = scale * 1.4426950408889634f;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint32_t grid = static_cast<uint32_t>(wgs);
-    return cache->head_dim == 64 ? launch_attend<64>(a, grid, stream) : launch_attend<128>(a, grid, stream);
+    return cache->head_dim == 64 ? launch_attend<64>(a, shape.many, grid, stream) : launch_attend<128>(a, shape.many, grid, stream);
 }
 
 }  // extern "C"
