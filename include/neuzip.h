@@ -558,7 +558,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
                            uint32_t rows, float scale, uint32_t window, uint64_t longest, void *d_out, void *d_scratch,
                            uint64_t scratch_bytes, void *hip_stream);
 uint64_t neuzip_cache_attention_scratch_bytes(const neuzip_cache *cache, const neuzip_sequences *sequences, uint32_t q_heads, uint32_t rows,
-                                              uint64_t longest);
+                                              uint32_t window, uint64_t longest);
 
 /*
  * neuzip_logits -- what is done to the output projection's result before a token is taken from it, row by row.  With c = how often a token

@@ -123,7 +123,7 @@ def _load():
     lib.neuzip_norm_backward_scratch_bytes.argtypes = [u64, u64]
     lib.neuzip_cache_append.argtypes = [cache, sequences, i32, vp, u64, vp, u64, vp, u64, u32, vp, vp, u64, u32, vp]
     lib.neuzip_cache_attention.argtypes = [cache, sequences, vp, u64, u32, u32, f32, u32, u64, vp, vp, u64, vp]
-    lib.neuzip_cache_attention_scratch_bytes.argtypes = [cache, sequences, u32, u32, u64]
+    lib.neuzip_cache_attention_scratch_bytes.argtypes = [cache, sequences, u32, u32, u32, u64]
     lib.neuzip_logits.argtypes = [vp, u32, u64, vp, u64, vp, vp, vp, vp, vp, vp, u64, vp, vp, u32, vp, vp, vp]
     for name in ("neuzip_embedding", "neuzip_embedding_grad", "neuzip_gated_linear", "neuzip_gated_forward", "neuzip_gated_backward",
                  "neuzip_linear_adapters", "neuzip_norm", "neuzip_norm_backward", "neuzip_cache_append", "neuzip_cache_attention",
@@ -949,8 +949,9 @@ def neuzip_cache_append(cache: KeyValueCache, sequences: Sequences, k: torch.Ten
     return q_out
 
 
-def neuzip_cache_attention_scratch_bytes(cache: KeyValueCache, sequences: Sequences, q_heads: int, rows: int, longest: int = 0) -> int:
-    return int(_lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, longest))
+def neuzip_cache_attention_scratch_bytes(cache: KeyValueCache, sequences: Sequences, q_heads: int, rows: int, window: int = 0,
+                                         longest: int = 0) -> int:
+    return int(_lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, window, longest))
 
 
 def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.Tensor, scale: float = None, window: int = 0,
@@ -970,7 +971,8 @@ def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.
         _here(out, torch.bfloat16, (rows, q_heads, dim), "out", device)
     if scale is None:
         scale = 1.0 / math.sqrt(dim)
-    scratch = _scratch_here(_lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, longest), scratch, q, device, stream)
+    room = _lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, window, longest)
+    scratch = _scratch_here(room, scratch, q, device, stream)
     rc = _lib.neuzip_cache_attention(cache._struct, sequences._struct, q.data_ptr(), q_row, q_heads, rows, scale, window, longest, out.data_ptr(),
                                      _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
     if rc != OK:

@@ -24,6 +24,7 @@ constexpr uint32_t kAttendThreads = 256;
 constexpr uint32_t kAttendFewRows = 16;
 constexpr uint32_t kAttendStep = 64;      // keys
 constexpr uint32_t kAttendLeastSteps = 4; // of a split: one for each wave
+constexpr float kAttendSlack = 6.0f;      // a row's weights may exceed 1 by so much (a factor of 64) before its sums are scaled down to a new maximum
 
 struct AttendArgs {
     SequencesView s;
@@ -36,6 +37,7 @@ struct AttendArgs {
     uint32_t q_heads, group;
     uint32_t window;
     uint32_t splits, tiles;
+    uint32_t most_keys; // that a tile's rows see, as the caller has it
     float scale;        // times log2(e)
 };
 
@@ -68,8 +70,17 @@ __device__ __forceinline__ uint32_t attend_bytes(int32_t begin, int32_t end, int
     return from & upto;
 }
 
+constexpr uint32_t kE4m3One = 0x38u;
 // bit 7 of the bytes that are NaN
 __device__ __forceinline__ uint32_t attend_nan_bytes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+// The bytes outside `keep`, and NaN, made 0; not 0 if there was NaN.
+__device__ __forceinline__ uint32_t attend_clean(uint32_t &w, uint32_t keep)
+{
+    w &= keep;
+    const uint32_t nans = attend_nan_bytes(w);
+    w &= ~((nans >> 7) * 0xFFu);
+    return nans;
+}
 
 // Which keys the rows of a tile see.
 struct AttendRange {
@@ -90,11 +101,31 @@ __device__ __forceinline__ AttendRange attend_range(const NewTokens &n, uint32_t
     return r;
 }
 
-// The steps begin .. end - 1 of split `split` of the steps that the keys of r take.
-__device__ __forceinline__ void attend_split(const AttendRange &r, uint32_t split, uint32_t splits, uint32_t &begin, uint32_t &end)
+// Whether some row does not see all keys of the step from k0 on.
+__device__ __forceinline__ bool attend_edge(const AttendRange &r, uint32_t k0) { return k0 < r.low_all || k0 + kAttendStep > r.high_all; }
+
+// The steps begin .. end - 1 of split `split` of the steps that the keys of r take.  A split has as many steps in every sequence, the longest's
+// divided by the splits: workgroups of a ragged batch are then equally long, short sequences have fewer of them.
+__device__ __forceinline__ void attend_split(const AttendArgs &a, const AttendRange &r, uint32_t split, uint32_t &begin, uint32_t &end)
 {
     const uint32_t first = r.low / kAttendStep, last = (r.high + kAttendStep - 1) / kAttendStep;
-    uint32_t each = (last - first + splits - 1) / splits;
+    if (a.splits == 1) {
+        begin = first;
+        end = last;
+        return;
+    }
+    int32_t longest = 0;
+    for (uint32_t s = threadIdx.x % 64; s < a.s.count; s += 64)
+        longest = max(longest, a.s.lengths[s]);
+#pragma unroll
+    for (int apart = 32; apart; apart >>= 1)
+        longest = max(longest, __shfl_xor(longest, apart));
+    uint32_t keys = static_cast<uint32_t>(longest);
+    keys = keys < a.most_keys ? keys : a.most_keys;
+    // (one step more: a window need not begin with a step.  At least so many that the splits hold all there are.)
+    uint32_t each = ((keys + kAttendStep - 1) / kAttendStep + 1 + a.splits - 1) / a.splits;
+    const uint32_t least = (last - first + a.splits - 1) / a.splits;
+    each = each > least ? each : least;
     each = each > kAttendLeastSteps ? each : kAttendLeastSteps;
     begin = first + split * each;
     begin = begin < last ? begin : last;
@@ -108,11 +139,12 @@ __device__ __forceinline__ uint64_t attend_row(const AttendArgs &a, const NewTok
 }
 
 template <uint32_t DIM>
-__global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const AttendArgs a)
+__global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const AttendArgs a)
 {
     constexpr uint32_t kWide = DIM / 64, kFeatures = DIM / 16, kWaves = kAttendThreads / 64, kStride = DIM + 4;
     __shared__ float sums[kWaves][kAttendFewRows][kStride];
     __shared__ float2 stats[kWaves][kAttendFewRows];
+    __shared__ attend_bf16x8_t queries[kWide * 2][64];
     const uint32_t split = blockIdx.x % a.splits, head = blockIdx.x / a.splits % a.c.heads, tile = blockIdx.x / a.splits / a.c.heads;
     const TileNumbers numbers = {kAttendFewRows, a.group, 1};
     const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
@@ -131,52 +163,75 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
     const bool mine = row0 + i < row_end;
     const uint32_t row = mine ? row0 + i : row0, position = n.first + row / a.group;
     const uint32_t my_high = mine ? position + 1 : 0, my_low = a.window && position + 1 > a.window ? position + 1 - a.window : 0;
-    attend_bf16x8_t q[kWide][2];
-    const uint16_t *q_at = a.q + (n.begin + row / a.group) * a.q_row + (head * a.group + row % a.group) * DIM + g * 16;
-#pragma unroll
-    for (uint32_t j = 0; j < kWide; ++j)
-#pragma unroll
-        for (uint32_t h = 0; h < 2; ++h)
-            q[j][h] = *reinterpret_cast<const attend_bf16x8_t *>(q_at + j * 64 + h * 8);
+    // (the query is read from LDS in every step: its 4 KB would be 16 registers of every wave, which three waves of a SIMD do not have)
+    if (wave < kWide * 2) {
+        const uint16_t *q_at = a.q + (n.begin + row / a.group) * a.q_row + (head * a.group + row % a.group) * DIM + g * 16;
+        queries[wave][lane] = *reinterpret_cast<const attend_bf16x8_t *>(q_at + wave / 2 * 64 + wave % 2 * 8);
+    }
+    __syncthreads();
 
     attend_f32x4_t o[kFeatures] = {};
     float top = -__builtin_inff(), total = 0.0f;
     uint32_t step, last;
-    attend_split(range, split, a.splits, step, last);
+    attend_split(a, range, split, step, last);
+    // Requests run ahead of the sums: the next step's pages are looked up a step before, its keys are asked for as soon as this step's are
+    // used up, its values behind this step's second product.
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
-    for (step += wave; step < last; step += kWaves) {
-        const uint32_t k0 = step * kAttendStep;
-        const uint32_t k_group = k0 + i / 4 * 16, v_group = k0 + g * 16;
-        const bool k_there = k_group < range.high && k_group + 16 > range.low, v_there = v_group < range.high && v_group + 16 > range.low;
-        uint32_t k_page = k_there ? page_of(a.s, s, k_group >> shift) : kNoPage, v_page = v_there ? page_of(a.s, s, v_group >> shift) : kNoPage;
-        const bool held = v_page != kNoPage;
-        k_page = k_page != kNoPage ? k_page : 0;  // (read, and not used)
-        v_page = held ? v_page : 0;
-        const uint64_t k_head = static_cast<uint64_t>(k_page) * a.c.heads + head, v_head = static_cast<uint64_t>(v_page) * a.c.heads + head;
-        const uint8_t *k_at = a.c.k + ((k_head << shift) + (k_group & inside) + i % 4) * DIM + g * 16;
-        const uint8_t *v_at = a.c.v + ((v_head * DIM + i) << shift) + (v_group & inside);
-        const float k_scale = a.c.k_scales[k_head], v_scale = held ? a.c.v_scales[v_head] : 1.0f;
-        uint4 k[4][kWide], v[kFeatures];
+    uint32_t k_page, v_page;
+    const auto find_pages = [&](uint32_t at) {
+        const uint32_t k_group = at * kAttendStep + i / 4 * 16, v_group = at * kAttendStep + g * 16;
+        k_page = at < last && k_group < range.high && k_group + 16 > range.low ? page_of(a.s, s, k_group >> shift) : kNoPage;
+        v_page = at < last && v_group < range.high && v_group + 16 > range.low ? page_of(a.s, s, v_group >> shift) : kNoPage;
+    };
+    uint4 k[4][kWide], v[kFeatures];
+    float k_scale, v_scale;
+    bool held;
+    uint32_t found = 0;  // NaN among values that not all rows see
+    const auto request_keys = [&](uint32_t at) {
+        const uint64_t page = static_cast<uint64_t>(k_page != kNoPage ? k_page : 0) * a.c.heads + head;  // (read, and not used)
+        const uint8_t *from = a.c.k + ((page << shift) + ((at * kAttendStep + i / 4 * 16) & inside) + i % 4) * DIM + g * 16;
+        k_scale = a.c.k_scales[page];
 #pragma unroll
         for (uint32_t t = 0; t < 4; ++t)
 #pragma unroll
             for (uint32_t j = 0; j < kWide; ++j)
-                k[t][j] = *reinterpret_cast<const uint4 *>(k_at + t * 4 * DIM + j * 64);
+                k[t][j] = *reinterpret_cast<const uint4 *>(from + t * 4 * DIM + j * 64);
+    };
+    const auto request_values = [&](uint32_t at) {
+        held = v_page != kNoPage;
+        const uint64_t page = static_cast<uint64_t>(held ? v_page : 0) * a.c.heads + head;
+        const uint8_t *from = a.c.v + ((page * DIM + i) << shift) + ((at * kAttendStep + g * 16) & inside);
+        v_scale = a.c.v_scales[page];
+        v_scale = held ? v_scale : 1.0f;
 #pragma unroll
         for (uint32_t f = 0; f < kFeatures; ++f)
-            v[f] = *reinterpret_cast<const uint4 *>(v_at + (static_cast<uint64_t>(f) * 16 << shift));
+            v[f] = *reinterpret_cast<const uint4 *>(from + (f * 16 << shift));
+    };
+    step += wave;
+    const uint32_t begin = step;
+    if (step < last) {
+        find_pages(step);
+        request_keys(step);
+        request_values(step);
+        find_pages(step + kWaves);
+    }
+    for (; step < last; step += kWaves) {
+        const uint32_t k0 = step * kAttendStep, v_group = k0 + g * 16;
+        asm volatile("" ::: "memory");  // (it stays in LDS)
         attend_f32x4_t score[4] = {};
 #pragma unroll
-        for (uint32_t t = 0; t < 4; ++t)
+        for (uint32_t j = 0; j < kWide; ++j) {
+            const attend_bf16x8_t first = queries[j * 2][lane], second = queries[j * 2 + 1][lane];
 #pragma unroll
-            for (uint32_t j = 0; j < kWide; ++j) {
-                score[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(k[t][j].x, k[t][j].y, k_scale), q[j][0], score[t], 0, 0, 0);
-                score[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(k[t][j].z, k[t][j].w, k_scale), q[j][1], score[t], 0, 0, 0);
+            for (uint32_t t = 0; t < 4; ++t) {
+                score[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(k[t][j].x, k[t][j].y, k_scale), first, score[t], 0, 0, 0);
+                score[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(k[t][j].z, k[t][j].w, k_scale), second, score[t], 0, 0, 0);
             }
-        // at an edge: what a row does not see, and values that no row sees (whatever is there may be NaN, and 0 * NaN is)
-        const bool edge = k0 < range.low_all || k0 + kAttendStep > range.high_all || __any(!held);
-        uint32_t nans = 0;
-        if (edge) {
+        }
+        // at an edge: what a row does not see; values that no row sees, and NaN (0 * NaN is), are made 0, and who sees NaN is looked up in the end
+        if (step + kWaves < last)
+            request_keys(step + kWaves);
+        if (attend_edge(range, k0) || __any(!held)) {
 #pragma unroll
             for (uint32_t t = 0; t < 4; ++t)
 #pragma unroll
@@ -188,10 +243,8 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
             const int32_t from = held ? static_cast<int32_t>(range.low - v_group) : 16, upto = held ? static_cast<int32_t>(range.high - v_group) : 0;
             const uint32_t m0 = attend_bytes(from, upto, 0), m1 = attend_bytes(from, upto, 1), m2 = attend_bytes(from, upto, 2), m3 = attend_bytes(from, upto, 3);
 #pragma unroll
-            for (uint32_t f = 0; f < kFeatures; ++f) {
-                v[f].x &= m0, v[f].y &= m1, v[f].z &= m2, v[f].w &= m3;
-                nans |= attend_nan_bytes(v[f].x) | attend_nan_bytes(v[f].y) | attend_nan_bytes(v[f].z) | attend_nan_bytes(v[f].w);
-            }
+            for (uint32_t f = 0; f < kFeatures; ++f)
+                found |= attend_clean(v[f].x, m0) | attend_clean(v[f].y, m1) | attend_clean(v[f].z, m2) | attend_clean(v[f].w, m3);
         }
         float most = -__builtin_inff();
 #pragma unroll
@@ -201,10 +254,16 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
                 most = fmaxf(most, score[t][r]);
         most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
-        const float now = fmaxf(top, most * a.scale), base = now == -__builtin_inff() ? 0.0f : now;
-        const float less = attend_exp2(top - base);
-        top = now;
-        total *= less;
+        most *= a.scale;
+        if (__any(most > top + kAttendSlack)) {
+            const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+            top = higher;
+            total *= less;
+#pragma unroll
+            for (uint32_t f = 0; f < kFeatures; ++f)
+                o[f] *= less;
+        }
+        const float base = top == -__builtin_inff() ? 0.0f : top;
 #pragma unroll
         for (uint32_t t = 0; t < 4; ++t)
 #pragma unroll
@@ -212,38 +271,6 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
                 score[t][r] = attend_exp2(score[t][r] * a.scale - base);
                 total += score[t][r];
             }
-#pragma unroll
-        for (uint32_t f = 0; f < kFeatures; ++f)
-            o[f] *= less;
-        if (__any(nans != 0)) {
-            // NaN among values that some rows see and others do not: the rows that see it have it
-#pragma unroll
-            for (uint32_t f = 0; f < kFeatures; ++f) {
-                attend_f32x4_t seen = {};
-                uint32_t w[4] = {v[f].x, v[f].y, v[f].z, v[f].w};
-#pragma unroll
-                for (uint32_t u = 0; u < 2; ++u) {
-                    uint32_t is[2];
-                    attend_bf16x8_t sees;
-#pragma unroll
-                    for (uint32_t b = 0; b < 2; ++b) {
-                        const uint32_t bits = attend_nan_bytes(w[2 * u + b]);
-                        is[b] = (bits >> 7) * 0x38u;  // 1.0
-                        w[2 * u + b] &= ~((bits >> 7) * 0xFFu);
-                    }
-#pragma unroll
-                    for (uint32_t e = 0; e < 8; ++e) {
-                        const uint32_t key = v_group + u * 8 + e;
-                        sees[e] = key >= my_low && key < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
-                    }
-                    seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(is[0], is[1], 1.0f), sees, seen, 0, 0, 0);
-                }
-                v[f] = make_uint4(w[0], w[1], w[2], w[3]);
-#pragma unroll
-                for (uint32_t r = 0; r < 4; ++r)
-                    o[f][r] = seen[r] > 0.0f ? __builtin_nanf("") : o[f][r];
-            }
-        }
         const attend_bf16x8_t p0 = attend_round(score[0][0], score[0][1], score[0][2], score[0][3], score[1][0], score[1][1], score[1][2], score[1][3]);
         const attend_bf16x8_t p1 = attend_round(score[2][0], score[2][1], score[2][2], score[2][3], score[3][0], score[3][1], score[3][2], score[3][3]);
 #pragma unroll
@@ -251,9 +278,36 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
             o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].x, v[f].y, v_scale), p0, o[f], 0, 0, 0);
             o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].z, v[f].w, v_scale), p1, o[f], 0, 0, 0);
         }
+        if (step + kWaves < last) {
+            request_values(step + kWaves);
+            find_pages(step + 2 * kWaves);
+        }
     }
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
+    if (__any(found != 0)) {
+        // a row that sees a value that is NaN has it: products of where NaN is with who sees it
+#pragma unroll
+        for (uint32_t f = 0; f < kFeatures; ++f) {
+            attend_f32x4_t seen = {};
+            for (step = begin; step < last; step += kWaves)
+#pragma unroll 1
+                for (uint32_t u = 0; u < 2; ++u) {
+                    const uint32_t key = step * kAttendStep + g * 16 + u * 8, page = page_of(a.s, s, key >> shift);
+                    const uint64_t from = ((static_cast<uint64_t>(page != kNoPage ? page : 0) * a.c.heads + head) * DIM + f * 16 + i) << shift;
+                    const uint2 bytes = *reinterpret_cast<const uint2 *>(a.c.v + from + (key & inside));
+                    attend_bf16x8_t sees;
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e)
+                        sees[e] = page != kNoPage && key + e >= my_low && key + e < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
+                    const attend_bf16x8_t is = attend_widen((attend_nan_bytes(bytes.x) >> 7) * kE4m3One, (attend_nan_bytes(bytes.y) >> 7) * kE4m3One, 1.0f);
+                    seen = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is, sees, seen, 0, 0, 0);
+                }
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r)
+                o[f][r] = seen[r] > 0.0f ? __builtin_nanf("") : o[f][r];
+        }
+    }
     if (g == 0)
         stats[wave][i] = make_float2(top, total);
 #pragma unroll
@@ -302,7 +356,6 @@ __global__ void __launch_bounds__(kAttendThreads) attend_few_kernel(const Attend
 // In LDS: row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4, its pieces of 16 bytes (8 features) in places p ^ c % kPieces;
 // the values' row is a feature, 64 keys in 8 pieces, in places p ^ feature % 8: what 8 lanes read together lies in different banks.
 constexpr uint32_t kAttendManyRows = 128;
-constexpr float kAttendSlack = 6.0f;  // by so much (a factor of 64) a row's weights may exceed 1 before its sums are scaled down to a new maximum
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float attend_f32x16_t;
 
@@ -318,7 +371,6 @@ template <uint32_t DIM>
 struct alignas(16) AttendStep {  // of 64 keys in LDS
     uint8_t k[kAttendStep * DIM * 2];
     uint8_t v[DIM * kAttendStep * 2];
-    uint32_t nans[4];   // by the waves that filled it: NaN among the values
     uint32_t there;     // bit i: keys 16 i .. 16 i + 15 have a page and are seen by some row
 };
 
@@ -341,7 +393,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 32, h = lane / 32;
     const AttendRange range = attend_range(n, row0 / a.group, (row_end - 1) / a.group, a.window);
     uint32_t step, last;
-    attend_split(range, split, a.splits, step, last);
+    attend_split(a, range, split, step, last);
 
     // the wave's rows, and the lane's
     const uint32_t wave0 = row0 + wave * 32 < row_end ? row0 + wave * 32 : row_end - 1, wave_end = wave0 + 32 < row_end ? wave0 + 32 : row_end;
@@ -384,6 +436,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         for (uint32_t i = 0; i < kItems; ++i)
             v_item[i] = *reinterpret_cast<const uint4 *>(a.c.v + ((page * DIM + v_feature + i * 64) << shift) + ((k0 + v_part * 16) & inside));
     };
+    uint32_t found = 0;  // NaN among values that not all rows see
     const auto put = [&](uint32_t at, AttendStep<DIM> &to) {
         const uint32_t k0 = at * kAttendStep;
 #pragma unroll
@@ -393,16 +446,14 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
             *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2) ^ (r % kPieces)) * 16) = attend_widen(k_item[i].x, k_item[i].y, k_scale[i]);
             *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2 + 1) ^ (r % kPieces)) * 16) = attend_widen(k_item[i].z, k_item[i].w, k_scale[i]);
         }
-        const bool edge = k0 < range.low_all || k0 + kAttendStep > range.high_all || __any(!v_there);
-        uint32_t nans = 0;
-        if (edge) {
+        if (attend_edge(range, k0) || __any(!v_there)) {
+            // values that not all rows see: those that none does, and NaN (0 * NaN is), are made 0; who sees NaN is looked up in the end
             const uint32_t v0 = k0 + v_part * 16;
             const int32_t from = v_there ? static_cast<int32_t>(range.low - v0) : 16, upto = v_there ? static_cast<int32_t>(range.high - v0) : 0;
 #pragma unroll
             for (uint32_t i = 0; i < kItems; ++i) {
-                v_item[i].x &= attend_bytes(from, upto, 0), v_item[i].y &= attend_bytes(from, upto, 1);
-                v_item[i].z &= attend_bytes(from, upto, 2), v_item[i].w &= attend_bytes(from, upto, 3);
-                nans |= attend_nan_bytes(v_item[i].x) | attend_nan_bytes(v_item[i].y) | attend_nan_bytes(v_item[i].z) | attend_nan_bytes(v_item[i].w);
+                found |= attend_clean(v_item[i].x, attend_bytes(from, upto, 0)) | attend_clean(v_item[i].y, attend_bytes(from, upto, 1));
+                found |= attend_clean(v_item[i].z, attend_bytes(from, upto, 2)) | attend_clean(v_item[i].w, attend_bytes(from, upto, 3));
             }
         }
 #pragma unroll
@@ -412,13 +463,9 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
             *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2) ^ (feature % 8)) * 16) = attend_widen(v_item[i].x, v_item[i].y, v_scale);
             *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2 + 1) ^ (feature % 8)) * 16) = attend_widen(v_item[i].z, v_item[i].w, v_scale);
         }
-        const bool any = __any(nans != 0);
         const uint32_t parts = static_cast<uint32_t>(__ballot(v_there)) & 15u;
-        if (lane == 0) {
-            to.nans[wave] = any;
-            if (wave == 0)
-                to.there = parts;
-        }
+        if (threadIdx.x == 0)
+            to.there = parts;
     };
 
     attend_f32x16_t o[DIM / 32] = {};
@@ -429,6 +476,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         find_pages(step + 1);
         put(step, steps[0]);
     }
+    const uint32_t begin = step;
     for (uint32_t turn = 0; step < last; ++step, turn ^= 1) {
         const AttendStep<DIM> &now = steps[turn];
         __syncthreads();
@@ -447,9 +495,9 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
                     const attend_bf16x8_t keys = *reinterpret_cast<const attend_bf16x8_t *>(now.k + (half * 32 + c) * DIM * 2 + ((j * 2 + h) ^ (c % kPieces)) * 16);
                     score[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys, q[j], score[half], 0, 0, 0);
                 }
-            const uint32_t there = now.there;
-            const bool edge = k0 < of_wave.low_all || k0 + kAttendStep > of_wave.high_all || there != 15u;
-            if (edge) {
+            const uint32_t there = __builtin_amdgcn_readfirstlane(now.there);
+            if (attend_edge(of_wave, k0) || there != 15u) {
+                asm volatile("");  // (a branch around it, not 130 instructions of every step)
 #pragma unroll
                 for (uint32_t half = 0; half < 2; ++half)
 #pragma unroll
@@ -482,50 +530,51 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
                     score[half][e] = attend_exp2(score[half][e] * a.scale - base);
                     total += score[half][e];
                 }
-            const bool nans = edge && (now.nans[0] | now.nans[1] | now.nans[2] | now.nans[3]);
-            if (nans) {
-                // NaN among values that some rows see and others do not: the rows that see it have it
-#pragma unroll
-                for (uint32_t f = 0; f < DIM / 32; ++f) {
-                    attend_f32x16_t seen = {};
-#pragma unroll
-                    for (uint32_t u = 0; u < 4; ++u) {
-                        attend_bf16x8_t is = *reinterpret_cast<const attend_bf16x8_t *>(now.v + (f * 32 + c) * kAttendStep * 2 + ((u / 2 * 4 + h * 2 + u % 2) ^ (c % 8)) * 16);
-                        attend_bf16x8_t sees;
-#pragma unroll
-                        for (uint32_t e = 0; e < 8; ++e) {
-                            const uint32_t key = k0 + u / 2 * 32 + h * 16 + u % 2 * 8 + e;
-                            is[e] = is[e] != is[e] ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
-                            sees[e] = key >= my_low && key < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
-                        }
-                        seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e)
-                        o[f][e] = seen[e] > 0.0f ? __builtin_nanf("") : o[f][e];
-                }
-            }
+            attend_bf16x8_t p[4];
 #pragma unroll
             for (uint32_t u = 0; u < 4; ++u) {
                 const attend_f32x16_t &w = score[u / 2];
                 const uint32_t e = u % 2 * 8;
-                const attend_bf16x8_t p = attend_round(w[e], w[e + 1], w[e + 2], w[e + 3], w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
-#pragma unroll
-                for (uint32_t f = 0; f < DIM / 32; ++f) {
-                    attend_bf16x8_t values = *reinterpret_cast<const attend_bf16x8_t *>(now.v + (f * 32 + c) * kAttendStep * 2 + ((u / 2 * 4 + h * 2 + u % 2) ^ (c % 8)) * 16);
-                    if (nans) {
-#pragma unroll
-                        for (uint32_t i = 0; i < 8; ++i)
-                            values[i] = values[i] != values[i] ? static_cast<__bf16>(0.0f) : values[i];
-                    }
-                    o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values, p, o[f], 0, 0, 0);
-                }
+                p[u] = attend_round(w[e], w[e + 1], w[e + 2], w[e + 3], w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
             }
+            const auto values_of = [&](uint32_t f, uint32_t u) {
+                return *reinterpret_cast<const attend_bf16x8_t *>(now.v + (f * 32 + c) * kAttendStep * 2 + ((u / 2 * 4 + h * 2 + u % 2) ^ (c % 8)) * 16);
+            };
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+                for (uint32_t f = 0; f < DIM / 32; ++f)
+                    o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values_of(f, u), p[u], o[f], 0, 0, 0);
         }
         if (more)
             put(step + 1, steps[turn ^ 1]);
     }
     total += __shfl_xor(total, 32);
+    if (__syncthreads_or(found != 0)) {
+        // a row that sees a value that is NaN has it: products of where NaN is with who sees it
+#pragma unroll
+        for (uint32_t f = 0; f < DIM / 32; ++f) {
+            attend_f32x16_t seen = {};
+            for (step = begin; step < last; ++step) {
+                const uint32_t k0 = step * kAttendStep;
+#pragma unroll 1
+                for (uint32_t u = 0; u < 4; ++u) {
+                    const uint32_t key = k0 + u / 2 * 32 + h * 16 + u % 2 * 8, page = page_of(a.s, s, key >> shift);
+                    const uint64_t at = ((static_cast<uint64_t>(page != kNoPage ? page : 0) * a.c.heads + head) * DIM + f * 32 + c) << shift;
+                    const uint2 bytes = *reinterpret_cast<const uint2 *>(a.c.v + at + (key & inside));
+                    attend_bf16x8_t sees;
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e)
+                        sees[e] = page != kNoPage && key + e >= my_low && key + e < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
+                    const attend_bf16x8_t is = attend_widen((attend_nan_bytes(bytes.x) >> 7) * kE4m3One, (attend_nan_bytes(bytes.y) >> 7) * kE4m3One, 1.0f);
+                    seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e)
+                o[f][e] = seen[e] > 0.0f ? __builtin_nanf("") : o[f][e];
+        }
+    }
     if (!mine)
         return;
     const uint64_t to = attend_row(a, n, head, row);
@@ -551,29 +600,58 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         }
 }
 
-// The splits of a row together; four features to a lane.
-template <uint32_t DIM>
+// The splits of a row together; four features to a lane, and GROUPS of lanes with every GROUPS-th split each.
+template <uint32_t DIM, uint32_t GROUPS>
 __global__ void __launch_bounds__(kAttendThreads) attend_join_kernel(const AttendArgs a)
 {
-    constexpr uint32_t kLanes = DIM / 4, kRows = kAttendThreads / kLanes;
+    constexpr uint32_t kLanes = DIM / 4, kRows = kAttendThreads / kLanes / GROUPS;
     const uint64_t count = static_cast<uint64_t>(a.s.rows) * a.q_heads;
-    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * kRows + threadIdx.x / kLanes;
+    const uint32_t group = threadIdx.x / kLanes % GROUPS, in_rows = threadIdx.x / (kLanes * GROUPS);
+    const uint64_t row = static_cast<uint64_t>(blockIdx.x) * kRows + in_rows;
     const uint32_t at = threadIdx.x % kLanes * 4;
     const int64_t token = static_cast<int64_t>(row / a.q_heads);
-    if (row >= count || token < a.s.starts[0] || token >= a.s.starts[a.s.count])
-        return;  // (a row of nobody's)
-    float all = -__builtin_inff();
-    for (uint32_t p = 0; p < a.splits; ++p)
-        all = fmaxf(all, a.stats[p * count + row].x);
-    const float base = all == -__builtin_inff() ? 0.0f : all;
-    float whole = 0.0f;
+    const bool here = row < count && token >= a.s.starts[0] && token < a.s.starts[a.s.count];  // (others are nobody's)
+    float all = -__builtin_inff(), whole = 0.0f;
     attend_f32x4_t sum = {};
-    for (uint32_t p = 0; p < a.splits; ++p) {
-        const float2 part = a.stats[p * count + row];
-        const float share = attend_exp2(part.x - base);
-        whole += share * part.y;
-        sum += share * *reinterpret_cast<const attend_f32x4_t *>(a.partial + (p * count + row) * DIM + at);
+    if (here) {
+        const float2 *stats = a.stats + row;
+        const float *partial = a.partial + row * DIM + at;
+#pragma unroll 4
+        for (uint32_t p = group; p < a.splits; p += GROUPS)
+            all = fmaxf(all, stats[p * count].x);
+        const float base = all == -__builtin_inff() ? 0.0f : all;
+#pragma unroll 4
+        for (uint32_t p = group; p < a.splits; p += GROUPS) {
+            const float2 part = stats[p * count];
+            const float share = attend_exp2(part.x - base);
+            whole += share * part.y;
+            sum += share * *reinterpret_cast<const attend_f32x4_t *>(partial + p * count * DIM);
+        }
     }
+    if constexpr (GROUPS > 1) {
+        __shared__ attend_f32x4_t sums[GROUPS][kRows * kLanes];
+        __shared__ float2 parts[GROUPS][kRows * kLanes];
+        const uint32_t place = in_rows * kLanes + threadIdx.x % kLanes;
+        sums[group][place] = sum;
+        parts[group][place] = make_float2(all, whole);
+        __syncthreads();
+        if (group)
+            return;
+#pragma unroll
+        for (uint32_t other = 1; other < GROUPS; ++other)
+            all = fmaxf(all, parts[other][place].x);
+        const float base = all == -__builtin_inff() ? 0.0f : all;
+        sum = {};
+        whole = 0.0f;
+#pragma unroll
+        for (uint32_t other = 0; other < GROUPS; ++other) {
+            const float share = attend_exp2(parts[other][place].x - base);
+            whole += share * parts[other][place].y;
+            sum += share * sums[other][place];
+        }
+    }
+    if (!here)
+        return;
     typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
     sum *= whole == 0.0f ? 0.0f : 1.0f / whole;
     *reinterpret_cast<bf16x4_t *>(a.out + row * DIM + at) = __builtin_convertvector(sum, bf16x4_t);

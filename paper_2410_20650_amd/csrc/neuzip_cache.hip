@@ -16,7 +16,8 @@ using namespace nz;
 namespace {
 
 constexpr uint64_t kAttendMostRows = 1ull << 27;  // rows times query heads
-constexpr uint32_t kAttendWgs = 1024;             // that a launch is split into at least, where its keys allow it
+constexpr uint32_t kAttendWgs = 512;              // that a launch is split into at least, where its keys allow it: two on a CU
+constexpr uint64_t kAttendUneven = 2;
 constexpr uint32_t kAttendMostSplits = 128;
 
 inline bool off(const void *p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) & (size - 1); }
@@ -64,11 +65,11 @@ void launch_append(const AppendArgs &a, uint32_t wgs, hipStream_t stream)
 struct AttendShape {
     bool many;  // rows to a workgroup
     uint64_t tiles;
-    uint32_t splits;
+    uint32_t splits, keys;
     uint64_t sums, bytes;  // of scratch memory: the partial sums, and with the rows' statistics
 };
 
-AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint32_t q_heads, uint32_t rows, uint64_t longest)
+AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint32_t q_heads, uint32_t rows, uint32_t window, uint64_t longest)
 {
     const uint64_t room = static_cast<uint64_t>(s->table_width) << page_shift(c);
     if (longest == 0 || longest > room)
@@ -76,12 +77,19 @@ AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint3
     const uint32_t group = q_heads / c->heads;
     AttendShape shape;
     shape.many = static_cast<uint64_t>(rows) * group > static_cast<uint64_t>(s->count) * kAttendFewRows;
-    shape.tiles = tile_count({shape.many ? kAttendManyRows : kAttendFewRows, group, 1}, rows, s->count);
+    const uint32_t tile = shape.many ? kAttendManyRows : kAttendFewRows;
+    shape.tiles = tile_count({tile, group, 1}, rows, s->count);
+    // the keys that a tile's rows see, at most
+    const uint64_t span = static_cast<uint64_t>(window) + tile / group + 1;
+    const uint64_t keys = window && span < longest ? span : longest;
     const uint64_t wgs = shape.tiles * c->heads;
-    uint64_t splits = (kAttendWgs + wgs - 1) / wgs;
-    const uint64_t most = (longest + kAttendStep * kAttendLeastSteps - 1) / (kAttendStep * kAttendLeastSteps);
-    splits = splits < most ? splits : most;
-    shape.splits = static_cast<uint32_t>(splits < kAttendMostSplits ? splits : kAttendMostSplits);
+    // (several sequences are seldom equally long: more splits, so that no CU waits long for another)
+    const uint64_t uneven = s->count < kAttendUneven ? s->count : kAttendUneven;
+    const uint64_t wanted = (uneven * kAttendWgs + wgs - 1) / wgs, most = keys / (kAttendStep * kAttendLeastSteps);
+    uint64_t splits = wanted < most ? wanted : most;
+    splits = splits < kAttendMostSplits ? splits : kAttendMostSplits;
+    shape.splits = splits ? static_cast<uint32_t>(splits) : 1;
+    shape.keys = static_cast<uint32_t>(keys);
     const uint64_t parts = shape.splits > 1 ? static_cast<uint64_t>(shape.splits) * rows * q_heads : 0;
     shape.sums = pad_to(parts * c->head_dim * sizeof(float), 256);
     shape.bytes = shape.sums + parts * sizeof(float2);
@@ -100,8 +108,12 @@ int launch_attend(const AttendArgs &a, bool many, uint32_t wgs, hipStream_t stre
     if (!hip_ok(hipGetLastError()))
         return NEUZIP_EHIP;
     if (a.splits > 1) {
-        const uint64_t count = static_cast<uint64_t>(a.s.rows) * a.q_heads, each = kAttendThreads / (DIM / 4);
-        hipLaunchKernelGGL((attend_join_kernel<DIM>), dim3(static_cast<uint32_t>((count + each - 1) / each)), dim3(kAttendThreads), 0, stream, a);
+        constexpr uint32_t kAll = kAttendThreads / (DIM / 4);  // rows of a workgroup, or groups of a row
+        const uint64_t count = static_cast<uint64_t>(a.s.rows) * a.q_heads;
+        if (a.splits <= kAll)
+            hipLaunchKernelGGL((attend_join_kernel<DIM, 1>), dim3(static_cast<uint32_t>((count + kAll - 1) / kAll)), dim3(kAttendThreads), 0, stream, a);
+        else
+            hipLaunchKernelGGL((attend_join_kernel<DIM, kAll>), dim3(static_cast<uint32_t>(count)), dim3(kAttendThreads), 0, stream, a);
         if (!hip_ok(hipGetLastError()))
             return NEUZIP_EHIP;
     }
@@ -164,12 +176,12 @@ int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *seque
 }
 
 uint64_t neuzip_cache_attention_scratch_bytes(const neuzip_cache *cache, const neuzip_sequences *sequences, uint32_t q_heads, uint32_t rows,
-                                              uint64_t longest)
+                                              uint32_t window, uint64_t longest)
 {
     if (!valid_cache(cache) || !valid_sequences(cache, sequences) || !valid_heads(cache, q_heads) || rows == 0 || sequences->count == 0 ||
         static_cast<uint64_t>(rows) * q_heads >= kAttendMostRows)
         return 0;
-    return attend_shape(cache, sequences, q_heads, rows, longest).bytes;
+    return attend_shape(cache, sequences, q_heads, rows, window, longest).bytes;
 }
 
 int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *sequences, const void *d_q, uint64_t q_row, uint32_t q_heads,
@@ -184,7 +196,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
         return NEUZIP_EINVAL;
     if (static_cast<uint64_t>(rows) * q_heads >= kAttendMostRows)
         return NEUZIP_EUNSUPPORTED;
-    const AttendShape shape = attend_shape(cache, sequences, q_heads, rows, longest);
+    const AttendShape shape = attend_shape(cache, sequences, q_heads, rows, window, longest);
     if (shape.bytes && (!d_scratch || scratch_bytes < shape.bytes))
         return NEUZIP_EINVAL;
     const uint64_t wgs = shape.tiles * cache->heads * shape.splits;
@@ -203,6 +215,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
     a.window = window;
     a.splits = shape.splits;
     a.tiles = static_cast<uint32_t>(shape.tiles);
+    a.most_keys = shape.keys;
     a.scale = scale * 1.4426950408889634f;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint32_t grid = static_cast<uint32_t>(wgs);

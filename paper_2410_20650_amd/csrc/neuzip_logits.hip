@@ -14,14 +14,20 @@ using namespace nz;
 namespace {
 
 constexpr uint32_t kLogitsMostRows = 65535;  // a grid's second dimension
+// From so many logits on there are enough long slices for all CUs; a long one reads the row's history once for four times as many tokens.
+constexpr uint64_t kLogitsMany = 512 * 4096;
 constexpr uint64_t kLogitsMostEntries = 0xFFFFFFFEull;
 
 inline bool off(const void *p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) & (size - 1); }
 
-template <int SLICE>
-void launch_logits(const LogitsArgs &a, uint32_t rows, hipStream_t stream)
+template <uint32_t SLICE, uint32_t THREADS>
+void launch_logits(const LogitsArgs &a, uint32_t rows, bool wide, hipStream_t stream)
 {
-    hipLaunchKernelGGL((logits_kernel<SLICE>), dim3((a.vocab + SLICE - 1) / SLICE, rows), dim3(kLogitsThreads), 0, stream, a);
+    const dim3 wgs((a.vocab + SLICE - 1) / SLICE, rows);
+    if (wide)
+        hipLaunchKernelGGL((logits_kernel<SLICE, THREADS, true>), wgs, dim3(THREADS), 0, stream, a);
+    else
+        hipLaunchKernelGGL((logits_kernel<SLICE, THREADS, false>), wgs, dim3(THREADS), 0, stream, a);
 }
 
 }  // namespace
@@ -70,7 +76,12 @@ int neuzip_logits(const float *d_logits, uint32_t rows, uint64_t vocab, const in
     a.mask_words = (vocab + 31) / 32;
     a.mask_count = masks;
     a.vocab = static_cast<uint32_t>(vocab);
-    launch_logits<1024>(a, rows, static_cast<hipStream_t>(hip_stream));
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const bool wide = vocab % 4 == 0 && !off(d_logits, 16) && !off(d_out, 16);
+    if (static_cast<uint64_t>(rows) * vocab >= kLogitsMany)
+        launch_logits<4096, 512>(a, rows, wide, stream);
+    else
+        launch_logits<1024, 256>(a, rows, wide, stream);
     return hip_ok(hipGetLastError()) ? NEUZIP_OK : NEUZIP_EHIP;
 }
 

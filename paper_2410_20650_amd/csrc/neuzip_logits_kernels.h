@@ -11,8 +11,6 @@
 
 namespace nz {
 
-constexpr uint32_t kLogitsThreads = 256;
-
 struct LogitsArgs {
     const float *logits;
     float *out;
@@ -44,33 +42,69 @@ __device__ __forceinline__ LogitsRange logits_range(const int32_t *starts, uint3
     return r;
 }
 
-template <int SLICE>
-__global__ void __launch_bounds__(kLogitsThreads) logits_kernel(const LogitsArgs a)
+// f(i) for i = threadIdx.x, + THREADS, ... below count, the loads of four of them on their way together
+template <uint32_t THREADS, class F>
+__device__ __forceinline__ void logits_each(const int64_t *tokens, uint64_t begin, uint64_t end, const F &f)
+{
+    for (uint64_t at = begin + threadIdx.x; at < end; at += 4 * THREADS) {
+        int64_t token[4];
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            token[j] = at + j * THREADS < end ? tokens[at + j * THREADS] : -1;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            f(at + j * THREADS, token[j]);
+    }
+}
+
+// WIDE: rows begin on 16 bytes, a lane has four tokens side by side; else they are THREADS apart.
+template <uint32_t SLICE, uint32_t THREADS, bool WIDE>
+__global__ void __launch_bounds__(THREADS) logits_kernel(const LogitsArgs a)
 {
 #pragma clang fp contract(off)
-    __shared__ uint32_t counts[SLICE], entries[SLICE];  // entries: one more than the last entry's number in the row, 0: none
+    constexpr uint32_t kQuads = SLICE / THREADS / 4;
+    __shared__ __align__(16) uint32_t counts[SLICE], entries[SLICE];  // entries: one more than the last entry's number in the row, 0: none
     const uint32_t row = blockIdx.y, first = blockIdx.x * SLICE;
     const uint32_t wide = a.vocab - first < SLICE ? a.vocab - first : SLICE;
-    const bool counted = a.history != nullptr, biased = a.bias_tokens != nullptr;
-    for (uint32_t i = threadIdx.x; i < SLICE; i += kLogitsThreads)
-        counts[i] = entries[i] = 0;
-    __syncthreads();
-    LogitsRange named = {0, 0};
-    if (counted) {
-        const LogitsRange r = logits_range(a.history_starts, row, a.history_tokens);
-        for (uint64_t i = r.begin + threadIdx.x; i < r.end; i += kLogitsThreads) {
-            const uint64_t at = static_cast<uint64_t>(a.history[i]) - first;
-            if (at < wide)
-                atomicAdd(&counts[at], 1u);
+    const uint64_t at = static_cast<uint64_t>(row) * a.vocab + first;
+    const auto place = [&](uint32_t quad, uint32_t c) { return WIDE ? (quad * THREADS + threadIdx.x) * 4 + c : (quad * 4 + c) * THREADS + threadIdx.x; };
+    // (on their way while the history is counted)
+    float x[kQuads][4];
+#pragma unroll
+    for (uint32_t quad = 0; quad < kQuads; ++quad) {
+        if constexpr (WIDE) {
+            if (place(quad, 0) < wide) {
+                const float4 v = *reinterpret_cast<const float4 *>(a.logits + at + place(quad, 0));
+                x[quad][0] = v.x, x[quad][1] = v.y, x[quad][2] = v.z, x[quad][3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (uint32_t c = 0; c < 4; ++c)
+                if (place(quad, c) < wide)
+                    x[quad][c] = a.logits[at + place(quad, c)];
         }
     }
-    if (biased) {
+    for (uint32_t i = threadIdx.x * 4; i < SLICE; i += THREADS * 4) {
+        *reinterpret_cast<uint4 *>(counts + i) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(entries + i) = make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    LogitsRange named = {0, 0};
+    if (a.history) {
+        const LogitsRange r = logits_range(a.history_starts, row, a.history_tokens);
+        logits_each<THREADS>(a.history, r.begin, r.end, [&](uint64_t, int64_t token) {
+            const uint64_t slot = static_cast<uint64_t>(token) - first;
+            if (token >= 0 && slot < wide)
+                atomicAdd(&counts[slot], 1u);
+        });
+    }
+    if (a.bias_tokens) {
         named = logits_range(a.bias_starts, row, a.bias_entries);
-        for (uint64_t i = named.begin + threadIdx.x; i < named.end; i += kLogitsThreads) {
-            const uint64_t at = static_cast<uint64_t>(a.bias_tokens[i]) - first;
-            if (at < wide)
-                atomicMax(&entries[at], static_cast<uint32_t>(i - named.begin) + 1);
-        }
+        logits_each<THREADS>(a.bias_tokens, named.begin, named.end, [&](uint64_t i, int64_t token) {
+            const uint64_t slot = static_cast<uint64_t>(token) - first;
+            if (token >= 0 && slot < wide)
+                atomicMax(&entries[slot], static_cast<uint32_t>(i - named.begin) + 1);
+        });
     }
     __syncthreads();
     const float repetition = a.repetition ? a.repetition[row] : 1.0f;
@@ -80,25 +114,35 @@ __global__ void __launch_bounds__(kLogitsThreads) logits_kernel(const LogitsArgs
     if (a.masks) {
         const int32_t id = a.mask_ids[row];
         if (id >= 0 && static_cast<uint32_t>(id) < a.mask_count)
-            mask = a.masks + id * a.mask_words;
+            mask = a.masks + static_cast<uint64_t>(id) * a.mask_words;
     }
-    const uint64_t at = static_cast<uint64_t>(row) * a.vocab + first;
-    for (uint32_t i = threadIdx.x; i < wide; i += kLogitsThreads) {
-        float x = a.logits[at + i];
-        const uint32_t count = counts[i], entry = entries[i];
-        if (count) {
-            x = x > 0.0f ? x / repetition : x * repetition;
-            x = x - frequency * static_cast<float>(count);
-            x = x - presence;
+#pragma unroll
+    for (uint32_t quad = 0; quad < kQuads; ++quad) {
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) {
+            const uint32_t i = place(quad, c);
+            if (i >= wide)
+                continue;
+            float &v = x[quad][c];
+            const uint32_t count = counts[i], entry = entries[i];
+            if (count) {
+                v = v > 0.0f ? v / repetition : v * repetition;
+                v = v - frequency * static_cast<float>(count);
+                v = v - presence;
+            }
+            if (entry)
+                v = v + a.bias_values[named.begin + entry - 1];
+            if (mask) {
+                const uint32_t token = first + i;
+                if (!((static_cast<uint32_t>(mask[token >> 5]) >> (token & 31u)) & 1u))
+                    v = -__builtin_inff();
+            }
+            if constexpr (!WIDE)
+                a.out[at + i] = v;
         }
-        if (entry)
-            x = x + a.bias_values[named.begin + entry - 1];
-        if (mask) {
-            const uint32_t token = first + i;
-            if (!((static_cast<uint32_t>(mask[token >> 5]) >> (token & 31u)) & 1u))
-                x = -__builtin_inff();
-        }
-        a.out[at + i] = x;
+        if constexpr (WIDE)
+            if (place(quad, 0) < wide)
+                *reinterpret_cast<float4 *>(a.out + at + place(quad, 0)) = make_float4(x[quad][0], x[quad][1], x[quad][2], x[quad][3]);
     }
 }
 
