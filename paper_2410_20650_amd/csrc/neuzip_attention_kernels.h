@@ -8,7 +8,7 @@
 // which in a page of the values are 16 consecutive bytes.  Bytes become bf16, times their page's scale, by one instruction for two (exact: e4m3 has 4
 // significant bits and scales are powers of two).
 //
-// attend_few_kernel: a workgroup has up to 16 rows, a wave every fourth step of 64 keys, keys and values from memory straight into registers; the four
+// attend_few_kernel: a workgroup has up to 16 rows, its waves a step of 64 keys each in turn, keys and values from memory straight into registers; the
 // waves' sums are joined in LDS.  Work is split over the keys too where there are few rows, and joined by attend_join_kernel.
 // What bounds it: the bytes of the cache.
 #pragma once
@@ -23,7 +23,6 @@ namespace nz {
 constexpr uint32_t kAttendThreads = 256;
 constexpr uint32_t kAttendFewRows = 16;
 constexpr uint32_t kAttendStep = 64;      // keys
-constexpr uint32_t kAttendLeastSteps = 4; // of a split: one for each wave
 constexpr float kAttendSlack = 6.0f;      // a row's weights may exceed 1 by so much (a factor of 64) before its sums are scaled down to a new maximum
 
 struct AttendArgs {
@@ -37,13 +36,24 @@ struct AttendArgs {
     uint32_t q_heads, group;
     uint32_t window;
     uint32_t splits, tiles;
-    uint32_t most_keys; // that a tile's rows see, as the caller has it
+    uint32_t most_keys;   // that a tile's rows see, as the caller has it
+    uint32_t least_steps; // of a split
     float scale;        // times log2(e)
 };
 
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 attend_bf16x8_t;
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 attend_bf16x2_t;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float attend_f32x4_t;
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float attend_f32x16_t;
+
+__device__ __forceinline__ float attend_max_of_halves(float v)
+{
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
+    const uint32_t low = both[0], high = both[1];  // (a bit cast of both[1] itself is taken for both[0]'s)
+    return fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
+}
 
 __device__ __forceinline__ float attend_exp2(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -126,7 +136,7 @@ __device__ __forceinline__ void attend_split(const AttendArgs &a, const AttendRa
     uint32_t each = ((keys + kAttendStep - 1) / kAttendStep + 1 + a.splits - 1) / a.splits;
     const uint32_t least = (last - first + a.splits - 1) / a.splits;
     each = each > least ? each : least;
-    each = each > kAttendLeastSteps ? each : kAttendLeastSteps;
+    each = each > a.least_steps ? each : a.least_steps;
     begin = first + split * each;
     begin = begin < last ? begin : last;
     end = last - begin > each ? begin + each : last;
@@ -138,12 +148,74 @@ __device__ __forceinline__ uint64_t attend_row(const AttendArgs &a, const NewTok
     return static_cast<uint64_t>(n.begin + r / a.group) * a.q_heads + head * a.group + r % a.group;
 }
 
-template <uint32_t DIM>
-__global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const AttendArgs a)
+// The waves' sums of a workgroup's rows together, and out.
+template <uint32_t DIM, uint32_t WAVES, uint32_t ROWS>
+__device__ __forceinline__ void attend_leave(const AttendArgs &a, const NewTokens &n, uint32_t head, uint32_t split, uint32_t row0, uint32_t row_end,
+                                             const float (&sums)[WAVES][ROWS][DIM + 4], const float2 (&stats)[WAVES][ROWS])
 {
-    constexpr uint32_t kWide = DIM / 64, kFeatures = DIM / 16, kWaves = kAttendThreads / 64, kStride = DIM + 4;
-    __shared__ float sums[kWaves][kAttendFewRows][kStride];
-    __shared__ float2 stats[kWaves][kAttendFewRows];
+    // lanes that share a row, kOf features each
+    constexpr uint32_t kOf = DIM * ROWS / (WAVES * 64);
+    const uint32_t r = threadIdx.x / (DIM / kOf), at = threadIdx.x % (DIM / kOf) * kOf;
+    if (row0 + r >= row_end)
+        return;
+    float all = -__builtin_inff(), whole = 0.0f, sum[kOf] = {};
+#pragma unroll
+    for (uint32_t w = 0; w < WAVES; ++w)
+        all = fmaxf(all, stats[w][r].x);
+    const float base = all == -__builtin_inff() ? 0.0f : all;
+#pragma unroll
+    for (uint32_t w = 0; w < WAVES; ++w) {
+        const float part = attend_exp2(stats[w][r].x - base);
+        whole += part * stats[w][r].y;
+#pragma unroll
+        for (uint32_t d = 0; d < kOf; ++d)
+            sum[d] += part * sums[w][r][at + d];
+    }
+    const uint64_t to = attend_row(a, n, head, row0 + r);
+    if (a.splits > 1) {
+        const uint64_t place = static_cast<uint64_t>(split) * a.s.rows * a.q_heads + to;
+        if (at == 0)
+            a.stats[place] = make_float2(all, whole);
+#pragma unroll
+        for (uint32_t d = 0; d < kOf; d += 2)
+            *reinterpret_cast<float2 *>(a.partial + place * DIM + at + d) = make_float2(sum[d], sum[d + 1]);
+        return;
+    }
+    const float once = whole == 0.0f ? 0.0f : 1.0f / whole;
+#pragma unroll
+    for (uint32_t d = 0; d < kOf; d += 2) {
+        typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2_t;
+        const f32x2_t v = {sum[d] * once, sum[d + 1] * once};
+        *reinterpret_cast<attend_bf16x2_t *>(a.out + to * DIM + at + d) = __builtin_convertvector(v, attend_bf16x2_t);
+    }
+}
+
+// Adds to `seen`, of every row, how many of the values of `feature` that it sees are NaN among 64 keys from k0 on (32 x 32 x 16).
+__device__ __forceinline__ attend_f32x16_t attend_nans(const AttendArgs &a, uint32_t s, uint32_t head, uint32_t dim, uint32_t feature, uint32_t k0, uint32_t half,
+                                                       uint32_t my_low, uint32_t my_high, attend_f32x16_t seen)
+{
+    const uint32_t shift = a.s.page_shift;
+#pragma unroll 1
+    for (uint32_t u = 0; u < 4; ++u) {
+        const uint32_t key = k0 + u / 2 * 32 + half * 16 + u % 2 * 8, page = page_of(a.s, s, key >> shift);
+        const uint64_t at = ((static_cast<uint64_t>(page != kNoPage ? page : 0) * a.c.heads + head) * dim + feature) << shift;
+        const uint2 bytes = *reinterpret_cast<const uint2 *>(a.c.v + at + (key & ((1u << shift) - 1)));
+        attend_bf16x8_t sees;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+            sees[e] = page != kNoPage && key + e >= my_low && key + e < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
+        const attend_bf16x8_t is = attend_widen((attend_nan_bytes(bytes.x) >> 7) * kE4m3One, (attend_nan_bytes(bytes.y) >> 7) * kE4m3One, 1.0f);
+        seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
+    }
+    return seen;
+}
+
+template <uint32_t DIM, uint32_t WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendArgs a)
+{
+    constexpr uint32_t kWide = DIM / 64, kFeatures = DIM / 16, kStride = DIM + 4;
+    __shared__ float sums[WAVES][kAttendFewRows][kStride];
+    __shared__ float2 stats[WAVES][kAttendFewRows];
     __shared__ attend_bf16x8_t queries[kWide * 2][64];
     const uint32_t split = blockIdx.x % a.splits, head = blockIdx.x / a.splits % a.c.heads, tile = blockIdx.x / a.splits / a.c.heads;
     const TileNumbers numbers = {kAttendFewRows, a.group, 1};
@@ -213,9 +285,9 @@ __global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const Att
         find_pages(step);
         request_keys(step);
         request_values(step);
-        find_pages(step + kWaves);
+        find_pages(step + WAVES);
     }
-    for (; step < last; step += kWaves) {
+    for (; step < last; step += WAVES) {
         const uint32_t k0 = step * kAttendStep, v_group = k0 + g * 16;
         asm volatile("" ::: "memory");  // (it stays in LDS)
         attend_f32x4_t score[4] = {};
@@ -229,8 +301,8 @@ __global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const Att
             }
         }
         // at an edge: what a row does not see; values that no row sees, and NaN (0 * NaN is), are made 0, and who sees NaN is looked up in the end
-        if (step + kWaves < last)
-            request_keys(step + kWaves);
+        if (step + WAVES < last)
+            request_keys(step + WAVES);
         if (attend_edge(range, k0) || __any(!held)) {
 #pragma unroll
             for (uint32_t t = 0; t < 4; ++t)
@@ -278,9 +350,9 @@ __global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const Att
             o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].x, v[f].y, v_scale), p0, o[f], 0, 0, 0);
             o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].z, v[f].w, v_scale), p1, o[f], 0, 0, 0);
         }
-        if (step + kWaves < last) {
-            request_values(step + kWaves);
-            find_pages(step + 2 * kWaves);
+        if (step + WAVES < last) {
+            request_values(step + WAVES);
+            find_pages(step + 2 * WAVES);
         }
     }
     total += __shfl_xor(total, 16);
@@ -290,7 +362,7 @@ __global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const Att
 #pragma unroll
         for (uint32_t f = 0; f < kFeatures; ++f) {
             attend_f32x4_t seen = {};
-            for (step = begin; step < last; step += kWaves)
+            for (step = begin; step < last; step += WAVES)
 #pragma unroll 1
                 for (uint32_t u = 0; u < 2; ++u) {
                     const uint32_t key = step * kAttendStep + g * 16 + u * 8, page = page_of(a.s, s, key >> shift);
@@ -314,40 +386,183 @@ __global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const Att
     for (uint32_t f = 0; f < kFeatures; ++f)
         *reinterpret_cast<attend_f32x4_t *>(&sums[wave][i][f * 16 + g * 4]) = o[f];
     __syncthreads();
-    // sixteen lanes to a row
-    const uint32_t r = threadIdx.x / 16, at = threadIdx.x % 16 * (DIM / 16);
-    if (row0 + r >= row_end)
+    attend_leave<DIM, WAVES, kAttendFewRows>(a, n, head, split, row0, row_end, sums, stats);
+}
+
+// ---- some rows: the same with 32 rows to a workgroup, in matrix instructions of 32 x 32.  Here the lane (row c = l % 32, half h = l / 32) has of
+// every 32 keys the ones 16 h .. 16 h + 15; row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4.
+constexpr uint32_t kAttendSomeRows = 32;
+
+template <uint32_t DIM>
+__global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const AttendArgs a)
+{
+    constexpr uint32_t kWide = DIM / 32, WAVES = kAttendThreads / 64, kStride = DIM + 4;
+    __shared__ float sums[WAVES][kAttendSomeRows][kStride];
+    __shared__ float2 stats[WAVES][kAttendSomeRows];
+    __shared__ attend_bf16x8_t queries[kWide * 2][64];
+    const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
+    const TileNumbers numbers = {kAttendSomeRows, a.group, 1};
+    const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
+    if (s >= a.s.count)
         return;
-    float all = -__builtin_inff(), whole = 0.0f, sum[DIM / 16] = {};
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w)
-        all = fmaxf(all, stats[w][r].x);
-    const float base = all == -__builtin_inff() ? 0.0f : all;
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        const float part = attend_exp2(stats[w][r].x - base);
-        whole += part * stats[w][r].y;
-#pragma unroll
-        for (uint32_t d = 0; d < DIM / 16; ++d)
-            sum[d] += part * sums[w][r][at + d];
-    }
-    const uint64_t to = attend_row(a, n, head, row0 + r);
-    if (a.splits > 1) {
-        const uint64_t place = static_cast<uint64_t>(split) * a.s.rows * a.q_heads + to;
-        if (at == 0)
-            a.stats[place] = make_float2(all, whole);
-#pragma unroll
-        for (uint32_t d = 0; d < DIM / 16; d += 4)
-            *reinterpret_cast<float4 *>(a.partial + place * DIM + at + d) = make_float4(sum[d], sum[d + 1], sum[d + 2], sum[d + 3]);
+    const NewTokens n = new_tokens(a.s, s);
+    const uint64_t row0_wide = (tile - first_tile(numbers, a.s.starts[s], s)) * kAttendSomeRows;
+    const uint32_t rows = n.count * a.group;
+    if (row0_wide >= rows)
         return;
-    }
-    const float once = whole == 0.0f ? 0.0f : 1.0f / whole;
+    const uint32_t row0 = static_cast<uint32_t>(row0_wide), row_end = rows - row0 < kAttendSomeRows ? rows : row0 + kAttendSomeRows;
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 32, h = lane / 32;
+    const AttendRange range = attend_range(n, row0 / a.group, (row_end - 1) / a.group, a.window);
+    const bool mine = row0 + c < row_end;
+    const uint32_t row = mine ? row0 + c : row0, position = n.first + row / a.group;
+    const uint32_t my_high = mine ? position + 1 : 0, my_low = a.window && position + 1 > a.window ? position + 1 - a.window : 0;
+    const uint16_t *q_at = a.q + (n.begin + row / a.group) * a.q_row + (head * a.group + row % a.group) * DIM + h * 16;
 #pragma unroll
-    for (uint32_t d = 0; d < DIM / 16; d += 4) {
-        typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
-        const attend_f32x4_t v = {sum[d] * once, sum[d + 1] * once, sum[d + 2] * once, sum[d + 3] * once};
-        *reinterpret_cast<bf16x4_t *>(a.out + to * DIM + at + d) = __builtin_convertvector(v, bf16x4_t);
+    for (uint32_t j = wave; j < kWide * 2; j += WAVES)
+        queries[j][lane] = *reinterpret_cast<const attend_bf16x8_t *>(q_at + j / 2 * 32 + j % 2 * 8);
+    __syncthreads();
+
+    attend_f32x16_t o[kWide] = {};
+    float top = -__builtin_inff(), total = 0.0f;
+    uint32_t step, last;
+    attend_split(a, range, split, step, last);
+    const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
+    const uint32_t k_row = c / 4 % 2 * 16 + c / 8 * 4 + c % 4;
+    uint32_t k_page[2], v_page[2];
+    const auto page_at = [&](uint32_t group) { return group < range.high && group + 16 > range.low ? page_of(a.s, s, group >> shift) : kNoPage; };
+    const auto find_pages = [&](uint32_t at) {
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x) {
+            const uint32_t k0 = at * kAttendStep + x * 32;
+            k_page[x] = at < last ? page_at(k0 + c / 4 % 2 * 16) : kNoPage;
+            v_page[x] = at < last ? page_at(k0 + h * 16) : kNoPage;
+        }
+    };
+    uint4 k[2][kWide], v[2][kWide];
+    float k_scale[2], v_scale[2];
+    bool held[2];
+    uint32_t found = 0;  // NaN among values that not all rows see
+    const auto request_keys = [&](uint32_t at) {
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x) {
+            const uint64_t page = static_cast<uint64_t>(k_page[x] != kNoPage ? k_page[x] : 0) * a.c.heads + head;  // (read, and not used)
+            const uint8_t *from = a.c.k + ((page << shift) + ((at * kAttendStep + x * 32 + k_row) & inside)) * DIM + h * 16;
+            k_scale[x] = a.c.k_scales[page];
+#pragma unroll
+            for (uint32_t j = 0; j < kWide; ++j)
+                k[x][j] = *reinterpret_cast<const uint4 *>(from + j * 32);
+        }
+    };
+    const auto request_values = [&](uint32_t at) {
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x) {
+            held[x] = v_page[x] != kNoPage;
+            const uint64_t page = static_cast<uint64_t>(held[x] ? v_page[x] : 0) * a.c.heads + head;
+            const uint8_t *from = a.c.v + ((page * DIM + c) << shift) + ((at * kAttendStep + x * 32 + h * 16) & inside);
+            v_scale[x] = a.c.v_scales[page];
+            v_scale[x] = held[x] ? v_scale[x] : 1.0f;
+#pragma unroll
+            for (uint32_t f = 0; f < kWide; ++f)
+                v[x][f] = *reinterpret_cast<const uint4 *>(from + (f * 32 << shift));
+        }
+    };
+    step += wave;
+    const uint32_t begin = step;
+    if (step < last) {
+        find_pages(step);
+        request_keys(step);
+        request_values(step);
+        find_pages(step + WAVES);
     }
+    for (; step < last; step += WAVES) {
+        const uint32_t k0 = step * kAttendStep;
+        asm volatile("" ::: "memory");  // (the queries stay in LDS)
+        attend_f32x16_t score[2] = {};
+#pragma unroll
+        for (uint32_t j = 0; j < kWide; ++j) {
+            const attend_bf16x8_t first = queries[j * 2][lane], second = queries[j * 2 + 1][lane];
+#pragma unroll
+            for (uint32_t x = 0; x < 2; ++x) {
+                score[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(k[x][j].x, k[x][j].y, k_scale[x]), first, score[x], 0, 0, 0);
+                score[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(k[x][j].z, k[x][j].w, k_scale[x]), second, score[x], 0, 0, 0);
+            }
+        }
+        if (step + WAVES < last)
+            request_keys(step + WAVES);
+        if (attend_edge(range, k0) || __any(!held[0] || !held[1])) {
+#pragma unroll
+            for (uint32_t x = 0; x < 2; ++x) {
+                const uint32_t group = k0 + x * 32 + h * 16;
+#pragma unroll
+                for (uint32_t e = 0; e < 16; ++e)
+                    if (!(held[x] && group + e >= my_low && group + e < my_high))
+                        score[x][e] = -__builtin_inff();
+                const int32_t from = held[x] ? static_cast<int32_t>(range.low - group) : 16, upto = held[x] ? static_cast<int32_t>(range.high - group) : 0;
+                const uint32_t m0 = attend_bytes(from, upto, 0), m1 = attend_bytes(from, upto, 1), m2 = attend_bytes(from, upto, 2), m3 = attend_bytes(from, upto, 3);
+#pragma unroll
+                for (uint32_t f = 0; f < kWide; ++f)
+                    found |= attend_clean(v[x][f].x, m0) | attend_clean(v[x][f].y, m1) | attend_clean(v[x][f].z, m2) | attend_clean(v[x][f].w, m3);
+            }
+        }
+        float most = -__builtin_inff();
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x)
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e)
+                most = fmaxf(most, score[x][e]);
+        most = attend_max_of_halves(most) * a.scale;
+        if (__any(most > top + kAttendSlack)) {
+            const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+            top = higher;
+            total *= less;
+#pragma unroll
+            for (uint32_t f = 0; f < kWide; ++f)
+                o[f] *= less;
+        }
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+        for (uint32_t x = 0; x < 2; ++x) {
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e) {
+                score[x][e] = attend_exp2(score[x][e] * a.scale - base);
+                total += score[x][e];
+            }
+            const attend_f32x16_t &w = score[x];
+            const attend_bf16x8_t p0 = attend_round(w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
+            const attend_bf16x8_t p1 = attend_round(w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]);
+#pragma unroll
+            for (uint32_t f = 0; f < kWide; ++f) {
+                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(v[x][f].x, v[x][f].y, v_scale[x]), p0, o[f], 0, 0, 0);
+                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(v[x][f].z, v[x][f].w, v_scale[x]), p1, o[f], 0, 0, 0);
+            }
+        }
+        if (step + WAVES < last) {
+            request_values(step + WAVES);
+            find_pages(step + 2 * WAVES);
+        }
+    }
+    total += __shfl_xor(total, 32);
+    if (__any(found != 0)) {
+        // a row that sees a value that is NaN has it: products of where NaN is with who sees it
+#pragma unroll
+        for (uint32_t f = 0; f < kWide; ++f) {
+            attend_f32x16_t seen = {};
+            for (step = begin; step < last; step += WAVES)
+                seen = attend_nans(a, s, head, DIM, f * 32 + c, step * kAttendStep, h, my_low, my_high, seen);
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e)
+                o[f][e] = seen[e] > 0.0f ? __builtin_nanf("") : o[f][e];
+        }
+    }
+    if (h == 0)
+        stats[wave][c] = make_float2(top, total);
+#pragma unroll
+    for (uint32_t f = 0; f < kWide; ++f)
+#pragma unroll
+        for (uint32_t e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4 *>(&sums[wave][c][f * 32 + e * 2 + h * 4]) = make_float4(o[f][e], o[f][e + 1], o[f][e + 2], o[f][e + 3]);
+    __syncthreads();
+    attend_leave<DIM, WAVES, kAttendSomeRows>(a, n, head, split, row0, row_end, sums, stats);
 }
 
 // ---- many rows: a workgroup has 128, a wave 32 of them.  A step's keys and values are widened once, by all four waves, into LDS, from where every wave
@@ -356,16 +571,6 @@ __global__ void __launch_bounds__(kAttendThreads, 3) attend_few_kernel(const Att
 // In LDS: row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4, its pieces of 16 bytes (8 features) in places p ^ c % kPieces;
 // the values' row is a feature, 64 keys in 8 pieces, in places p ^ feature % 8: what 8 lanes read together lies in different banks.
 constexpr uint32_t kAttendManyRows = 128;
-
-typedef __attribute__((__vector_size__(16 * sizeof(float)))) float attend_f32x16_t;
-
-__device__ __forceinline__ float attend_max_of_halves(float v)
-{
-    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
-    const auto both = __builtin_amdgcn_permlane32_swap(bits, bits, false, false);
-    const uint32_t low = both[0], high = both[1];  // (a bit cast of both[1] itself is taken for both[0]'s)
-    return fmaxf(__builtin_bit_cast(float, low), __builtin_bit_cast(float, high));
-}
 
 template <uint32_t DIM>
 struct alignas(16) AttendStep {  // of 64 keys in LDS
@@ -555,21 +760,8 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
 #pragma unroll
         for (uint32_t f = 0; f < DIM / 32; ++f) {
             attend_f32x16_t seen = {};
-            for (step = begin; step < last; ++step) {
-                const uint32_t k0 = step * kAttendStep;
-#pragma unroll 1
-                for (uint32_t u = 0; u < 4; ++u) {
-                    const uint32_t key = k0 + u / 2 * 32 + h * 16 + u % 2 * 8, page = page_of(a.s, s, key >> shift);
-                    const uint64_t at = ((static_cast<uint64_t>(page != kNoPage ? page : 0) * a.c.heads + head) * DIM + f * 32 + c) << shift;
-                    const uint2 bytes = *reinterpret_cast<const uint2 *>(a.c.v + at + (key & inside));
-                    attend_bf16x8_t sees;
-#pragma unroll
-                    for (uint32_t e = 0; e < 8; ++e)
-                        sees[e] = page != kNoPage && key + e >= my_low && key + e < my_high ? static_cast<__bf16>(1.0f) : static_cast<__bf16>(0.0f);
-                    const attend_bf16x8_t is = attend_widen((attend_nan_bytes(bytes.x) >> 7) * kE4m3One, (attend_nan_bytes(bytes.y) >> 7) * kE4m3One, 1.0f);
-                    seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(is, sees, seen, 0, 0, 0);
-                }
-            }
+            for (step = begin; step < last; ++step)
+                seen = attend_nans(a, s, head, DIM, f * 32 + c, step * kAttendStep, h, my_low, my_high, seen);
 #pragma unroll
             for (uint32_t e = 0; e < 16; ++e)
                 o[f][e] = seen[e] > 0.0f ? __builtin_nanf("") : o[f][e];

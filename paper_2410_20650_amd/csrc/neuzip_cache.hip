@@ -16,8 +16,11 @@ using namespace nz;
 namespace {
 
 constexpr uint64_t kAttendMostRows = 1ull << 27;  // rows times query heads
-constexpr uint32_t kAttendWgs = 512;              // that a launch is split into at least, where its keys allow it: two on a CU
-constexpr uint64_t kAttendUneven = 2;
+constexpr uint32_t kAttendCus = 256;
+constexpr uint32_t kAttendWaves = 2048;     // that a launch is split into, where its keys allow it: two to a SIMD
+constexpr uint32_t kAttendWaveSteps = 2;    // of each wave of a split at least, few rows
+constexpr uint64_t kAttendManyWgs = 512;
+constexpr uint32_t kAttendManySteps = 8;    // of a split at least, many rows
 constexpr uint32_t kAttendMostSplits = 128;
 
 inline bool off(const void *p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) & (size - 1); }
@@ -63,9 +66,10 @@ void launch_append(const AppendArgs &a, uint32_t wgs, hipStream_t stream)
 }
 
 struct AttendShape {
-    bool many;  // rows to a workgroup
+    uint32_t rows;   // to a workgroup
+    uint32_t waves;  // to a workgroup
     uint64_t tiles;
-    uint32_t splits, keys;
+    uint32_t splits, keys, least_steps;
     uint64_t sums, bytes;  // of scratch memory: the partial sums, and with the rows' statistics
 };
 
@@ -76,16 +80,22 @@ AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint3
         longest = room;
     const uint32_t group = q_heads / c->heads;
     AttendShape shape;
-    shape.many = static_cast<uint64_t>(rows) * group > static_cast<uint64_t>(s->count) * kAttendFewRows;
-    const uint32_t tile = shape.many ? kAttendManyRows : kAttendFewRows;
+    // rows to a workgroup: as many as a sequence has, about; 128 only where that leaves enough workgroups
+    const uint64_t all = static_cast<uint64_t>(rows) * group;
+    shape.rows = all <= static_cast<uint64_t>(s->count) * kAttendFewRows                                ? kAttendFewRows
+                 : all / kAttendManyRows * c->heads < kAttendManyWgs ? kAttendSomeRows
+                                                                                                    : kAttendManyRows;
+    const uint32_t tile = shape.rows;
     shape.tiles = tile_count({tile, group, 1}, rows, s->count);
+    // workgroups that have something to do, about
+    const uint64_t full = (all + tile - 1) / tile;
+    const uint64_t wgs = (full > s->count ? full : s->count) * c->heads;
+    shape.waves = tile == kAttendFewRows && wgs <= kAttendCus ? 8 : 4;
     // the keys that a tile's rows see, at most
     const uint64_t span = static_cast<uint64_t>(window) + tile / group + 1;
     const uint64_t keys = window && span < longest ? span : longest;
-    const uint64_t wgs = shape.tiles * c->heads;
-    // (several sequences are seldom equally long: more splits, so that no CU waits long for another)
-    const uint64_t uneven = s->count < kAttendUneven ? s->count : kAttendUneven;
-    const uint64_t wanted = (uneven * kAttendWgs + wgs - 1) / wgs, most = keys / (kAttendStep * kAttendLeastSteps);
+    shape.least_steps = tile == kAttendManyRows ? kAttendManySteps : kAttendWaveSteps * shape.waves;
+    const uint64_t wanted = (kAttendWaves + wgs * shape.waves - 1) / (wgs * shape.waves), most = keys / (kAttendStep * shape.least_steps);
     uint64_t splits = wanted < most ? wanted : most;
     splits = splits < kAttendMostSplits ? splits : kAttendMostSplits;
     shape.splits = splits ? static_cast<uint32_t>(splits) : 1;
@@ -99,12 +109,16 @@ AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint3
 inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_heads > 0 && q_heads % c->heads == 0; }
 
 template <uint32_t DIM>
-int launch_attend(const AttendArgs &a, bool many, uint32_t wgs, hipStream_t stream)
+int launch_attend(const AttendArgs &a, const AttendShape &shape, uint32_t wgs, hipStream_t stream)
 {
-    if (many)
+    if (shape.rows == kAttendSomeRows)
+        hipLaunchKernelGGL((attend_some_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    else if (shape.rows == kAttendManyRows)
         hipLaunchKernelGGL((attend_many_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    else if (shape.waves == 8)
+        hipLaunchKernelGGL((attend_few_kernel<DIM, 8>), dim3(wgs), dim3(512), 0, stream, a);
     else
-        hipLaunchKernelGGL((attend_few_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+        hipLaunchKernelGGL((attend_few_kernel<DIM, 4>), dim3(wgs), dim3(256), 0, stream, a);
     if (!hip_ok(hipGetLastError()))
         return NEUZIP_EHIP;
     if (a.splits > 1) {
@@ -200,7 +214,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
     if (shape.bytes && (!d_scratch || scratch_bytes < shape.bytes))
         return NEUZIP_EINVAL;
     const uint64_t wgs = shape.tiles * cache->heads * shape.splits;
-    if (too_many_wgs(wgs, kAttendThreads))
+    if (too_many_wgs(wgs, 512))
         return NEUZIP_EUNSUPPORTED;
     AttendArgs a;
     a.s = view_of(cache, sequences, rows);
@@ -216,10 +230,11 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
     a.splits = shape.splits;
     a.tiles = static_cast<uint32_t>(shape.tiles);
     a.most_keys = shape.keys;
+    a.least_steps = shape.least_steps;
     a.scale = scale * 1.4426950408889634f;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint32_t grid = static_cast<uint32_t>(wgs);
-    return cache->head_dim == 64 ? launch_attend<64>(a, shape.many, grid, stream) : launch_attend<128>(a, shape.many, grid, stream);
+    return cache->head_dim == 64 ? launch_attend<64>(a, shape, grid, stream) : launch_attend<128>(a, shape, grid, stream);
 }
 
 }  // extern "C"
