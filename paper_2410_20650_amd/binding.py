@@ -160,13 +160,14 @@ def library():
     return _lib
 
 
-def _stream_handle(stream):
+def _stream_handle(stream, device=None):
+    """device: the current one, where the caller has looked it up."""
     if stream is None:
         # (torch.cuda.current_stream() makes an object of it first: 3 us of the host's 8 for a small call; the other is torch's own affair
         # and may be gone from one version to the next)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
-            return ctypes.c_void_p(raw(torch.cuda.current_device()))
+            return ctypes.c_void_p(raw(torch.cuda.current_device() if device is None else device))
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
@@ -790,7 +791,7 @@ def neuzip_norm(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: tor
     else:
         _here(y, torch.bfloat16, shape, "y", device)
     rc = _lib.neuzip_norm(x.data_ptr(), x_type, _pointer(residual), _pointer(total), total_type, weight.data_ptr(), tokens, width, eps,
-                          y.data_ptr(), _stream_handle(stream))
+                          y.data_ptr(), _stream_handle(stream, device))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_norm")
     return y if residual is None else (y, total)
@@ -830,7 +831,7 @@ def neuzip_norm_backward(total: torch.Tensor, weight: torch.Tensor, grad_y: torc
     if grad_weight is not None:
         scratch = _scratch_here(_lib.neuzip_norm_backward_scratch_bytes(tokens, width), scratch, total, device, stream)
     rc = _lib.neuzip_norm_backward(total.data_ptr(), total_type, weight.data_ptr(), grad_y.data_ptr(), _pointer(grad_total), tokens, width, eps,
-                                   _pointer(grad_x), _pointer(grad_weight), _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+                                   _pointer(grad_x), _pointer(grad_weight), _pointer(scratch), _bytes_of(scratch), _stream_handle(stream, device))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_norm_backward")
     return grad_x, grad_weight
@@ -943,7 +944,7 @@ def neuzip_cache_append(cache: KeyValueCache, sequences: Sequences, k: torch.Ten
         if rotary_rows < sequences._struct.table_width * cache.page_tokens:
             raise ValueError("rotary must have a row for each position that the table has room for")
     rc = _lib.neuzip_cache_append(cache._struct, sequences._struct, kind, k.data_ptr(), k_row, v.data_ptr(), v_row, _pointer(q), q_row, q_heads,
-                                  _pointer(q_out), _pointer(rotary), rotary_rows, rows, _stream_handle(stream))
+                                  _pointer(q_out), _pointer(rotary), rotary_rows, rows, _stream_handle(stream, device))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_cache_append")
     return q_out
@@ -966,7 +967,7 @@ def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.
     if q_heads == 0 or q_heads % cache.heads:
         raise ValueError("the query heads are a multiple of the cache's heads")
     if out is None:
-        out = _empty(q.shape, torch.bfloat16, q.device, stream)
+        out = _empty_like(q, torch.bfloat16, stream)    # (without gaps, also where q's rows lie apart)
     else:
         _here(out, torch.bfloat16, (rows, q_heads, dim), "out", device)
     if scale is None:
@@ -974,7 +975,7 @@ def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.
     room = _lib.neuzip_cache_attention_scratch_bytes(cache._struct, sequences._struct, q_heads, rows, window, longest)
     scratch = _scratch_here(room, scratch, q, device, stream)
     rc = _lib.neuzip_cache_attention(cache._struct, sequences._struct, q.data_ptr(), q_row, q_heads, rows, scale, window, longest, out.data_ptr(),
-                                     _pointer(scratch), _bytes_of(scratch), _stream_handle(stream))
+                                     _pointer(scratch), _bytes_of(scratch), _stream_handle(stream, device))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_cache_attention")
     return out
@@ -1030,7 +1031,7 @@ def neuzip_logits(logits: torch.Tensor, history: torch.Tensor = None, history_st
         _here(out, torch.float32, (rows, vocab), "out", device)
     rc = _lib.neuzip_logits(logits.data_ptr(), rows, vocab, _pointer(history), history_tokens, _pointer(history_starts), _pointer(repetition),
                             _pointer(frequency), _pointer(presence), _pointer(bias), _pointer(bias_values), entries, _pointer(bias_starts),
-                            _pointer(masks), count, _pointer(mask_ids), out.data_ptr(), _stream_handle(stream))
+                            _pointer(masks), count, _pointer(mask_ids), out.data_ptr(), _stream_handle(stream, device))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_logits")
     return out

@@ -18,7 +18,7 @@ namespace nz {
 constexpr uint32_t kNormThreads = 256;       // a workgroup of the forward pass with rows of up to 256 lanes
 constexpr uint32_t kNormBackThreads = 1024;  // and of the backward pass: one on a CU
 constexpr uint32_t kNormMostWgs = 256;       // of the backward pass, so many parts of dw
-constexpr uint32_t kNormJoinColumns = 64;
+constexpr uint32_t kNormJoinColumns = 16;
 
 struct NormArgs {
     const void *x, *residual;
@@ -242,22 +242,30 @@ __global__ void __launch_bounds__(kNormBackThreads) norm_back_kernel(const NormB
     }
 }
 
-// dw: the sum of `count` rows of `width` floats, kNormJoinColumns columns to a workgroup, sixteen runs of rows side by side.
+// dw: the sum of `count` rows of `width` floats, kNormJoinColumns columns to a workgroup, 64 runs of rows side by side.  (Its time is one way to
+// memory and back, 3.x us, whatever there is to add.)
 inline __global__ void __launch_bounds__(256) norm_join_kernel(const float *parts, float *grad_weight, uint32_t count, uint32_t width)
 {
-    __shared__ float4 sums[16][kNormJoinColumns / 4];
-    const uint32_t x = threadIdx.x % 16, y = threadIdx.x / 16, col = blockIdx.x * kNormJoinColumns + x * 4;
+    __shared__ float4 sums[4][kNormJoinColumns / 4];
+    const uint32_t x = threadIdx.x % 4, y = threadIdx.x / 4, col = blockIdx.x * kNormJoinColumns + x * 4;
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (col < width)
-        for (uint32_t r = y; r < count; r += 16) {
+#pragma unroll 4
+        for (uint32_t r = y; r < count; r += 64) {
             const float4 v = *reinterpret_cast<const float4 *>(parts + static_cast<uint64_t>(r) * width + col);
             sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
         }
-    sums[y][x] = sum;
+#pragma unroll
+    for (int apart = 4; apart < 64; apart *= 2) {
+        sum.x += __shfl_xor(sum.x, apart), sum.y += __shfl_xor(sum.y, apart);
+        sum.z += __shfl_xor(sum.z, apart), sum.w += __shfl_xor(sum.w, apart);
+    }
+    if (threadIdx.x % 64 < 4)
+        sums[threadIdx.x / 64][x] = sum;
     __syncthreads();
     if (y == 0 && col < width) {
 #pragma unroll
-        for (int i = 1; i < 16; ++i) {
+        for (int i = 1; i < 4; ++i) {
             const float4 v = sums[i][x];
             sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
         }
