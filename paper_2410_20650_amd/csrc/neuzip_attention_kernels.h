@@ -565,25 +565,27 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     attend_leave<DIM, WAVES, kAttendSomeRows>(a, n, head, split, row0, row_end, sums, stats);
 }
 
-// ---- many rows: a workgroup has 128, a wave 32 of them.  A step's keys and values are widened once, by all four waves, into LDS, from where every wave
-// reads them as operands; the next step's bytes are on their way meanwhile, and the pages of the one behind it.  Here the lane (row c = l % 32, half
-// h = l / 32) has of every 32 keys the ones 16 h .. 16 h + 15.
-// In LDS: row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4, its pieces of 16 bytes (8 features) in places p ^ c % kPieces;
-// the values' row is a feature, 64 keys in 8 pieces, in places p ^ feature % 8: what 8 lanes read together lies in different banks.
+// ---- many rows: a wave has 32 rows, a workgroup 128.  A step's keys and values are widened once, by all four waves, into LDS, from where every wave reads
+// them as operands; the next step's bytes are on their way meanwhile, and the pages of the one behind it.  Lanes hold keys as above.
+// In LDS: row c of 32 of the keys' operand, its pieces of 16 bytes (8 features) in places p ^ c % 16 (rows of 128 bytes: p ^ c / 2 % 8); the values' row is
+// a feature, 64 keys in 8 pieces, in places p ^ feature / 2 % 8: the sixteen lanes that read together, 0 to 3, 12 to 15, 20 to 27 or the others, find different banks.
+// What bounds it: a step of a wave takes the matrix cores 1024 cycles (head_dim 128), the vector unit about 1450 (exponentials 512, the rest of the softmax
+// 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD and half of it overlaps.  A prompt of 4096 tokens, 32
+// query heads on 8, takes 164 us, 835 TFLOP/s.  A wave with 64 rows halves what LDS reads, but fills 400 registers and is alone on its SIMD: 350 us; with the
+// next step's products beside this step's exponentials in the program 169 us: 256 registers leave none for operands on their way.
 constexpr uint32_t kAttendManyRows = 128;
+constexpr int kSchedVector = 0x2, kSchedMatrix = 0x8, kSchedLds = 0x100;  // kinds of instructions (sched_group_barrier)
 
-template <uint32_t DIM>
-struct alignas(16) AttendStep {  // of 64 keys in LDS
-    uint8_t k[kAttendStep * DIM * 2];
-    uint8_t v[DIM * kAttendStep * 2];
-    uint32_t there;     // bit i: keys 16 i .. 16 i + 15 have a page and are seen by some row
-};
-
-template <uint32_t DIM>
+// WIDE: a step lies in one page
+template <uint32_t DIM, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const AttendArgs a)
 {
-    constexpr uint32_t kPieces = DIM / 8, kItems = DIM / 64;  // items: 16 bytes of the cache, of keys and of values, to a thread
-    __shared__ AttendStep<DIM> steps[2];
+    constexpr uint32_t kPieces = DIM / 8, kBytes = kAttendStep * DIM * 2;
+    constexpr uint32_t kItems = kAttendStep * DIM / 16 / kAttendThreads;  // 16 bytes of the cache, of keys and of values, to a thread
+    constexpr uint32_t kKeysApart = kAttendStep / kItems, kFeaturesApart = DIM / kItems;
+    __shared__ __align__(16) uint8_t key_space[2][kBytes];
+    __shared__ __align__(16) uint8_t value_space[2][kBytes];
+    __shared__ uint4 there_space[2];  // of four times 16 keys: not 0 if they have a page
     const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
     const TileNumbers numbers = {kAttendManyRows, a.group, 1};
     const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
@@ -597,63 +599,77 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     const uint32_t row0 = static_cast<uint32_t>(row0_wide), row_end = rows - row0 < kAttendManyRows ? rows : row0 + kAttendManyRows;
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 32, h = lane / 32;
     const AttendRange range = attend_range(n, row0 / a.group, (row_end - 1) / a.group, a.window);
-    uint32_t step, last;
-    attend_split(a, range, split, step, last);
+    uint32_t begin, last;
+    attend_split(a, range, split, begin, last);
 
     // the wave's rows, and the lane's
     const uint32_t wave0 = row0 + wave * 32 < row_end ? row0 + wave * 32 : row_end - 1, wave_end = wave0 + 32 < row_end ? wave0 + 32 : row_end;
     const AttendRange of_wave = attend_range(n, wave0 / a.group, (wave_end - 1) / a.group, a.window);
     const bool mine = row0 + wave * 32 + c < row_end;
-    const uint32_t row = mine ? row0 + wave * 32 + c : row_end - 1, position = n.first + row / a.group;
-    const uint32_t my_high = mine ? position + 1 : 0, my_low = a.window && position + 1 > a.window ? position + 1 - a.window : 0;
+    const uint32_t row = mine ? row0 + wave * 32 + c : row_end - 1, behind = n.first + row / a.group + 1;
+    const uint32_t my_high = mine ? behind : 0, my_low = a.window && behind > a.window ? behind - a.window : 0;
     attend_bf16x8_t q[DIM / 16];
     const uint16_t *q_at = a.q + (n.begin + row / a.group) * a.q_row + (head * a.group + row % a.group) * DIM + h * 8;
 #pragma unroll
     for (uint32_t j = 0; j < DIM / 16; ++j)
         q[j] = *reinterpret_cast<const attend_bf16x8_t *>(q_at + j * 16);
 
-    // the thread's items of a step: a key's 16 features (keys 32 apart where there are two), a feature's 16 keys
+    // the thread's items of a step: a key's 16 features, a feature's 16 keys
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     const uint32_t k_key = threadIdx.x / (DIM / 16), k_part = threadIdx.x % (DIM / 16), v_feature = threadIdx.x / 4, v_part = threadIdx.x % 4;
-    uint32_t k_page[kItems], v_page;
-    const auto find_pages = [&](uint32_t at) {
-        const uint32_t k0 = at * kAttendStep;
+    uint32_t k_page[WIDE ? 1 : kItems], v_page;
+    const auto find_key_pages = [&](uint32_t at) {
 #pragma unroll
-        for (uint32_t i = 0; i < kItems; ++i)
-            k_page[i] = at < last ? page_of(a.s, s, (k0 + k_key + i * 32) >> shift) : kNoPage;
-        v_page = at < last && k0 + v_part * 16 < range.high && k0 + v_part * 16 + 16 > range.low ? page_of(a.s, s, (k0 + v_part * 16) >> shift) : kNoPage;
+        for (uint32_t i = 0; i < (WIDE ? 1 : kItems); ++i)
+            k_page[i] = at < last ? page_of(a.s, s, (at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) >> shift) : kNoPage;
+    };
+    const auto find_value_pages = [&](uint32_t at) {
+        const uint32_t v0 = at * kAttendStep + (WIDE ? 0 : v_part * 16);
+        v_page = at < last && (WIDE || (v0 < range.high && v0 + 16 > range.low)) ? page_of(a.s, s, v0 >> shift) : kNoPage;
     };
     uint4 k_item[kItems], v_item[kItems];
-    float k_scale[kItems], v_scale;
-    bool v_there;
-    const auto request = [&](uint32_t at) {
-        const uint32_t k0 = at * kAttendStep;
+    float k_scale[WIDE ? 1 : kItems], v_scale;
+    bool k_there[WIDE ? 1 : kItems], v_there;
+    const auto request_keys = [&](uint32_t at) {
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
-            const uint64_t page = static_cast<uint64_t>(k_page[i] != kNoPage ? k_page[i] : 0) * a.c.heads + head;  // (read, and not used)
-            k_scale[i] = a.c.k_scales[page];
-            k_item[i] = *reinterpret_cast<const uint4 *>(a.c.k + ((page << shift) + ((k0 + k_key + i * 32) & inside)) * DIM + k_part * 16);
+            const uint32_t p = WIDE ? 0 : i;
+            k_there[p] = k_page[p] != kNoPage;
+            const uint64_t page = static_cast<uint64_t>(k_there[p] ? k_page[p] : 0) * a.c.heads + head;  // (read, and not used)
+            k_scale[p] = a.c.k_scales[page];
+            const uint8_t *from = a.c.k + ((page << shift) + ((at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) & inside)) * DIM;
+            k_item[i] = *reinterpret_cast<const uint4 *>(from + (WIDE ? (k_key + i * kKeysApart) * DIM : 0) + k_part * 16);
         }
+    };
+    const auto request_values = [&](uint32_t at) {
         v_there = v_page != kNoPage;
         const uint64_t page = static_cast<uint64_t>(v_there ? v_page : 0) * a.c.heads + head;
-        v_scale = v_there ? a.c.v_scales[page] : 1.0f;
+        v_scale = a.c.v_scales[page];
+        v_scale = v_there ? v_scale : 1.0f;
+        const uint8_t *from = a.c.v + (page * DIM << shift) + ((at * kAttendStep + (WIDE ? 0 : v_part * 16)) & inside);
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i)
-            v_item[i] = *reinterpret_cast<const uint4 *>(a.c.v + ((page * DIM + v_feature + i * 64) << shift) + ((k0 + v_part * 16) & inside));
+            v_item[i] = *reinterpret_cast<const uint4 *>(from + ((v_feature + i * kFeaturesApart) << shift) + (WIDE ? v_part * 16 : 0));
     };
-    uint32_t found = 0;  // NaN among values that not all rows see
-    const auto put = [&](uint32_t at, AttendStep<DIM> &to) {
-        const uint32_t k0 = at * kAttendStep;
+    const auto put_keys = [&](uint32_t turn) {
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
-            const uint32_t key = k_key + i * 32, x = key % 32, r = key / 32 * 32 + x / 4 % 4 * 8 + x / 16 * 4 + x % 4;
-            uint8_t *line = to.k + r * DIM * 2;
-            *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2) ^ (r % kPieces)) * 16) = attend_widen(k_item[i].x, k_item[i].y, k_scale[i]);
-            *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2 + 1) ^ (r % kPieces)) * 16) = attend_widen(k_item[i].z, k_item[i].w, k_scale[i]);
+            const uint32_t p = WIDE ? 0 : i, key = k_key + i * kKeysApart, x = key % 32, r = key / 32 * 32 + x / 4 % 4 * 8 + x / 16 * 4 + x % 4;
+            const uint32_t turned = r / (16 / kPieces) % kPieces;
+            uint8_t *line = key_space[turn] + r * DIM * 2;
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2) ^ turned) * 16) = attend_widen(k_item[i].x, k_item[i].y, k_scale[p]);
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((k_part * 2 + 1) ^ turned) * 16) = attend_widen(k_item[i].z, k_item[i].w, k_scale[p]);
+            if (!WIDE && k_part == 0 && key % 16 == 0)
+                reinterpret_cast<uint32_t *>(&there_space[turn])[key / 16] = k_there[p];
         }
-        if (attend_edge(range, k0) || __any(!v_there)) {
+        if (WIDE && threadIdx.x == 0)
+            there_space[turn] = make_uint4(k_there[0], k_there[0], k_there[0], k_there[0]);
+    };
+    uint32_t found = 0;  // NaN among values that not all rows see
+    const auto put_values = [&](uint32_t at, uint32_t turn) {
+        if (attend_edge(range, at * kAttendStep) || __any(!v_there)) {
             // values that not all rows see: those that none does, and NaN (0 * NaN is), are made 0; who sees NaN is looked up in the end
-            const uint32_t v0 = k0 + v_part * 16;
+            const uint32_t v0 = at * kAttendStep + v_part * 16;
             const int32_t from = v_there ? static_cast<int32_t>(range.low - v0) : 16, upto = v_there ? static_cast<int32_t>(range.high - v0) : 0;
 #pragma unroll
             for (uint32_t i = 0; i < kItems; ++i) {
@@ -663,96 +679,122 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         }
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
-            const uint32_t feature = v_feature + i * 64;
-            uint8_t *line = to.v + feature * kAttendStep * 2;
-            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2) ^ (feature % 8)) * 16) = attend_widen(v_item[i].x, v_item[i].y, v_scale);
-            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2 + 1) ^ (feature % 8)) * 16) = attend_widen(v_item[i].z, v_item[i].w, v_scale);
+            const uint32_t feature = v_feature + i * kFeaturesApart;
+            uint8_t *line = value_space[turn] + feature * kAttendStep * 2;
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2) ^ (feature / 2 % 8)) * 16) = attend_widen(v_item[i].x, v_item[i].y, v_scale);
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2 + 1) ^ (feature / 2 % 8)) * 16) = attend_widen(v_item[i].z, v_item[i].w, v_scale);
         }
-        const uint32_t parts = static_cast<uint32_t>(__ballot(v_there)) & 15u;
-        if (threadIdx.x == 0)
-            to.there = parts;
     };
 
     attend_f32x16_t o[DIM / 32] = {};
-    float top = -__builtin_inff(), total = 0.0f;
-    if (step < last) {
-        find_pages(step);
-        request(step);
-        find_pages(step + 1);
-        put(step, steps[0]);
-    }
-    const uint32_t begin = step;
-    for (uint32_t turn = 0; step < last; ++step, turn ^= 1) {
-        const AttendStep<DIM> &now = steps[turn];
-        __syncthreads();
-        const bool more = step + 1 < last;
-        if (more) {
-            request(step + 1);
-            find_pages(step + 2);
-        }
-        const uint32_t k0 = step * kAttendStep;
-        if (k0 < of_wave.high && k0 + kAttendStep > of_wave.low) {
-            attend_f32x16_t score[2] = {};
+    float top = -__builtin_inff(), total = 0.0f, most = 0.0f;
+    const auto products = [&](attend_f32x16_t (&score)[2], uint32_t turn) {
 #pragma unroll
-            for (uint32_t half = 0; half < 2; ++half)
+        for (uint32_t j = 0; j < DIM / 16; ++j)
 #pragma unroll
-                for (uint32_t j = 0; j < DIM / 16; ++j) {
-                    const attend_bf16x8_t keys = *reinterpret_cast<const attend_bf16x8_t *>(now.k + (half * 32 + c) * DIM * 2 + ((j * 2 + h) ^ (c % kPieces)) * 16);
-                    score[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys, q[j], score[half], 0, 0, 0);
-                }
-            const uint32_t there = __builtin_amdgcn_readfirstlane(now.there);
-            if (attend_edge(of_wave, k0) || there != 15u) {
-                asm volatile("");  // (a branch around it, not 130 instructions of every step)
-#pragma unroll
-                for (uint32_t half = 0; half < 2; ++half)
-#pragma unroll
-                    for (uint32_t e = 0; e < 16; ++e) {
-                        const uint32_t key = k0 + half * 32 + h * 16 + e;
-                        if (!(key >= my_low && key < my_high && (there >> (half * 2 + h) & 1u)))
-                            score[half][e] = -__builtin_inff();
-                    }
+            for (uint32_t half = 0; half < 2; ++half) {
+                const attend_bf16x8_t keys = *reinterpret_cast<const attend_bf16x8_t *>(key_space[turn] + (half * 32 + c) * DIM * 2 +
+                                                                                        ((j * 2 + h) ^ (c / (16 / kPieces) % kPieces)) * 16);
+                score[half] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys, q[j], j ? score[half] : attend_f32x16_t{}, 0, 0, 0);
             }
-            float most = -__builtin_inff();
-#pragma unroll
-            for (uint32_t half = 0; half < 2; ++half)
-#pragma unroll
-                for (uint32_t e = 0; e < 16; ++e)
-                    most = fmaxf(most, score[half][e]);
-            most = attend_max_of_halves(most) * a.scale;
-            if (__any(most > top + kAttendSlack)) {
-                const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
-                top = higher;
-                total *= less;
-#pragma unroll
-                for (uint32_t f = 0; f < DIM / 32; ++f)
-                    o[f] *= less;
-            }
-            const float base = top == -__builtin_inff() ? 0.0f : top;
+    };
+    // what the rows do not see, and their maxima
+    const auto look = [&](attend_f32x16_t (&score)[2], uint32_t at, uint32_t turn) {
+        const uint4 there = there_space[turn];
+        const uint32_t k0 = at * kAttendStep;
+        if (attend_edge(of_wave, k0) || __builtin_amdgcn_readfirstlane(there.x & there.y & there.z & there.w) == 0) {
+            asm volatile("");  // (a branch around it, not 130 instructions of every step)
+            const uint32_t have[2] = {h ? there.y : there.x, h ? there.w : there.z};
 #pragma unroll
             for (uint32_t half = 0; half < 2; ++half)
 #pragma unroll
                 for (uint32_t e = 0; e < 16; ++e) {
-                    score[half][e] = attend_exp2(score[half][e] * a.scale - base);
-                    total += score[half][e];
+                    const uint32_t key = k0 + half * 32 + h * 16 + e;
+                    if (!(key >= my_low && key < my_high && have[half]))
+                        score[half][e] = -__builtin_inff();
                 }
-            attend_bf16x8_t p[4];
-#pragma unroll
-            for (uint32_t u = 0; u < 4; ++u) {
-                const attend_f32x16_t &w = score[u / 2];
-                const uint32_t e = u % 2 * 8;
-                p[u] = attend_round(w[e], w[e + 1], w[e + 2], w[e + 3], w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
-            }
-            const auto values_of = [&](uint32_t f, uint32_t u) {
-                return *reinterpret_cast<const attend_bf16x8_t *>(now.v + (f * 32 + c) * kAttendStep * 2 + ((u / 2 * 4 + h * 2 + u % 2) ^ (c % 8)) * 16);
-            };
-#pragma unroll
-            for (uint32_t u = 0; u < 4; ++u)
-#pragma unroll
-                for (uint32_t f = 0; f < DIM / 32; ++f)
-                    o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values_of(f, u), p[u], o[f], 0, 0, 0);
         }
-        if (more)
-            put(step + 1, steps[turn ^ 1]);
+        most = -__builtin_inff();
+#pragma unroll
+        for (uint32_t half = 0; half < 2; ++half)
+#pragma unroll
+            for (uint32_t e = 0; e < 16; ++e)
+                most = fmaxf(most, score[half][e]);
+        most = attend_max_of_halves(most) * a.scale;
+    };
+    if (begin < last) {
+        find_key_pages(begin);
+        find_value_pages(begin);
+        request_keys(begin);
+        request_values(begin);
+        find_key_pages(begin + 1);
+        find_value_pages(begin + 1);
+        put_keys(0);
+        put_values(begin, 0);
+    }
+    uint32_t step = begin;
+    for (uint32_t turn = 0; step < last; ++step, turn ^= 1) {
+        __syncthreads();
+        if (step + 1 < last) {
+            request_keys(step + 1);
+            request_values(step + 1);
+            find_key_pages(step + 2);
+            find_value_pages(step + 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        attend_f32x16_t now[2];
+        products(now, turn);
+        // (six operands on their way from LDS before the first product, one more behind each)
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, 6, 0);
+#pragma unroll
+        for (uint32_t g = 0; g < DIM / 8 - 6; ++g) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 6, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        look(now, step, turn);
+        if (__any(most > top + kAttendSlack)) {
+            const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+            top = higher;
+            total *= less;
+#pragma unroll
+            for (uint32_t f = 0; f < DIM / 32; ++f)
+                o[f] *= less;
+        }
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+            attend_f32x16_t &w = now[u / 2];
+            const uint32_t e = u % 2 * 8;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                w[e + i] = attend_exp2(w[e + i] * a.scale - base);
+                total += w[e + i];
+            }
+            const attend_bf16x8_t p = attend_round(w[e], w[e + 1], w[e + 2], w[e + 3], w[e + 4], w[e + 5], w[e + 6], w[e + 7]);
+#pragma unroll
+            for (uint32_t f = 0; f < DIM / 32; ++f) {
+                const attend_bf16x8_t values = *reinterpret_cast<const attend_bf16x8_t *>(value_space[turn] + (f * 32 + c) * kAttendStep * 2 +
+                                                                                          ((u / 2 * 4 + h * 2 + u % 2) ^ (c / 2 % 8)) * 16);
+                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values, p, o[f], 0, 0, 0);
+            }
+        }
+        // (four operands before the exponentials; then the products, the remaining exponentials between them)
+        __builtin_amdgcn_sched_group_barrier(kSchedLds, 4, 1);
+        __builtin_amdgcn_sched_group_barrier(kSchedVector, 34, 1);
+#pragma unroll
+        for (uint32_t g = 0; g < DIM / 8 - 4; ++g) {
+            __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 1);
+            __builtin_amdgcn_sched_group_barrier(kSchedVector, 8, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 4, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (step + 1 < last) {
+            put_keys(turn ^ 1);
+            put_values(step + 1, turn ^ 1);
+        }
     }
     total += __shfl_xor(total, 32);
     if (__syncthreads_or(found != 0)) {

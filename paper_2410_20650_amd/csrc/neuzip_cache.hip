@@ -19,8 +19,8 @@ constexpr uint64_t kAttendMostRows = 1ull << 27;  // rows times query heads
 constexpr uint32_t kAttendCus = 256;
 constexpr uint32_t kAttendWaves = 2048;     // that a launch is split into, where its keys allow it: two to a SIMD
 constexpr uint32_t kAttendWaveSteps = 2;    // of each wave of a split at least, few rows
-constexpr uint64_t kAttendManyWgs = 512;
-constexpr uint32_t kAttendManySteps = 8;    // of a split at least, many rows
+constexpr uint64_t kAttendManyWgs = 390;
+constexpr uint32_t kAttendManySteps = 16;    // of a split at least, many rows
 constexpr uint32_t kAttendMostSplits = 128;
 
 inline bool off(const void *p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) & (size - 1); }
@@ -111,10 +111,13 @@ inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_head
 template <uint32_t DIM>
 int launch_attend(const AttendArgs &a, const AttendShape &shape, uint32_t wgs, hipStream_t stream)
 {
+    const bool wide = (1u << a.s.page_shift) >= kAttendStep;
     if (shape.rows == kAttendSomeRows)
         hipLaunchKernelGGL((attend_some_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    else if (shape.rows == kAttendManyRows && wide)
+        hipLaunchKernelGGL((attend_many_kernel<DIM, true>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
     else if (shape.rows == kAttendManyRows)
-        hipLaunchKernelGGL((attend_many_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+        hipLaunchKernelGGL((attend_many_kernel<DIM, false>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
     else if (shape.waves == 8)
         hipLaunchKernelGGL((attend_few_kernel<DIM, 8>), dim3(wgs), dim3(512), 0, stream, a);
     else
