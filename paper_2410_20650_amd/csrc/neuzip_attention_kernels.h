@@ -92,6 +92,8 @@ __device__ __forceinline__ uint32_t attend_clean(uint32_t &w, uint32_t keep)
     return nans;
 }
 
+constexpr uint32_t attend_shift(uint32_t rows) { return rows == 16 ? 4 : rows == 32 ? 5 : 7; }
+
 // Which keys the rows of a tile see.
 struct AttendRange {
     uint32_t low, high;          // any row: low .. high - 1
@@ -116,7 +118,7 @@ __device__ __forceinline__ bool attend_edge(const AttendRange &r, uint32_t k0) {
 
 // The steps begin .. end - 1 of split `split` of the steps that the keys of r take.  A split has as many steps in every sequence, the longest's
 // divided by the splits: workgroups of a ragged batch are then equally long, short sequences have fewer of them.
-__device__ __forceinline__ void attend_split(const AttendArgs &a, const AttendRange &r, uint32_t split, uint32_t &begin, uint32_t &end)
+__device__ __forceinline__ void attend_split(const AttendArgs &a, uint32_t longest, const AttendRange &r, uint32_t split, uint32_t &begin, uint32_t &end)
 {
     const uint32_t first = r.low / kAttendStep, last = (r.high + kAttendStep - 1) / kAttendStep;
     if (a.splits == 1) {
@@ -124,14 +126,7 @@ __device__ __forceinline__ void attend_split(const AttendArgs &a, const AttendRa
         end = last;
         return;
     }
-    int32_t longest = 0;
-    for (uint32_t s = threadIdx.x % 64; s < a.s.count; s += 64)
-        longest = max(longest, a.s.lengths[s]);
-#pragma unroll
-    for (int apart = 32; apart; apart >>= 1)
-        longest = max(longest, __shfl_xor(longest, apart));
-    uint32_t keys = static_cast<uint32_t>(longest);
-    keys = keys < a.most_keys ? keys : a.most_keys;
+    const uint32_t keys = longest < a.most_keys ? longest : a.most_keys;
     // (one step more: a window need not begin with a step.  At least so many that the splits hold all there are.)
     uint32_t each = ((keys + kAttendStep - 1) / kAttendStep + 1 + a.splits - 1) / a.splits;
     const uint32_t least = (last - first + a.splits - 1) / a.splits;
@@ -218,12 +213,12 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     __shared__ float2 stats[WAVES][kAttendFewRows];
     __shared__ attend_bf16x8_t queries[kWide * 2][64];
     const uint32_t split = blockIdx.x % a.splits, head = blockIdx.x / a.splits % a.c.heads, tile = blockIdx.x / a.splits / a.c.heads;
-    const TileNumbers numbers = {kAttendFewRows, a.group, 1};
-    const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
-    if (s >= a.s.count)
+    const Found at = find_sequence(a.s, {attend_shift(kAttendFewRows), a.group, 1}, tile, a.splits > 1);
+    if (at.s >= a.s.count)
         return;
-    const NewTokens n = new_tokens(a.s, s);
-    const uint64_t row0_wide = (tile - first_tile(numbers, a.s.starts[s], s)) * kAttendFewRows;
+    const uint32_t s = at.s;
+    const NewTokens n = at.n;
+    const uint64_t row0_wide = at.tile * kAttendFewRows;
     const uint32_t rows = n.count * a.group;
     if (row0_wide >= rows)
         return;
@@ -245,7 +240,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     attend_f32x4_t o[kFeatures] = {};
     float top = -__builtin_inff(), total = 0.0f;
     uint32_t step, last;
-    attend_split(a, range, split, step, last);
+    attend_split(a, at.longest, range, split, step, last);
     // Requests run ahead of the sums: the next step's pages are looked up a step before, its keys are asked for as soon as this step's are
     // used up, its values behind this step's second product.
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
@@ -401,12 +396,12 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     __shared__ float2 stats[WAVES][kAttendSomeRows];
     __shared__ attend_bf16x8_t queries[kWide * 2][64];
     const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
-    const TileNumbers numbers = {kAttendSomeRows, a.group, 1};
-    const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
-    if (s >= a.s.count)
+    const Found at = find_sequence(a.s, {attend_shift(kAttendSomeRows), a.group, 1}, tile, a.splits > 1);
+    if (at.s >= a.s.count)
         return;
-    const NewTokens n = new_tokens(a.s, s);
-    const uint64_t row0_wide = (tile - first_tile(numbers, a.s.starts[s], s)) * kAttendSomeRows;
+    const uint32_t s = at.s;
+    const NewTokens n = at.n;
+    const uint64_t row0_wide = at.tile * kAttendSomeRows;
     const uint32_t rows = n.count * a.group;
     if (row0_wide >= rows)
         return;
@@ -425,7 +420,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     attend_f32x16_t o[kWide] = {};
     float top = -__builtin_inff(), total = 0.0f;
     uint32_t step, last;
-    attend_split(a, range, split, step, last);
+    attend_split(a, at.longest, range, split, step, last);
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     const uint32_t k_row = c / 4 % 2 * 16 + c / 8 * 4 + c % 4;
     uint32_t k_page[2], v_page[2];
@@ -587,12 +582,12 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     __shared__ __align__(16) uint8_t value_space[2][kBytes];
     __shared__ uint4 there_space[2];  // of four times 16 keys: not 0 if they have a page
     const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
-    const TileNumbers numbers = {kAttendManyRows, a.group, 1};
-    const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
-    if (s >= a.s.count)
+    const Found at = find_sequence(a.s, {attend_shift(kAttendManyRows), a.group, 1}, tile, a.splits > 1);
+    if (at.s >= a.s.count)
         return;
-    const NewTokens n = new_tokens(a.s, s);
-    const uint64_t row0_wide = (tile - first_tile(numbers, a.s.starts[s], s)) * kAttendManyRows;
+    const uint32_t s = at.s;
+    const NewTokens n = at.n;
+    const uint64_t row0_wide = at.tile * kAttendManyRows;
     const uint32_t rows = n.count * a.group;
     if (row0_wide >= rows)
         return;
@@ -600,7 +595,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 32, h = lane / 32;
     const AttendRange range = attend_range(n, row0 / a.group, (row_end - 1) / a.group, a.window);
     uint32_t begin, last;
-    attend_split(a, range, split, begin, last);
+    attend_split(a, at.longest, range, split, begin, last);
 
     // the wave's rows, and the lane's
     const uint32_t wave0 = row0 + wave * 32 < row_end ? row0 + wave * 32 : row_end - 1, wave_end = wave0 + 32 < row_end ? wave0 + 32 : row_end;

@@ -86,7 +86,7 @@ AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint3
                  : all / kAttendManyRows * c->heads < kAttendManyWgs ? kAttendSomeRows
                                                                                                     : kAttendManyRows;
     const uint32_t tile = shape.rows;
-    shape.tiles = tile_count({tile, group, 1}, rows, s->count);
+    shape.tiles = tile_count({attend_shift(tile), group, 1}, rows, s->count);
     // workgroups that have something to do, about
     const uint64_t full = (all + tile - 1) / tile;
     const uint64_t wgs = (full > s->count ? full : s->count) * c->heads;
@@ -158,7 +158,7 @@ int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *seque
         return NEUZIP_EINVAL;
     if (d_q && (q_heads == 0 || !valid_rows(d_q, q_row, static_cast<uint64_t>(q_heads) * cache->head_dim, size) || off(d_q_out, 16)))
         return NEUZIP_EINVAL;
-    const TileNumbers numbers = {cache->page_tokens, 1, 2};
+    const TileNumbers numbers = {page_shift(cache), 1, 2};
     const uint64_t tiles = tile_count(numbers, rows, sequences->count);
     const uint64_t wgs = tiles * cache->heads * 2 + (d_q ? rows : 0);
     if (cache->heads >= (1u << 16) || too_many_wgs(wgs, kAppendThreads))

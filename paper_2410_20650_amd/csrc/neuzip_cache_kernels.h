@@ -35,22 +35,61 @@ struct AppendArgs {
     uint32_t tiles;  // workgroups: tiles * heads * 2, and behind them one for each row of q
 };
 
-// The last s in 0 .. count - 1 with first_tile(s) <= id (a wave works it out together); count if there is none.
-__device__ __forceinline__ uint32_t sequence_of(const int32_t *starts, uint32_t count, const TileNumbers &t, uint64_t id)
+// The sequence that a tile of number `id` is in.
+struct Found {
+    uint32_t s;          // the last in 0 .. count - 1 with first_tile(s) <= id; count if there is none
+    NewTokens n;
+    uint64_t tile;       // id, counted from the sequence's first
+    uint32_t longest;    // no sequence has more tokens
+};
+
+// A wave works it out together.  Up to 63 sequences are all read at once, so that what comes next waits for memory once.
+__device__ __forceinline__ Found find_sequence(const SequencesView &v, const TileNumbers &t, uint64_t id, bool with_longest)
 {
     const uint32_t lane = threadIdx.x % 64;
-    uint32_t base = 0, left = count;
-    while (left > 1) {
-        const uint32_t step = (left + 63) / 64, at = base + lane * step;
-        const bool before = lane * step < left && first_tile(t, starts[at], at) <= id;
-        const uint32_t last = __popcll(__ballot(before));
-        if (last == 0)
-            return count;
-        base += (last - 1) * step;
-        left -= (last - 1) * step;
-        left = left < step ? left : step;
+    Found f;
+    int32_t longest = 0;
+    if (v.count < 64) {
+        const uint32_t at = lane < v.count ? lane : v.count - 1;
+        const int32_t begin = v.starts[at], end = v.starts[at + 1], length = v.lengths[at];
+        const uint32_t before = __popcll(__ballot(lane < v.count && first_tile(t, begin, lane) <= id));
+        f.s = before ? before - 1 : v.count;
+        const uint32_t from = __builtin_amdgcn_readfirstlane(before ? before - 1 : 0);
+        f.n = new_tokens(v, __builtin_amdgcn_readlane(begin, from), __builtin_amdgcn_readlane(end, from), __builtin_amdgcn_readlane(length, from));
+        const uint64_t first = first_tile(t, __builtin_amdgcn_readlane(begin, from), from);
+        if (first > id)  // (starts that do not ascend)
+            f.s = v.count;
+        f.tile = id - first;
+        longest = length;
+    } else {
+        uint32_t base = 0, left = v.count;
+        while (left > 1) {
+            const uint32_t step = (left + 63) / 64, at = base + lane * step;
+            const bool before = lane * step < left && first_tile(t, v.starts[at], at) <= id;
+            const uint32_t last = __popcll(__ballot(before));
+            if (last == 0) {
+                f.s = v.count;
+                return f;
+            }
+            base += (last - 1) * step;
+            left -= (last - 1) * step;
+            left = left < step ? left : step;
+        }
+        f.n = new_tokens(v, base);
+        const uint64_t first = first_tile(t, v.starts[base], base);
+        f.s = first <= id ? base : v.count;
+        f.tile = id - first;
+        if (with_longest)
+            for (uint32_t s = lane; s < v.count; s += 64)
+                longest = max(longest, v.lengths[s]);
     }
-    return left && first_tile(t, starts[base], base) <= id ? base : count;
+    if (with_longest) {
+#pragma unroll
+        for (int apart = 32; apart; apart >>= 1)
+            longest = max(longest, __shfl_xor(longest, apart));
+        f.longest = longest > 0 ? static_cast<uint32_t>(longest) : 0;
+    }
+    return f;
 }
 
 __device__ __forceinline__ void append_load(const float *from, float (&v)[8])
@@ -111,10 +150,10 @@ __device__ __forceinline__ uint32_t append_again(uint32_t w, float ratio)
 template <class T>
 __device__ __forceinline__ void append_queries(const AppendArgs &a, uint32_t row, uint32_t dim)
 {
-    const uint32_t s = sequence_of(a.s.starts, a.s.count, {1, 1, 0}, row);
-    if (s >= a.s.count || static_cast<int64_t>(row) >= a.s.starts[s + 1])
+    const Found found = find_sequence(a.s, {0, 1, 0}, row, false);
+    const NewTokens n = found.n;
+    if (found.s >= a.s.count || found.tile >= n.count)
         return;  // behind the last sequence
-    const NewTokens n = new_tokens(a.s, s);
     const uint32_t half = dim / 2, pieces = half / 8;
     const T *q = static_cast<const T *>(a.q) + row * a.q_row;
     const float *angle = a.rotary ? a.rotary + static_cast<uint64_t>(n.first + (row - n.begin)) * dim : nullptr;
@@ -152,15 +191,15 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
     const uint32_t shift = a.s.page_shift, size = 1u << shift;
     const uint32_t tile = blockIdx.x / (a.c.heads * 2), head = blockIdx.x / 2 % a.c.heads;
     const bool values = blockIdx.x % 2;
-    const TileNumbers numbers = {size, 1, 2};
-    const uint32_t s = sequence_of(a.s.starts, a.s.count, numbers, tile);
-    if (s >= a.s.count)
+    const Found found = find_sequence(a.s, {shift, 1, 2}, tile, false);
+    if (found.s >= a.s.count)
         return;
-    const NewTokens n = new_tokens(a.s, s);
-    const uint32_t number = (n.first >> shift) + static_cast<uint32_t>(tile - first_tile(numbers, a.s.starts[s], s));
-    if (n.length == 0 || number > (n.length - 1) >> shift)
+    const NewTokens n = found.n;
+    const uint64_t number_wide = (n.first >> shift) + found.tile;
+    if (n.length == 0 || number_wide > (n.length - 1) >> shift)
         return;
-    const uint32_t page = page_of(a.s, s, number);
+    const uint32_t number = static_cast<uint32_t>(number_wide);
+    const uint32_t page = page_of(a.s, found.s, number);
     if (page == kNoPage)
         return;
     // the new tokens' places in the page: begin .. end - 1

@@ -27,9 +27,9 @@ struct NewTokens {
     uint32_t length;        // of the sequence, with them; 0: it is left out
 };
 
-NZ_BOTH NewTokens new_tokens(const SequencesView &v, uint32_t s)
+// begin, end, length: starts[s], starts[s + 1] and lengths[s]
+NZ_BOTH NewTokens new_tokens(const SequencesView &v, int32_t begin, int32_t end, int32_t length)
 {
-    const int32_t begin = v.starts[s], end = v.starts[s + 1], length = v.lengths[s];
     NewTokens t = {0, 0, 0, 0};
     if (begin < 0 || end <= begin || static_cast<uint32_t>(end) > v.rows)
         return t;
@@ -41,6 +41,7 @@ NZ_BOTH NewTokens new_tokens(const SequencesView &v, uint32_t s)
     t.first = t.length - t.count;
     return t;
 }
+NZ_BOTH NewTokens new_tokens(const SequencesView &v, uint32_t s) { return new_tokens(v, v.starts[s], v.starts[s + 1], v.lengths[s]); }
 
 constexpr uint32_t kNoPage = 0xFFFFFFFFu;
 
@@ -53,21 +54,21 @@ NZ_BOTH uint32_t page_of(const SequencesView &v, uint32_t s, uint32_t number)
     return page >= 0 && static_cast<uint32_t>(page) < v.pages ? static_cast<uint32_t>(page) : kNoPage;
 }
 
-// A call's work is cut into tiles that lie in one sequence each, up to `unit` rows (or rows times `group`) long; how many a sequence has is known
+// A call's work is cut into tiles that lie in one sequence each, up to 2^shift rows (or rows times `group`) long; how many a sequence has is known
 // on the device alone.  So each sequence gets a range of numbers that is sure to be long enough, from where the rows before it would end if they
-// lay in whole tiles, and `slack` more for each sequence; numbers that no tile takes have nothing to do.
-//   n rows in tiles of their own: ceil(n / unit) <= floor((a + n) / unit) - floor(a / unit) + 1, slack 1
-//   n tokens in pages, from anywhere in a page on: ceil(n / unit) + 1 at most, slack 2
+// lay in whole tiles, and `slack` more for each sequence; numbers that no tile takes have nothing to do.  With u = 2^shift:
+//   n rows in tiles of their own: ceil(n / u) <= floor((a + n) / u) - floor(a / u) + 1, slack 1
+//   n tokens in pages of u, from anywhere in a page on: ceil(n / u) + 1 at most, slack 2
 struct TileNumbers {
-    uint32_t unit, group, slack;
+    uint32_t shift, group, slack;
 };
 NZ_BOTH uint64_t first_tile(const TileNumbers &t, int32_t start, uint32_t s)
 {
-    return (start > 0 ? static_cast<uint64_t>(start) * t.group / t.unit : 0) + static_cast<uint64_t>(t.slack) * s;
+    return (start > 0 ? static_cast<uint64_t>(start) * t.group >> t.shift : 0) + static_cast<uint64_t>(t.slack) * s;
 }
 NZ_BOTH uint64_t tile_count(const TileNumbers &t, uint32_t rows, uint32_t count)
 {
-    return static_cast<uint64_t>(rows) * t.group / t.unit + static_cast<uint64_t>(t.slack) * count + (t.slack == 0);
+    return (static_cast<uint64_t>(rows) * t.group >> t.shift) + static_cast<uint64_t>(t.slack) * count + (t.slack == 0);
 }
 
 }  // namespace nz

@@ -75,7 +75,7 @@ int main()
             continue;
         // pages that tokens go to
         {
-            const TileNumbers t = {page, 1, 2};
+            const TileNumbers t = {shift, 1, 2};
             std::map<std::pair<uint32_t, uint32_t>, int> got;
             for (uint64_t id = 0; id < tile_count(t, rows, count); ++id) {
                 const uint32_t s = sequence_of(starts, count, t, id);
@@ -97,9 +97,9 @@ int main()
             require(got.size() == want, "no other pages");
         }
         // tiles of rows
-        for (uint32_t unit : {1u, 16u, 128u}) {
-            const uint32_t group = unit == 1 ? 1 : 1 + below(9);
-            const TileNumbers t = {unit, group, unit == 1 ? 0u : 1u};
+        for (uint32_t tile_shift : {0u, 4u, 5u, 7u}) {
+            const uint32_t unit = 1u << tile_shift, group = unit == 1 ? 1 : 1 + below(9);
+            const TileNumbers t = {tile_shift, group, unit == 1 ? 0u : 1u};
             std::map<std::pair<uint32_t, uint32_t>, int> got;
             for (uint64_t id = 0; id < tile_count(t, rows, count); ++id) {
                 const uint32_t s = sequence_of(starts, count, t, id);
