@@ -16,7 +16,7 @@ HEADERS = [os.path.join(ROOT, "include", "neuzip.h")] + [
     for name in ("neuzip_format.h", "neuzip_host.h", "neuzip_walk.h", "neuzip_compress_kernels.h", "neuzip_decode_kernels.h",
                  "neuzip_linear_kernels.h", "neuzip_linear_launch.h", "neuzip_embedding_kernels.h",
                  "neuzip_gated_shape.h", "neuzip_gated_kernels.h", "neuzip_adapters_kernels.h", "neuzip_norm_kernels.h",
-                 "neuzip_cache_kernels.h", "neuzip_attention_kernels.h", "neuzip_logits_kernels.h")]
+                 "neuzip_sequences.h", "neuzip_cache_kernels.h", "neuzip_attention_shape.h", "neuzip_attention_kernels.h", "neuzip_logits_kernels.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -16,13 +16,12 @@
 #include <hip/hip_runtime.h>
 #include <cstdint>
 
+#include "neuzip_attention_shape.h"
 #include "neuzip_cache_kernels.h"
 
 namespace nz {
 
 constexpr uint32_t kAttendThreads = 256;
-constexpr uint32_t kAttendFewRows = 16;
-constexpr uint32_t kAttendStep = 64;      // keys
 constexpr float kAttendSlack = 6.0f;      // a row's weights may exceed 1 by so much (a factor of 64) before its sums are scaled down to a new maximum
 
 struct AttendArgs {
@@ -91,8 +90,6 @@ __device__ __forceinline__ uint32_t attend_clean(uint32_t &w, uint32_t keep)
     w &= ~((nans >> 7) * 0xFFu);
     return nans;
 }
-
-constexpr uint32_t attend_shift(uint32_t rows) { return rows == 16 ? 4 : rows == 32 ? 5 : 7; }
 
 // Which keys the rows of a tile see.
 struct AttendRange {
@@ -386,7 +383,6 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
 
 // ---- some rows: the same with 32 rows to a workgroup, in matrix instructions of 32 x 32.  Here the lane (row c = l % 32, half h = l / 32) has of
 // every 32 keys the ones 16 h .. 16 h + 15; row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4.
-constexpr uint32_t kAttendSomeRows = 32;
 
 template <uint32_t DIM>
 __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const AttendArgs a)
@@ -568,7 +564,6 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 // 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD and half of it overlaps.  A prompt of 4096 tokens, 32
 // query heads on 8, takes 164 us, 835 TFLOP/s.  A wave with 64 rows halves what LDS reads, but fills 400 registers and is alone on its SIMD: 350 us; with the
 // next step's products beside this step's exponentials in the program 169 us: 256 registers leave none for operands on their way.
-constexpr uint32_t kAttendManyRows = 128;
 constexpr int kSchedVector = 0x2, kSchedMatrix = 0x8, kSchedLds = 0x100;  // kinds of instructions (sched_group_barrier)
 
 // WIDE: a step lies in one page

@@ -1,0 +1,65 @@
+// Which kernel a call of the attention takes, and into how many workgroups its work is cut.  (No device code in here: a host program can include it.)
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "neuzip_sequences.h"
+
+namespace nz {
+
+constexpr uint32_t kAttendFewRows = 16, kAttendSomeRows = 32, kAttendManyRows = 128;  // of a workgroup: a sequence's newest tokens times the query heads of a head
+constexpr uint32_t kAttendStep = 64;        // keys
+constexpr uint32_t kAttendCus = 256;
+constexpr uint32_t kAttendWaves = 2048;     // that a launch is split into, where its keys allow it: two to a SIMD
+constexpr uint32_t kAttendWaveSteps = 2;    // of each wave of a split at least, few and some rows
+constexpr uint32_t kAttendManySteps = 16;   // of a split at least, many rows
+constexpr uint32_t kAttendMostSplits = 128;
+
+constexpr uint32_t attend_shift(uint32_t rows) { return rows == 16 ? 4 : rows == 32 ? 5 : 7; }
+
+struct AttendShape {
+    uint32_t rows;   // to a workgroup
+    uint32_t waves;  // to a workgroup
+    uint64_t tiles;
+    uint32_t splits, keys, least_steps;
+    uint64_t sums, bytes;  // of scratch memory: the partial sums, and with the rows' statistics
+};
+
+// Whether tiles of 128 rows, `tiles` of them with all heads, are taken rather than tiles of 32: a step costs less there and takes longer, so there
+// has to be enough work to fill the CUs.  us, tiles of 32 / 128: head_dim 128, 8 heads, prompts of 1024 tokens (256 tiles of up to 16 steps) 33 / 40, 2 of
+// 1024 46 / 42, 8 of 512 65 / 46, 512 tokens behind 7680 (128 tiles of 128 steps) 118 / 95, 16 parts of 64 behind 2000 99 / 105; head_dim 64, 2048
+// tokens (512 tiles) 44 / 54, 8 of 512 (822) 38 / 28, 4096 (1024) 129 / 107, 16 parts of 64 (402) 54 / 75.
+inline bool attend_is_large(uint32_t head_dim, uint64_t tiles, uint64_t steps) { return head_dim == 128 ? tiles * steps >= 4608 : tiles >= 700; }
+
+// heads: of the cache; count: sequences; longest: no sequence has more tokens
+inline AttendShape attend_shape(uint32_t heads, uint32_t head_dim, uint32_t count, uint32_t q_heads, uint32_t rows, uint32_t window, uint64_t longest)
+{
+    const uint32_t group = q_heads / heads;
+    AttendShape shape;
+    const uint64_t all = static_cast<uint64_t>(rows) * group;
+    // the keys that a tile's rows see, at most
+    const uint64_t span = static_cast<uint64_t>(window) + kAttendManyRows / group + 1;
+    const uint64_t keys = window && span < longest ? span : longest;
+    shape.rows = all <= static_cast<uint64_t>(count) * kAttendFewRows                                                            ? kAttendFewRows
+                 : attend_is_large(head_dim, all / kAttendManyRows * heads, keys / kAttendStep) ? kAttendManyRows
+                                                                                                      : kAttendSomeRows;
+    const uint32_t tile = shape.rows;
+    shape.tiles = tile_count({attend_shift(tile), group, 1}, rows, count);
+    // workgroups that have something to do, about
+    const uint64_t full = (all + tile - 1) / tile;
+    const uint64_t wgs = (full > count ? full : count) * heads;
+    shape.waves = tile == kAttendFewRows && wgs <= kAttendCus ? 8 : 4;
+    shape.least_steps = tile == kAttendManyRows ? kAttendManySteps : kAttendWaveSteps * shape.waves;
+    const uint64_t wanted = (kAttendWaves + wgs * shape.waves - 1) / (wgs * shape.waves), most = keys / (kAttendStep * shape.least_steps);
+    uint64_t splits = wanted < most ? wanted : most;
+    splits = splits < kAttendMostSplits ? splits : kAttendMostSplits;
+    shape.splits = splits ? static_cast<uint32_t>(splits) : 1;
+    shape.keys = static_cast<uint32_t>(keys);
+    const uint64_t parts = shape.splits > 1 ? static_cast<uint64_t>(shape.splits) * rows * q_heads : 0;
+    shape.sums = (parts * head_dim * sizeof(float) + 255) / 256 * 256;
+    shape.bytes = shape.sums + parts * 2 * sizeof(float);
+    return shape;
+}
+
+}  // namespace nz

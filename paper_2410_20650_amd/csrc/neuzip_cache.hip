@@ -8,6 +8,7 @@
 #include "neuzip.h"
 
 #include "neuzip_attention_kernels.h"
+#include "neuzip_attention_shape.h"
 #include "neuzip_cache_kernels.h"
 #include "neuzip_host.h"
 
@@ -16,12 +17,6 @@ using namespace nz;
 namespace {
 
 constexpr uint64_t kAttendMostRows = 1ull << 27;  // rows times query heads
-constexpr uint32_t kAttendCus = 256;
-constexpr uint32_t kAttendWaves = 2048;     // that a launch is split into, where its keys allow it: two to a SIMD
-constexpr uint32_t kAttendWaveSteps = 2;    // of each wave of a split at least, few rows
-constexpr uint64_t kAttendManyWgs = 390;
-constexpr uint32_t kAttendManySteps = 16;    // of a split at least, many rows
-constexpr uint32_t kAttendMostSplits = 128;
 
 inline bool off(const void *p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) & (size - 1); }
 
@@ -65,45 +60,10 @@ void launch_append(const AppendArgs &a, uint32_t wgs, hipStream_t stream)
         hipLaunchKernelGGL((append_kernel<T, DIM, 4>), dim3(wgs), dim3(kAppendThreads), 0, stream, a);
 }
 
-struct AttendShape {
-    uint32_t rows;   // to a workgroup
-    uint32_t waves;  // to a workgroup
-    uint64_t tiles;
-    uint32_t splits, keys, least_steps;
-    uint64_t sums, bytes;  // of scratch memory: the partial sums, and with the rows' statistics
-};
-
-AttendShape attend_shape(const neuzip_cache *c, const neuzip_sequences *s, uint32_t q_heads, uint32_t rows, uint32_t window, uint64_t longest)
+inline AttendShape shape_of(const neuzip_cache *c, const neuzip_sequences *s, uint32_t q_heads, uint32_t rows, uint32_t window, uint64_t longest)
 {
     const uint64_t room = static_cast<uint64_t>(s->table_width) << page_shift(c);
-    if (longest == 0 || longest > room)
-        longest = room;
-    const uint32_t group = q_heads / c->heads;
-    AttendShape shape;
-    // rows to a workgroup: as many as a sequence has, about; 128 only where that leaves enough workgroups
-    const uint64_t all = static_cast<uint64_t>(rows) * group;
-    shape.rows = all <= static_cast<uint64_t>(s->count) * kAttendFewRows                                ? kAttendFewRows
-                 : all / kAttendManyRows * c->heads < kAttendManyWgs ? kAttendSomeRows
-                                                                                                    : kAttendManyRows;
-    const uint32_t tile = shape.rows;
-    shape.tiles = tile_count({attend_shift(tile), group, 1}, rows, s->count);
-    // workgroups that have something to do, about
-    const uint64_t full = (all + tile - 1) / tile;
-    const uint64_t wgs = (full > s->count ? full : s->count) * c->heads;
-    shape.waves = tile == kAttendFewRows && wgs <= kAttendCus ? 8 : 4;
-    // the keys that a tile's rows see, at most
-    const uint64_t span = static_cast<uint64_t>(window) + tile / group + 1;
-    const uint64_t keys = window && span < longest ? span : longest;
-    shape.least_steps = tile == kAttendManyRows ? kAttendManySteps : kAttendWaveSteps * shape.waves;
-    const uint64_t wanted = (kAttendWaves + wgs * shape.waves - 1) / (wgs * shape.waves), most = keys / (kAttendStep * shape.least_steps);
-    uint64_t splits = wanted < most ? wanted : most;
-    splits = splits < kAttendMostSplits ? splits : kAttendMostSplits;
-    shape.splits = splits ? static_cast<uint32_t>(splits) : 1;
-    shape.keys = static_cast<uint32_t>(keys);
-    const uint64_t parts = shape.splits > 1 ? static_cast<uint64_t>(shape.splits) * rows * q_heads : 0;
-    shape.sums = pad_to(parts * c->head_dim * sizeof(float), 256);
-    shape.bytes = shape.sums + parts * sizeof(float2);
-    return shape;
+    return attend_shape(c->heads, c->head_dim, s->count, q_heads, rows, window, longest && longest < room ? longest : room);
 }
 
 inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_heads > 0 && q_heads % c->heads == 0; }
@@ -198,7 +158,7 @@ uint64_t neuzip_cache_attention_scratch_bytes(const neuzip_cache *cache, const n
     if (!valid_cache(cache) || !valid_sequences(cache, sequences) || !valid_heads(cache, q_heads) || rows == 0 || sequences->count == 0 ||
         static_cast<uint64_t>(rows) * q_heads >= kAttendMostRows)
         return 0;
-    return attend_shape(cache, sequences, q_heads, rows, window, longest).bytes;
+    return shape_of(cache, sequences, q_heads, rows, window, longest).bytes;
 }
 
 int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *sequences, const void *d_q, uint64_t q_row, uint32_t q_heads,
@@ -213,7 +173,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
         return NEUZIP_EINVAL;
     if (static_cast<uint64_t>(rows) * q_heads >= kAttendMostRows)
         return NEUZIP_EUNSUPPORTED;
-    const AttendShape shape = attend_shape(cache, sequences, q_heads, rows, window, longest);
+    const AttendShape shape = shape_of(cache, sequences, q_heads, rows, window, longest);
     if (shape.bytes && (!d_scratch || scratch_bytes < shape.bytes))
         return NEUZIP_EINVAL;
     const uint64_t wgs = shape.tiles * cache->heads * shape.splits;
