@@ -108,9 +108,7 @@ def test_form_with_pages_that_are_not_there_and_nan(nz, case):
     sequences = nz.Sequences(ints(starts), ints(lengths), ints(table))
     n, length = starts[1], lengths[0]
     gone = max(0, (length - n - (20 if window else page + 20)) // page)
-    wanted = table[0][gone]
     low, high = gone * page, min((gone + 1) * page, length)
-    # the same with the page's keys made so that nobody takes them: all scores there are far below the others'
     hole = [row[:] for row in table]
     hole[0][gone] = -1 if gone % 2 else 1 << 28
     got = nz.neuzip_cache_attention(cache, nz.Sequences(ints(starts), ints(lengths), ints(hole)), q, window=window)
@@ -126,7 +124,6 @@ def test_form_with_pages_that_are_not_there_and_nan(nz, case):
         bound = (2.0 ** -8 + (2 * (dim + 8) * spread + length / 16 + 300) * 2.0 ** -24) * (p @ v.abs()) * (1 + 2.0 ** -7) + 2.0 ** -8 * (p @ v).abs() + 1e-30
         off = (got[:n, h * group].double() - p @ v).abs() - bound
         assert not bool(torch.isnan(off).any()) and bool((off <= 0).all()), float(off.max())
-    del wanted
     before = nz.neuzip_cache_attention(cache, sequences, q, window=window)
     poisoned, feature, head = length - (n + 1) // 2, dim - 3, heads - 1
     cache.v.view(torch.uint8)[table[0][poisoned // page], head, feature, poisoned % page] = 0x7F
