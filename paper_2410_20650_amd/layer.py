@@ -145,6 +145,58 @@ class AdaptedLinear:
                                          ids, base.bias)
 
 
+class ResidualNorm:
+    """What stands between two layers: stream <- stream + x, y = stream / rms(stream) * weight.  The weight is not compressed: float32, as the biases."""
+
+    def __init__(self, weight: torch.Tensor, eps: float = 1e-5):
+        self.weight, self.eps = weight.to(torch.float32).contiguous(), float(eps)
+
+    def forward(self, x: torch.Tensor, stream: torch.Tensor = None):
+        """x: a layer's result (bf16 or float32) and the stream it is added to, in whose type the sum is held; without a stream x is the stream.
+        Returns (y, stream), y in bf16."""
+        if stream is None:
+            return nz.neuzip_norm(x.contiguous(), self.weight, self.eps), x
+        return nz.neuzip_norm(x.contiguous(), self.weight, self.eps, stream.contiguous())
+
+    def backward_and_update(self, stream: torch.Tensor, grad_y: torch.Tensor, grad_stream: torch.Tensor, lr: float):
+        """The norm's part of the backward loop.  stream: as forward returned it; grad_stream: the gradient that comes back along it (bf16), or None.
+        Returns the gradient of the stream before and of x, which is one (bf16); the weight has made its step."""
+        if grad_stream is not None:
+            grad_stream = grad_stream.contiguous()
+        grad_x, grad_weight = nz.neuzip_norm_backward(stream.contiguous(), self.weight, grad_y.contiguous(), self.eps, grad_stream)
+        self.weight.sub_(grad_weight, alpha=float(lr))
+        return grad_x
+
+
+class CompressedAttention:
+    """The attention block of a served model: the projections to queries, keys and values and back, all four stored as lossless blobs, around a cache that
+    holds the keys and values of the tokens so far in 8 bits."""
+
+    def __init__(self, w_q: torch.Tensor, w_k: torch.Tensor, w_v: torch.Tensor, w_o: torch.Tensor, head_dim: int, rotary: torch.Tensor = None,
+                 window: int = 0, guard: int = 8):
+        self.queries, self.keys, self.values, self.out = (CompressedLinear(w, guard=guard) for w in (w_q, w_k, w_v, w_o))
+        self.head_dim, self.heads, self.window = head_dim, w_k.shape[0] // head_dim, int(window)
+        if (w_k.shape != w_v.shape or w_q.shape[1] != w_k.shape[1] or w_k.shape[0] % head_dim or self.heads == 0 or w_q.shape[0] % w_k.shape[0]
+                or w_o.shape[1] != w_q.shape[0]):
+            raise ValueError("projections to query heads, as many or several to each head of the keys and values, and back")
+        self.rotary = None if rotary is None else rotary.to(torch.float32).contiguous()
+
+    def new_cache(self, pages: int, page_tokens: int = 64, device="cuda") -> nz.KeyValueCache:
+        return nz.KeyValueCache.empty(pages, self.heads, self.head_dim, page_tokens, device)
+
+    def forward(self, x: torch.Tensor, cache: nz.KeyValueCache, sequences: nz.Sequences, space: torch.Tensor, longest: int = 0) -> torch.Tensor:
+        """x: rows x in_features, bf16, the newest tokens of the sequences, whose lengths count them already.  They are put into the cache and look back at
+        it.  Returns float32 rows x out_features."""
+        parts = (self.queries, self.keys, self.values)
+        if x.shape[0] <= 64 and self.queries.in_features % 128 == 0:     # (one launch for the three)
+            q, k, v = nz.neuzip_linear_batch([p.blob for p in parts], [p.out_features for p in parts], self.queries.in_features, x.contiguous())
+        else:
+            q, k, v = (p.forward(x, space) for p in parts)
+        turned = nz.neuzip_cache_append(cache, sequences, k, v, q, self.rotary)
+        seen = nz.neuzip_cache_attention(cache, sequences, turned, window=self.window, longest=longest)
+        return self.out.forward(seen.view(x.shape[0], -1), space)
+
+
 def training_step(layers, x: torch.Tensor, target: torch.Tensor, lr: float, space: torch.Tensor,
                   grad_space: torch.Tensor, observer=None):
     """One step of Alg. 1 on a stack of CompressedLinear layers with ReLU between them and a squared

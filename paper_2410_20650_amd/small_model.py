@@ -1,9 +1,10 @@
 """A small model whose weights are all held compressed: an embedding, a gated feed-forward block with its projection back, and an
 output projection.  Trained layer by layer as Alg. 1 has it, then served token by token with the adapters of several requests.
 
-    python -m paper_2410_20650_amd.small_model [--steps 8] [--tokens 512]
+    python -m paper_2410_20650_amd.small_model [--steps 8] [--tokens 512] [--norm] [--answer 16]
 
-prints the loss of every step, what the weights take, and how the served outputs differ from the trained model's.
+prints the loss of every step, what the weights take, and how the served outputs differ from the trained model's.  --norm: with a norm in front of the
+block.  --answer: lets a small decoder, whose attention looks back at a cache of 8-bit keys and values, answer a few prompts with so many tokens.
 """
 import argparse
 
@@ -11,13 +12,13 @@ import torch
 
 from . import binding as nz
 from . import inputs
-from .layer import AdaptedLinear, CompressedEmbedding, CompressedGatedBlock, CompressedLinear
+from .layer import AdaptedLinear, CompressedAttention, CompressedEmbedding, CompressedGatedBlock, CompressedLinear, ResidualNorm
 
 
 class SmallModel:
-    """y = W_out (h + W_down (act(W_gate h) * W_up h)) with h = scale * embedding[token]."""
+    """y = W_out (h + W_down (act(W_gate n) * W_up n)) with h = scale * embedding[token], n = h or, with a norm, h / rms(h) * weight."""
 
-    def __init__(self, rows=2000, width=256, hidden=640, classes=128, activation=nz.SILU, seed=1, device="cuda:0"):
+    def __init__(self, rows=2000, width=256, hidden=640, classes=128, activation=nz.SILU, seed=1, device="cuda:0", norm=False):
         def weight(shape, tag, std):
             return inputs.gaussian_bf16(shape, seed * 100 + tag, std=std, device=device)
 
@@ -25,6 +26,7 @@ class SmallModel:
         self.block = CompressedGatedBlock(weight((hidden, width), 1, width ** -0.5), weight((hidden, width), 2, width ** -0.5), activation)
         self.down = CompressedLinear(weight((width, hidden), 3, hidden ** -0.5))
         self.out = CompressedLinear(weight((classes, width), 4, width ** -0.5))
+        self.norm = ResidualNorm(torch.ones(width, device=device)) if norm else None
         most = max(rows * width, 2 * ((hidden * width + 7) // 8 * 8), classes * width)
         # one temporary space for whatever weight is in use, and one for its gradient
         self.space = torch.zeros(most, dtype=torch.bfloat16, device=device)
@@ -33,10 +35,13 @@ class SmallModel:
     def blobs(self):
         return [self.embedding.blob, *self.block.blobs, self.down.blob, self.out.blob]
 
+    def _block_input(self, h):
+        return h if self.norm is None else self.norm.forward(h)[0]
+
     def forward(self, tokens):
         """Returns (y, the inputs of the layers)."""
         h = self.embedding.forward(tokens)
-        gated = self.block.forward(h, self.space)
+        gated = self.block.forward(self._block_input(h), self.space)
         mixed = (h.float() + self.down.forward(gated, self.space)).to(torch.bfloat16)
         return self.out.forward(mixed, self.space), (h, gated, mixed)
 
@@ -49,24 +54,102 @@ class SmallModel:
         grad = (diff / tokens.numel()).to(torch.bfloat16)
         grad, _ = self.out.backward_and_update(mixed, grad, lr, self.space, self.grad_space)
         grad_gated, _ = self.down.backward_and_update(gated, grad.contiguous(), lr, self.space, self.grad_space)
-        grad_h, _ = self.block.backward_and_update(h, grad_gated, lr, self.space, self.grad_space)
-        self.embedding.backward_and_update(tokens, (grad.float() + grad_h.float()).to(torch.bfloat16), lr, self.space, self.grad_space)
+        grad_h, _ = self.block.backward_and_update(self._block_input(h), grad_gated, lr, self.space, self.grad_space)
+        if self.norm is None:
+            grad_h = (grad.float() + grad_h.float()).to(torch.bfloat16)
+        else:       # (what goes round the block is added on the way)
+            grad_h = self.norm.backward_and_update(h, grad_h, grad, lr)
+        self.embedding.backward_and_update(tokens, grad_h, lr, self.space, self.grad_space)
         return loss
 
     def serve(self, tokens, adapted: AdaptedLinear, ids):
         """The outputs of single tokens of many requests, the output projection with each request's adapter."""
         h = self.embedding.forward(tokens)
-        mixed = (h.float() + self.down.forward(self.block.forward(h, self.space), self.space)).to(torch.bfloat16)
+        mixed = (h.float() + self.down.forward(self.block.forward(self._block_input(h), self.space), self.space)).to(torch.bfloat16)
         return adapted.forward(mixed, ids)
+
+
+class SmallDecoder:
+    """A decoder of compressed weights: an embedding, layers of attention and gated block with a norm in front of each, a norm, and an output projection."""
+
+    def __init__(self, rows=1000, width=256, hidden=640, layers=2, heads=2, group=2, head_dim=64, positions=1024, window=0, seed=5, device="cuda:0"):
+        def weight(shape, tag, std):
+            return inputs.gaussian_bf16(shape, seed * 100 + tag, std=std, device=device)
+
+        def norm():
+            return ResidualNorm(torch.ones(width, device=device))
+
+        angle = torch.arange(positions, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, head_dim, 2, dtype=torch.float64) / head_dim)
+        rotary = torch.cat([angle.cos(), angle.sin()], dim=1).float().to(device)
+        self.rows, self.positions, self.device = rows, positions, device
+        self.embedding = CompressedEmbedding(weight((rows, width), 0, 1.0))
+        self.layers = []
+        for i in range(layers):
+            at, back = 10 * (i + 1), width ** -0.5
+            attention = CompressedAttention(weight((heads * group * head_dim, width), at, back), weight((heads * head_dim, width), at + 1, back),
+                                            weight((heads * head_dim, width), at + 2, back),
+                                            weight((width, heads * group * head_dim), at + 3, (heads * group * head_dim) ** -0.5), head_dim, rotary, window)
+            block = CompressedGatedBlock(weight((hidden, width), at + 4, back), weight((hidden, width), at + 5, back))
+            self.layers.append((norm(), attention, norm(), block, CompressedLinear(weight((width, hidden), at + 6, hidden ** -0.5))))
+        self.norm, self.out = norm(), CompressedLinear(weight((rows, width), 1, width ** -0.5))
+        most = max(rows * width, heads * group * head_dim * width, 2 * ((hidden * width + 7) // 8 * 8))
+        self.space = torch.zeros(most, dtype=torch.bfloat16, device=device)
+
+    def caches(self, pages, page_tokens=64):
+        return [attention.new_cache(pages, page_tokens, self.device) for _, attention, _, _, _ in self.layers]
+
+    def forward(self, tokens, caches, sequences, longest=0):
+        """tokens: the newest of the sequences (int64).  Returns their logits, float32 tokens x rows."""
+        x, stream = self.embedding.forward(tokens), None
+        for (before, attention, between, block, down), cache in zip(self.layers, caches):
+            y, stream = before.forward(x, stream)
+            y, stream = between.forward(attention.forward(y, cache, sequences, self.space, longest), stream)
+            x = down.forward(block.forward(y, self.space), self.space)
+        y, _ = self.norm.forward(x, stream)
+        return self.out.forward(y, self.space)
+
+    def answer(self, prompts, steps, presence=0.5, bias=None, allowed=None, page_tokens=64):
+        """The likeliest token after each prompt (a list of int64 tensors), `steps` times over; returns sequences x steps.  presence: what a token that the answer
+        has already is penalised by.  bias: (tokens, values) for every sequence.  allowed: a mask of ceil(rows / 32) words (int32) that all obey."""
+        count, device = len(prompts), self.device
+        lengths = [p.numel() for p in prompts]
+        pages = (max(lengths) + steps + page_tokens - 1) // page_tokens
+        if pages * page_tokens > self.positions:
+            raise ValueError("prompts and answers need more positions than there are angles for")
+        caches = self.caches(count * pages, page_tokens)
+        table = torch.arange(count * pages, dtype=torch.int32, device=device).view(count, pages)
+        starts = torch.tensor([0] + lengths).cumsum(0).to(torch.int32).to(device)
+        held = torch.tensor(lengths, dtype=torch.int32, device=device)
+        penalty = torch.full((count,), float(presence), device=device)
+        masks = mask_ids = named = values = named_starts = None
+        if allowed is not None:
+            masks, mask_ids = allowed.view(1, -1), torch.zeros(count, dtype=torch.int32, device=device)
+        if bias is not None:
+            named, values = bias[0].repeat(count), bias[1].repeat(count)
+            named_starts = torch.arange(count + 1, dtype=torch.int32, device=device) * bias[0].numel()
+        logits = self.forward(torch.cat(prompts), caches, nz.Sequences(starts, held, table))[starts[1:].long() - 1]
+        answers = torch.empty((count, steps), dtype=torch.int64, device=device)
+        singles = nz.Sequences(torch.arange(count + 1, dtype=torch.int32, device=device), held, table)
+        for step in range(steps):
+            history_starts = torch.arange(count + 1, dtype=torch.int32, device=device) * step
+            logits = nz.neuzip_logits(logits.contiguous(), answers[:, :step].contiguous().view(-1), history_starts, presence=penalty, bias=named,
+                                      bias_values=values, bias_starts=named_starts, masks=masks, mask_ids=mask_ids)
+            answers[:, step] = logits.argmax(dim=1)
+            if step + 1 < steps:
+                held += 1
+                logits = self.forward(answers[:, step].contiguous(), caches, singles)
+        return answers
 
 
 def main(argv=None):
     parser = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     parser.add_argument("--steps", type=int, default=8)
     parser.add_argument("--tokens", type=int, default=512)
+    parser.add_argument("--norm", action="store_true")
+    parser.add_argument("--answer", type=int, default=0)
     args = parser.parse_args(argv)
     device = "cuda:0"
-    model = SmallModel(device=device)
+    model = SmallModel(device=device, norm=args.norm)
     generator = torch.Generator(device=device)
     generator.manual_seed(7)
     tokens = torch.randint(0, model.embedding.rows, (args.tokens,), generator=generator, device=device)
@@ -90,6 +173,11 @@ def main(argv=None):
           f"the others by {float(apart[ids >= 0].mean()):.3f} on average", flush=True)
     for blob in model.blobs():
         nz.neuzip_check(blob)
+    if args.answer:
+        decoder = SmallDecoder(device=device)
+        prompts = [tokens[:5] % decoder.rows, tokens[5:75] % decoder.rows, tokens[75:76] % decoder.rows]
+        for prompt, answer in zip(prompts, decoder.answer(prompts, args.answer)):
+            print(f"answer to {prompt.numel()} tokens: {answer.tolist()}", flush=True)
     return losses
 
 
