@@ -736,7 +736,7 @@ def neuzip_linear_adapters(weight: Blob, out_features: int, in_features: int, x:
 
 def _here(t, dtype, shape, what, device):
     """_expect of a tensor on the current device, where the call's kernels run.  (Most are as they should be: one look at each thing.)"""
-    if not (t.shape == shape and t.dtype == dtype and t.get_device() == device and t.is_contiguous()):
+    if not (t.dtype is dtype and t.shape == shape and t.get_device() == device and t.is_contiguous()):
         _expect(t, dtype, shape, what)
         if t.get_device() != device:
             raise ValueError(f"{what} must be on the current device, cuda:{device}")
@@ -744,6 +744,8 @@ def _here(t, dtype, shape, what, device):
 
 
 def _scratch_here(size, scratch, t, device, stream):
+    if size == 0 and scratch is None:
+        return None
     scratch = _own_scratch(size, scratch, t.device, stream)
     if scratch is not None and scratch.get_device() != device:
         raise ValueError(f"scratch memory must be on the current device, cuda:{device}")
@@ -981,19 +983,6 @@ def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.
     return out
 
 
-def _entries(tokens, starts, rows, what, device):
-    if tokens is None:
-        if starts is not None:
-            raise ValueError(f"{what} and its starts come together")
-        return 0
-    count = tokens.numel()
-    _here(tokens, torch.int64, (count,), what, device)
-    if starts is None:
-        raise ValueError(f"{what} and its starts come together")
-    _here(starts, torch.int32, (rows + 1,), what + "_starts", device)
-    return count
-
-
 def neuzip_logits(logits: torch.Tensor, history: torch.Tensor = None, history_starts: torch.Tensor = None, repetition: torch.Tensor = None,
                   frequency: torch.Tensor = None, presence: torch.Tensor = None, bias: torch.Tensor = None, bias_values: torch.Tensor = None,
                   bias_starts: torch.Tensor = None, masks: torch.Tensor = None, mask_ids: torch.Tensor = None, out: torch.Tensor = None,
@@ -1006,32 +995,32 @@ def neuzip_logits(logits: torch.Tensor, history: torch.Tensor = None, history_st
     if logits.dim() != 2:
         raise ValueError("logits must be rows x vocab")
     rows, vocab = logits.shape
-    _here(logits, torch.float32, (rows, vocab), "logits", device)
-    history_tokens = _entries(history, history_starts, rows, "history", device)
-    entries = _entries(bias, bias_starts, rows, "bias", device)
-    if (bias is None) != (bias_values is None):
-        raise ValueError("bias and bias_values come together")
-    if bias_values is not None:
-        _here(bias_values, torch.float32, (entries,), "bias_values", device)
-    for t, what in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence")):
-        if t is not None:
-            _here(t, torch.float32, (rows,), what, device)
-    count = 0
+    if (history is None) != (history_starts is None) or not (bias is None) == (bias_values is None) == (bias_starts is None):
+        raise ValueError("tokens come with their starts, biases with their values")
     if (masks is None) != (mask_ids is None):
         raise ValueError("masks and mask_ids come together")
-    if masks is not None:
-        count = masks.shape[0] if masks.dim() else 0
-        _here(masks, torch.int32, (count, (vocab + 31) // 32), "masks", device)
-        _here(mask_ids, torch.int32, (rows,), "mask_ids", device)
-        if count == 0:
-            masks = mask_ids = None
+    history_tokens = history.numel() if history is not None else 0
+    entries = bias.numel() if bias is not None else 0
+    count = masks.shape[0] if masks is not None and masks.dim() else 0
     if out is None:
         out = _empty_like(logits, torch.float32, stream)
-    elif out is not logits:
-        _here(out, torch.float32, (rows, vocab), "out", device)
-    rc = _lib.neuzip_logits(logits.data_ptr(), rows, vocab, _pointer(history), history_tokens, _pointer(history_starts), _pointer(repetition),
-                            _pointer(frequency), _pointer(presence), _pointer(bias), _pointer(bias_values), entries, _pointer(bias_starts),
-                            _pointer(masks), count, _pointer(mask_ids), out.data_ptr(), _stream_handle(stream, device))
+    f32, i32, i64, one, behind = torch.float32, torch.int32, torch.int64, (rows,), (rows + 1,)
+    pointers = []
+    for t, dtype, shape, what in ((logits, f32, (rows, vocab), "logits"), (history, i64, (history_tokens,), "history"),
+                                  (history_starts, i32, behind, "history_starts"), (repetition, f32, one, "repetition"), (frequency, f32, one, "frequency"),
+                                  (presence, f32, one, "presence"), (bias, i64, (entries,), "bias"), (bias_values, f32, (entries,), "bias_values"),
+                                  (bias_starts, i32, behind, "bias_starts"), (masks, i32, (count, (vocab + 31) // 32), "masks"), (mask_ids, i32, one, "mask_ids"),
+                                  (out, f32, (rows, vocab), "out")):
+        if t is None:
+            pointers.append(None)
+        else:
+            _here(t, dtype, shape, what, device)
+            pointers.append(t.data_ptr())
+    x, history, history_starts, repetition, frequency, presence, bias, bias_values, bias_starts, masks, mask_ids, y = pointers
+    if count == 0:
+        masks = mask_ids = None
+    rc = _lib.neuzip_logits(x, rows, vocab, history, history_tokens, history_starts, repetition, frequency, presence, bias, bias_values, entries,
+                            bias_starts, masks, count, mask_ids, y, _stream_handle(stream, device))
     if rc != OK:
         raise NeuzipError(rc, "neuzip_logits")
     return out
