@@ -202,7 +202,8 @@ __device__ __forceinline__ attend_f32x16_t attend_nans(const AttendArgs &a, uint
     return seen;
 }
 
-template <uint32_t DIM, uint32_t WAVES>
+// WIDE: a step lies in one page
+template <uint32_t DIM, uint32_t WAVES, bool WIDE>
 __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendArgs a)
 {
     constexpr uint32_t kWide = DIM / 64, kFeatures = DIM / 16, kStride = DIM + 4;
@@ -243,6 +244,10 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     uint32_t k_page, v_page;
     const auto find_pages = [&](uint32_t at) {
+        if constexpr (WIDE) {
+            k_page = v_page = at < last ? page_of(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift)) : kNoPage;
+            return;
+        }
         const uint32_t k_group = at * kAttendStep + i / 4 * 16, v_group = at * kAttendStep + g * 16;
         k_page = at < last && k_group < range.high && k_group + 16 > range.low ? page_of(a.s, s, k_group >> shift) : kNoPage;
         v_page = at < last && v_group < range.high && v_group + 16 > range.low ? page_of(a.s, s, v_group >> shift) : kNoPage;
@@ -253,7 +258,8 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     uint32_t found = 0;  // NaN among values that not all rows see
     const auto request_keys = [&](uint32_t at) {
         const uint64_t page = static_cast<uint64_t>(k_page != kNoPage ? k_page : 0) * a.c.heads + head;  // (read, and not used)
-        const uint8_t *from = a.c.k + ((page << shift) + ((at * kAttendStep + i / 4 * 16) & inside) + i % 4) * DIM + g * 16;
+        const uint8_t *from = WIDE ? a.c.k + ((page << shift) + (at * kAttendStep & inside)) * DIM + (i / 4 * 16 + i % 4) * DIM + g * 16
+                                   : a.c.k + ((page << shift) + ((at * kAttendStep + i / 4 * 16) & inside) + i % 4) * DIM + g * 16;
         k_scale = a.c.k_scales[page];
 #pragma unroll
         for (uint32_t t = 0; t < 4; ++t)
@@ -264,7 +270,8 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     const auto request_values = [&](uint32_t at) {
         held = v_page != kNoPage;
         const uint64_t page = static_cast<uint64_t>(held ? v_page : 0) * a.c.heads + head;
-        const uint8_t *from = a.c.v + ((page * DIM + i) << shift) + ((at * kAttendStep + g * 16) & inside);
+        const uint8_t *from = WIDE ? a.c.v + (page * DIM << shift) + (at * kAttendStep & inside) + (i << shift) + g * 16
+                                   : a.c.v + ((page * DIM + i) << shift) + ((at * kAttendStep + g * 16) & inside);
         v_scale = a.c.v_scales[page];
         v_scale = held ? v_scale : 1.0f;
 #pragma unroll
@@ -384,7 +391,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
 // ---- some rows: the same with 32 rows to a workgroup, in matrix instructions of 32 x 32.  Here the lane (row c = l % 32, half h = l / 32) has of
 // every 32 keys the ones 16 h .. 16 h + 15; row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4.
 
-template <uint32_t DIM>
+template <uint32_t DIM, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const AttendArgs a)
 {
     constexpr uint32_t kWide = DIM / 32, WAVES = kAttendThreads / 64, kStride = DIM + 4;
@@ -422,6 +429,10 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     uint32_t k_page[2], v_page[2];
     const auto page_at = [&](uint32_t group) { return group < range.high && group + 16 > range.low ? page_of(a.s, s, group >> shift) : kNoPage; };
     const auto find_pages = [&](uint32_t at) {
+        if constexpr (WIDE) {
+            k_page[0] = k_page[1] = v_page[0] = v_page[1] = at < last ? page_of(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift)) : kNoPage;
+            return;
+        }
 #pragma unroll
         for (uint32_t x = 0; x < 2; ++x) {
             const uint32_t k0 = at * kAttendStep + x * 32;
@@ -437,7 +448,8 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 #pragma unroll
         for (uint32_t x = 0; x < 2; ++x) {
             const uint64_t page = static_cast<uint64_t>(k_page[x] != kNoPage ? k_page[x] : 0) * a.c.heads + head;  // (read, and not used)
-            const uint8_t *from = a.c.k + ((page << shift) + ((at * kAttendStep + x * 32 + k_row) & inside)) * DIM + h * 16;
+            const uint8_t *from = WIDE ? a.c.k + ((page << shift) + ((at * kAttendStep + x * 32) & inside)) * DIM + k_row * DIM + h * 16
+                                       : a.c.k + ((page << shift) + ((at * kAttendStep + x * 32 + k_row) & inside)) * DIM + h * 16;
             k_scale[x] = a.c.k_scales[page];
 #pragma unroll
             for (uint32_t j = 0; j < kWide; ++j)
@@ -449,7 +461,8 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
         for (uint32_t x = 0; x < 2; ++x) {
             held[x] = v_page[x] != kNoPage;
             const uint64_t page = static_cast<uint64_t>(held[x] ? v_page[x] : 0) * a.c.heads + head;
-            const uint8_t *from = a.c.v + ((page * DIM + c) << shift) + ((at * kAttendStep + x * 32 + h * 16) & inside);
+            const uint8_t *from = WIDE ? a.c.v + (page * DIM << shift) + ((at * kAttendStep + x * 32) & inside) + (c << shift) + h * 16
+                                       : a.c.v + ((page * DIM + c) << shift) + ((at * kAttendStep + x * 32 + h * 16) & inside);
             v_scale[x] = a.c.v_scales[page];
             v_scale[x] = held[x] ? v_scale[x] : 1.0f;
 #pragma unroll
@@ -566,7 +579,6 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 // next step's products beside this step's exponentials in the program 169 us: 256 registers leave none for operands on their way.
 constexpr int kSchedVector = 0x2, kSchedMatrix = 0x8, kSchedLds = 0x100;  // kinds of instructions (sched_group_barrier)
 
-// WIDE: a step lies in one page
 template <uint32_t DIM, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const AttendArgs a)
 {

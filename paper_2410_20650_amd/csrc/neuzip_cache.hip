@@ -68,20 +68,26 @@ inline AttendShape shape_of(const neuzip_cache *c, const neuzip_sequences *s, ui
 
 inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_heads > 0 && q_heads % c->heads == 0; }
 
+template <uint32_t DIM, bool WIDE>
+void launch_attend_as(const AttendArgs &a, const AttendShape &shape, uint32_t wgs, hipStream_t stream)
+{
+    if (shape.rows == kAttendManyRows)
+        hipLaunchKernelGGL((attend_many_kernel<DIM, WIDE>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    else if (shape.rows == kAttendSomeRows)
+        hipLaunchKernelGGL((attend_some_kernel<DIM, WIDE>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    else if (shape.waves == 8)
+        hipLaunchKernelGGL((attend_few_kernel<DIM, 8, WIDE>), dim3(wgs), dim3(512), 0, stream, a);
+    else
+        hipLaunchKernelGGL((attend_few_kernel<DIM, 4, WIDE>), dim3(wgs), dim3(256), 0, stream, a);
+}
+
 template <uint32_t DIM>
 int launch_attend(const AttendArgs &a, const AttendShape &shape, uint32_t wgs, hipStream_t stream)
 {
-    const bool wide = (1u << a.s.page_shift) >= kAttendStep;
-    if (shape.rows == kAttendSomeRows)
-        hipLaunchKernelGGL((attend_some_kernel<DIM>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
-    else if (shape.rows == kAttendManyRows && wide)
-        hipLaunchKernelGGL((attend_many_kernel<DIM, true>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
-    else if (shape.rows == kAttendManyRows)
-        hipLaunchKernelGGL((attend_many_kernel<DIM, false>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
-    else if (shape.waves == 8)
-        hipLaunchKernelGGL((attend_few_kernel<DIM, 8>), dim3(wgs), dim3(512), 0, stream, a);
+    if ((1u << a.s.page_shift) >= kAttendStep)
+        launch_attend_as<DIM, true>(a, shape, wgs, stream);
     else
-        hipLaunchKernelGGL((attend_few_kernel<DIM, 4>), dim3(wgs), dim3(256), 0, stream, a);
+        launch_attend_as<DIM, false>(a, shape, wgs, stream);
     if (!hip_ok(hipGetLastError()))
         return NEUZIP_EHIP;
     if (a.splits > 1) {
