@@ -35,6 +35,7 @@ struct AttendArgs {
     uint32_t q_heads, group;
     uint32_t window;
     uint32_t splits, tiles;
+    TileNumbers numbers;  // of the tiles
     uint32_t most_keys;   // that a tile's rows see, as the caller has it
     uint32_t least_steps; // of a split
     float scale;        // times log2(e)
@@ -211,7 +212,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     __shared__ float2 stats[WAVES][kAttendFewRows];
     __shared__ attend_bf16x8_t queries[kWide * 2][64];
     const uint32_t split = blockIdx.x % a.splits, head = blockIdx.x / a.splits % a.c.heads, tile = blockIdx.x / a.splits / a.c.heads;
-    const Found at = find_sequence(a.s, {attend_shift(kAttendFewRows), a.group, 1}, tile, a.splits > 1);
+    const Found at = find_sequence(a.s, a.numbers, tile, a.splits > 1);
     if (at.s >= a.s.count)
         return;
     const uint32_t s = at.s;
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     __shared__ float2 stats[WAVES][kAttendSomeRows];
     __shared__ attend_bf16x8_t queries[kWide * 2][64];
     const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
-    const Found at = find_sequence(a.s, {attend_shift(kAttendSomeRows), a.group, 1}, tile, a.splits > 1);
+    const Found at = find_sequence(a.s, a.numbers, tile, a.splits > 1);
     if (at.s >= a.s.count)
         return;
     const uint32_t s = at.s;
@@ -589,7 +590,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     __shared__ __align__(16) uint8_t value_space[2][kBytes];
     __shared__ uint4 there_space[2];  // of four times 16 keys: not 0 if they have a page
     const uint32_t head = blockIdx.x % a.c.heads, split = blockIdx.x / a.c.heads % a.splits, tile = a.tiles - 1 - blockIdx.x / a.c.heads / a.splits;
-    const Found at = find_sequence(a.s, {attend_shift(kAttendManyRows), a.group, 1}, tile, a.splits > 1);
+    const Found at = find_sequence(a.s, a.numbers, tile, a.splits > 1);
     if (at.s >= a.s.count)
         return;
     const uint32_t s = at.s;

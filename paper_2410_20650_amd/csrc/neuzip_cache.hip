@@ -198,6 +198,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
     a.window = window;
     a.splits = shape.splits;
     a.tiles = static_cast<uint32_t>(shape.tiles);
+    a.numbers = shape.numbers;
     a.most_keys = shape.keys;
     a.least_steps = shape.least_steps;
     a.scale = scale * 1.4426950408889634f;

@@ -43,13 +43,13 @@ struct Found {
     uint32_t longest;    // no sequence has more tokens
 };
 
-// A wave works it out together.  Up to 63 sequences are all read at once, so that what comes next waits for memory once.
+// A wave works it out together.  Up to 64 sequences are all read at once, so that what comes next waits for memory once.
 __device__ __forceinline__ Found find_sequence(const SequencesView &v, const TileNumbers &t, uint64_t id, bool with_longest)
 {
     const uint32_t lane = threadIdx.x % 64;
     Found f;
     int32_t longest = 0;
-    if (v.count < 64) {
+    if (v.count <= 64) {
         const uint32_t at = lane < v.count ? lane : v.count - 1;
         const int32_t begin = v.starts[at], end = v.starts[at + 1], length = v.lengths[at];
         const uint32_t before = __popcll(__ballot(lane < v.count && first_tile(t, begin, lane) <= id));

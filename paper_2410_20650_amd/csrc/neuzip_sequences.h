@@ -59,6 +59,7 @@ NZ_BOTH uint32_t page_of(const SequencesView &v, uint32_t s, uint32_t number)
 // lay in whole tiles, and `slack` more for each sequence; numbers that no tile takes have nothing to do.  With u = 2^shift:
 //   n rows in tiles of their own: ceil(n / u) <= floor((a + n) / u) - floor(a / u) + 1, slack 1
 //   n tokens in pages of u, from anywhere in a page on: ceil(n / u) + 1 at most, slack 2
+//   a row's own number, or `group` of them (shift 0): slack 0
 struct TileNumbers {
     uint32_t shift, group, slack;
 };
@@ -68,7 +69,7 @@ NZ_BOTH uint64_t first_tile(const TileNumbers &t, int32_t start, uint32_t s)
 }
 NZ_BOTH uint64_t tile_count(const TileNumbers &t, uint32_t rows, uint32_t count)
 {
-    return (static_cast<uint64_t>(rows) * t.group >> t.shift) + static_cast<uint64_t>(t.slack) * count + (t.slack == 0);
+    return (static_cast<uint64_t>(rows) * t.group >> t.shift) + static_cast<uint64_t>(t.slack) * count;
 }
 
 }  // namespace nz

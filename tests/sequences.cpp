@@ -116,6 +116,26 @@ int main()
                     require(got[{s, r}] == 1, "a row once");
             require(got.size() == want, "no other rows");
         }
+        // tiles of rows that are counted row by row
+        for (uint32_t unit : {16u, 32u, 128u}) {
+            const uint32_t group = 1 + below(40);
+            const TileNumbers t = {0, (group + unit - 1) / unit, 0};
+            std::map<std::pair<uint32_t, uint32_t>, int> got;
+            for (uint64_t id = 0; id < tile_count(t, rows, count); ++id) {
+                const uint32_t s = sequence_of(starts, count, t, id);
+                if (s >= count)
+                    continue;
+                const NewTokens n = new_tokens(v, s);
+                const uint64_t row0 = (id - first_tile(t, starts[s], s)) * unit;
+                for (uint64_t r = row0; r < row0 + unit && r < static_cast<uint64_t>(n.count) * group; ++r)
+                    ++got[{s, static_cast<uint32_t>(r)}];
+            }
+            size_t want = 0;
+            for (uint32_t s = 0; s < count; ++s)
+                for (uint32_t r = 0; r < new_tokens(v, s).count * group; ++r, ++want)
+                    require(got[{s, r}] == 1, "a row once, counted by rows");
+            require(got.size() == want, "no other rows, counted by rows");
+        }
     }
     std::printf("ok\n");
     return 0;

@@ -214,6 +214,16 @@ def test_long_ones(nz, counts, lengths, q_heads, dim, page):
     check_attention(nz, cache, plain, table, counts, lengths, q_heads, seed=42, window=1000)
 
 
+@pytest.mark.parametrize("count", [63, 64, 65, 200])
+@pytest.mark.parametrize("group", [1, 20])
+def test_many_sequences(nz, count, group):
+    lengths = [1 + (37 * i) % 150 for i in range(count)]
+    cache, plain, table = filled(nz, lengths, 1, 16, 64, seed=45)
+    check_attention(nz, cache, plain, table, [1] * count, lengths, group, seed=46, padding=1)
+    some = [(i * 7) % 3 for i in range(count)]
+    check_attention(nz, cache, plain, table, [min(n, m) for n, m in zip(some, lengths)], lengths, group, seed=47)
+
+
 def test_a_table_with_much_more_room(nz):
     lengths = [70, 300]
     cache, plain, table = filled(nz, lengths, 2, 64, 128, seed=50)
