@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kNormBackThreads) norm_back_kernel(const NormB
                 squares += space[turn][0][row_first + i], both += space[turn][1][row_first + i];
         }
         const float n = 1.0f / sqrtf(squares * a.per_width + a.eps);
-        const float back = n * n * n * (both * a.per_width);
+        const float pull = n * (both * a.per_width);  // (n^3 by itself would leave binary32 where rows are very small or large)
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
             const uint32_t col = (p * THREADS + lane) * 8;
@@ -208,8 +208,9 @@ __global__ void __launch_bounds__(kNormBackThreads) norm_back_kernel(const NormB
                     norm_load(a.grad_total + at + col, out);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    out[i] += n * (g[p][i] * w[p][i]) - t[p][i] * back;
-                    dw[p][i] += g[p][i] * (t[p][i] * n);
+                    const float tn = t[p][i] * n;
+                    out[i] += n * (g[p][i] * w[p][i] - tn * pull);
+                    dw[p][i] += g[p][i] * tn;
                 }
                 if (a.grad_x)
                     norm_store(a.grad_x + at + col, out);

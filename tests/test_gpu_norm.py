@@ -112,6 +112,25 @@ def test_gradients_against_differences(nz, width):
         assert abs(float(grad_weight[c]) - want) <= 1e-5 * (1 + abs(want))
 
 
+@pytest.mark.parametrize("stream", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-15, 1e15])
+def test_very_small_and_large_rows(nz, size, stream):
+    """1 / rms to the third power is no binary32 number there, the gradients are."""
+    tokens, width = 5, 264
+    total = normal(tokens, width, seed=14, std=size, dtype=TYPES[stream])
+    weight, grad_y = 1 + normal(width, seed=15, std=0.2), normal(tokens, width, seed=16, dtype=torch.bfloat16)
+    s, w, gy = total.double(), weight.double(), grad_y.double()
+    n = 1 / s.square().mean(dim=1, keepdim=True).sqrt()
+    want = s * n * w
+    within(nz.neuzip_norm(total, weight, 0.0), want, want.abs() * (2.0 ** -8 + (width / 1024 + 20) * ULP))
+    grad_x, grad_weight = nz.neuzip_norm_backward(total, weight, grad_y, 0.0)
+    g = gy * w
+    want = n * (g - s * n ** 2 * (g * s).mean(dim=1, keepdim=True))
+    within(grad_x, want, want.abs() * 2.0 ** -8 + 3 * (width / 512 + 20) * ULP * n * (g.abs() + s.abs() * n ** 2 * (g * s).abs().mean(dim=1, keepdim=True)))
+    terms = gy * s * n
+    within(grad_weight, terms.sum(dim=0), (tokens + width / 1024 + 40) * ULP * terms.abs().sum(dim=0))
+
+
 def test_no_tokens(nz):
     weight = torch.ones(64, device=DEV)
     none = torch.empty(0, 64, dtype=torch.bfloat16, device=DEV)
