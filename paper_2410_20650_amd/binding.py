@@ -968,6 +968,8 @@ def neuzip_cache_attention(cache: KeyValueCache, sequences: Sequences, q: torch.
     rows, q_row = _rows_of(q, q_heads, dim, torch.bfloat16, "q", device)
     if q_heads == 0 or q_heads % cache.heads:
         raise ValueError("the query heads are a multiple of the cache's heads")
+    if not 0 <= window < 1 << 32 or not 0 <= longest < 1 << 32:
+        raise ValueError("window and longest are numbers of tokens")
     if out is None:
         out = _empty_like(q, torch.bfloat16, stream)    # (without gaps, also where q's rows lie apart)
     else:

@@ -137,6 +137,13 @@ def test_refused(called, call, name):
     assert reached(called) == []
 
 
+@pytest.mark.parametrize("bad", [dict(window=-1), dict(window=1 << 32), dict(longest=-1), dict(longest=1 << 64)])
+def test_numbers_of_tokens_that_are_none(called, bad):
+    with pytest.raises(ValueError):
+        nz.neuzip_cache_attention(cache(), sequences(), Stub((TOKENS, HEADS * GROUP, DIM)), **bad)
+    assert reached(called) == []
+
+
 def test_rows_that_lie_apart(called):
     """Parts of a projection's rows are taken as they are, if rows begin on 16 bytes; a row's own elements have no gaps."""
     part = (TOKENS, HEADS * DIM)
