@@ -499,7 +499,7 @@ typedef struct {
  * The sequences of a call, ragged: sequence s has the rows d_starts[s] .. d_starts[s + 1] - 1 of the call's tensors, its newest tokens, and with
  * them d_lengths[s] tokens in all; token p of it is in page d_table[s * table_width + p / page_tokens] of the cache, at p % page_tokens.
  *
- *   d_starts    count + 1 32-bit integers, ascending.  Rows from d_starts[count] on belong to nobody (a padded batch): they are not
+ *   d_starts    count + 1 32-bit integers, not negative, ascending, up to the tensors' rows.  Rows from d_starts[count] on belong to nobody (a padded batch): they are not
  *               read, and what they are in an output stays as it is.
  *   d_lengths   count 32-bit integers.  A sequence with fewer tokens than rows, or with more than table_width * page_tokens, is left out: nothing
  *               of it is appended, its rows of an attention's output are zeros.
@@ -530,7 +530,8 @@ typedef struct {
  *   d_rotary    rotary_rows x head_dim floats: of position p the head_dim / 2 cosines, then the sines; rotary_rows at least table_width * page_tokens
  *               (else EINVAL).  NULL (and 0): nothing is rotated.
  *   rows        of the tensors.
- * A page that is appended to belongs to one sequence, and to no other call at that time.  All pointers to values are aligned to 16 bytes.
+ * A page that is appended to belongs to one sequence, once in its table, and to no other call at that time.  A left-out sequence's rows of q_out
+ * are zeros.  All pointers to values are aligned to 16 bytes.
  * Never allocates, never synchronises; results do not change from run to run.
  */
 int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *sequences, int type, const void *d_k, uint64_t k_row,
