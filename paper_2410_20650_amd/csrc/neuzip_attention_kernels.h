@@ -135,6 +135,31 @@ __device__ __forceinline__ void attend_split(const AttendArgs &a, uint32_t longe
     end = last - begin > each ? begin + each : last;
 }
 
+// What the table says of a page, asked for a step before it is needed.  It is looked at only then: a check right behind the request would wait for it, and
+// for the keys and values that were requested before it.
+struct AttendEntry {
+    uint32_t page;
+    bool in;
+};
+// UNIFORM: number is the same for all lanes
+template <bool UNIFORM>
+__device__ __forceinline__ AttendEntry attend_ask(const SequencesView &v, uint32_t s, uint32_t number, bool wanted)
+{
+    uint32_t zero = 0;
+    if constexpr (UNIFORM)
+        asm volatile("v_mov_b32 %0, 0" : "=v"(zero));  // (a vector load: scalar ones are waited for together with all that comes from LDS)
+    AttendEntry e;
+    e.in = wanted && number < v.table_width;
+    e.page = static_cast<uint32_t>((v.table + static_cast<uint64_t>(s) * v.table_width + (e.in ? number : 0))[zero]);
+    return e;
+}
+template <bool UNIFORM>
+__device__ __forceinline__ uint32_t attend_told(const SequencesView &v, const AttendEntry &e)
+{
+    const uint32_t page = UNIFORM ? __builtin_amdgcn_readfirstlane(e.page) : e.page;
+    return e.in && page < v.pages ? page : kNoPage;
+}
+
 // Where the sums of a row go: index of its token's head.
 __device__ __forceinline__ uint64_t attend_row(const AttendArgs &a, const NewTokens &n, uint32_t head, uint32_t r)
 {
@@ -243,21 +268,22 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     // Requests run ahead of the sums: the next step's pages are looked up a step before, its keys are asked for as soon as this step's are
     // used up, its values behind this step's second product.
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
-    uint32_t k_page, v_page;
+    AttendEntry k_entry, v_entry;
     const auto find_pages = [&](uint32_t at) {
         if constexpr (WIDE) {
-            k_page = v_page = at < last ? page_of(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift)) : kNoPage;
+            k_entry = v_entry = attend_ask<true>(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift), at < last);
             return;
         }
         const uint32_t k_group = at * kAttendStep + i / 4 * 16, v_group = at * kAttendStep + g * 16;
-        k_page = at < last && k_group < range.high && k_group + 16 > range.low ? page_of(a.s, s, k_group >> shift) : kNoPage;
-        v_page = at < last && v_group < range.high && v_group + 16 > range.low ? page_of(a.s, s, v_group >> shift) : kNoPage;
+        k_entry = attend_ask<false>(a.s, s, k_group >> shift, at < last && k_group < range.high && k_group + 16 > range.low);
+        v_entry = attend_ask<false>(a.s, s, v_group >> shift, at < last && v_group < range.high && v_group + 16 > range.low);
     };
     uint4 k[4][kWide], v[kFeatures];
     float k_scale, v_scale;
     bool held;
     uint32_t found = 0;  // NaN among values that not all rows see
     const auto request_keys = [&](uint32_t at) {
+        const uint32_t k_page = attend_told<WIDE>(a.s, k_entry);
         const uint64_t page = static_cast<uint64_t>(k_page != kNoPage ? k_page : 0) * a.c.heads + head;  // (read, and not used)
         const uint8_t *from = WIDE ? a.c.k + ((page << shift) + (at * kAttendStep & inside)) * DIM + (i / 4 * 16 + i % 4) * DIM + g * 16
                                    : a.c.k + ((page << shift) + ((at * kAttendStep + i / 4 * 16) & inside) + i % 4) * DIM + g * 16;
@@ -268,13 +294,15 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
             for (uint32_t j = 0; j < kWide; ++j)
                 k[t][j] = *reinterpret_cast<const uint4 *>(from + t * 4 * DIM + j * 64);
     };
-    const auto request_values = [&](uint32_t at) {
+    // (and the entries of the step `next`, before the values: whoever waits for them does not wait for these)
+    const auto request_values = [&](uint32_t at, uint32_t next) {
+        const uint32_t v_page = attend_told<WIDE>(a.s, v_entry);
         held = v_page != kNoPage;
+        find_pages(next);
         const uint64_t page = static_cast<uint64_t>(held ? v_page : 0) * a.c.heads + head;
         const uint8_t *from = WIDE ? a.c.v + (page * DIM << shift) + (at * kAttendStep & inside) + (i << shift) + g * 16
                                    : a.c.v + ((page * DIM + i) << shift) + ((at * kAttendStep + g * 16) & inside);
         v_scale = a.c.v_scales[page];
-        v_scale = held ? v_scale : 1.0f;
 #pragma unroll
         for (uint32_t f = 0; f < kFeatures; ++f)
             v[f] = *reinterpret_cast<const uint4 *>(from + (f * 16 << shift));
@@ -284,8 +312,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     if (step < last) {
         find_pages(step);
         request_keys(step);
-        request_values(step);
-        find_pages(step + WAVES);
+        request_values(step, step + WAVES);
     }
     for (; step < last; step += WAVES) {
         const uint32_t k0 = step * kAttendStep, v_group = k0 + g * 16;
@@ -344,16 +371,15 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
                 total += score[t][r];
             }
         const attend_bf16x8_t p0 = attend_round(score[0][0], score[0][1], score[0][2], score[0][3], score[1][0], score[1][1], score[1][2], score[1][3]);
+        const float of_values = held ? v_scale : 1.0f;
         const attend_bf16x8_t p1 = attend_round(score[2][0], score[2][1], score[2][2], score[2][3], score[3][0], score[3][1], score[3][2], score[3][3]);
 #pragma unroll
         for (uint32_t f = 0; f < kFeatures; ++f) {
-            o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].x, v[f].y, v_scale), p0, o[f], 0, 0, 0);
-            o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].z, v[f].w, v_scale), p1, o[f], 0, 0, 0);
+            o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].x, v[f].y, of_values), p0, o[f], 0, 0, 0);
+            o[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(attend_widen(v[f].z, v[f].w, of_values), p1, o[f], 0, 0, 0);
         }
-        if (step + WAVES < last) {
-            request_values(step + WAVES);
-            find_pages(step + 2 * WAVES);
-        }
+        if (step + WAVES < last)
+            request_values(step + WAVES, step + 2 * WAVES);
     }
     total += __shfl_xor(total, 16);
     total += __shfl_xor(total, 32);
@@ -427,18 +453,18 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     attend_split(a, at.longest, range, split, step, last);
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     const uint32_t k_row = c / 4 % 2 * 16 + c / 8 * 4 + c % 4;
-    uint32_t k_page[2], v_page[2];
-    const auto page_at = [&](uint32_t group) { return group < range.high && group + 16 > range.low ? page_of(a.s, s, group >> shift) : kNoPage; };
+    AttendEntry k_entry[2], v_entry[2];
     const auto find_pages = [&](uint32_t at) {
+        const auto entry_at = [&](uint32_t group) { return attend_ask<false>(a.s, s, group >> shift, at < last && group < range.high && group + 16 > range.low); };
         if constexpr (WIDE) {
-            k_page[0] = k_page[1] = v_page[0] = v_page[1] = at < last ? page_of(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift)) : kNoPage;
+            k_entry[0] = k_entry[1] = v_entry[0] = v_entry[1] = attend_ask<true>(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift), at < last);
             return;
         }
 #pragma unroll
         for (uint32_t x = 0; x < 2; ++x) {
             const uint32_t k0 = at * kAttendStep + x * 32;
-            k_page[x] = at < last ? page_at(k0 + c / 4 % 2 * 16) : kNoPage;
-            v_page[x] = at < last ? page_at(k0 + h * 16) : kNoPage;
+            k_entry[x] = entry_at(k0 + c / 4 % 2 * 16);
+            v_entry[x] = entry_at(k0 + h * 16);
         }
     };
     uint4 k[2][kWide], v[2][kWide];
@@ -448,7 +474,8 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     const auto request_keys = [&](uint32_t at) {
 #pragma unroll
         for (uint32_t x = 0; x < 2; ++x) {
-            const uint64_t page = static_cast<uint64_t>(k_page[x] != kNoPage ? k_page[x] : 0) * a.c.heads + head;  // (read, and not used)
+            const uint32_t k_page = attend_told<WIDE>(a.s, k_entry[x]);
+            const uint64_t page = static_cast<uint64_t>(k_page != kNoPage ? k_page : 0) * a.c.heads + head;  // (read, and not used)
             const uint8_t *from = WIDE ? a.c.k + ((page << shift) + ((at * kAttendStep + x * 32) & inside)) * DIM + k_row * DIM + h * 16
                                        : a.c.k + ((page << shift) + ((at * kAttendStep + x * 32 + k_row) & inside)) * DIM + h * 16;
             k_scale[x] = a.c.k_scales[page];
@@ -457,7 +484,10 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
                 k[x][j] = *reinterpret_cast<const uint4 *>(from + j * 32);
         }
     };
-    const auto request_values = [&](uint32_t at) {
+    // (and the entries of the step `next`, before the values: whoever waits for them does not wait for these)
+    const auto request_values = [&](uint32_t at, uint32_t next) {
+        const uint32_t v_page[2] = {attend_told<WIDE>(a.s, v_entry[0]), attend_told<WIDE>(a.s, v_entry[1])};
+        find_pages(next);
 #pragma unroll
         for (uint32_t x = 0; x < 2; ++x) {
             held[x] = v_page[x] != kNoPage;
@@ -465,7 +495,6 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
             const uint8_t *from = WIDE ? a.c.v + (page * DIM << shift) + ((at * kAttendStep + x * 32) & inside) + (c << shift) + h * 16
                                        : a.c.v + ((page * DIM + c) << shift) + ((at * kAttendStep + x * 32 + h * 16) & inside);
             v_scale[x] = a.c.v_scales[page];
-            v_scale[x] = held[x] ? v_scale[x] : 1.0f;
 #pragma unroll
             for (uint32_t f = 0; f < kWide; ++f)
                 v[x][f] = *reinterpret_cast<const uint4 *>(from + (f * 32 << shift));
@@ -476,8 +505,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     if (step < last) {
         find_pages(step);
         request_keys(step);
-        request_values(step);
-        find_pages(step + WAVES);
+        request_values(step, step + WAVES);
     }
     for (; step < last; step += WAVES) {
         const uint32_t k0 = step * kAttendStep;
@@ -533,18 +561,17 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
                 total += score[x][e];
             }
             const attend_f32x16_t &w = score[x];
+            const float of_values = held[x] ? v_scale[x] : 1.0f;
             const attend_bf16x8_t p0 = attend_round(w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]);
             const attend_bf16x8_t p1 = attend_round(w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]);
 #pragma unroll
             for (uint32_t f = 0; f < kWide; ++f) {
-                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(v[x][f].x, v[x][f].y, v_scale[x]), p0, o[f], 0, 0, 0);
-                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(v[x][f].z, v[x][f].w, v_scale[x]), p1, o[f], 0, 0, 0);
+                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(v[x][f].x, v[x][f].y, of_values), p0, o[f], 0, 0, 0);
+                o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(attend_widen(v[x][f].z, v[x][f].w, of_values), p1, o[f], 0, 0, 0);
             }
         }
-        if (step + WAVES < last) {
-            request_values(step + WAVES);
-            find_pages(step + 2 * WAVES);
-        }
+        if (step + WAVES < last)
+            request_values(step + WAVES, step + 2 * WAVES);
     }
     total += __shfl_xor(total, 32);
     if (__any(found != 0)) {
@@ -620,15 +647,18 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     // the thread's items of a step: a key's 16 features, a feature's 16 keys
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     const uint32_t k_key = threadIdx.x / (DIM / 16), k_part = threadIdx.x % (DIM / 16), v_feature = threadIdx.x / 4, v_part = threadIdx.x % 4;
-    uint32_t k_page[WIDE ? 1 : kItems], v_page;
+    AttendEntry k_entry[WIDE ? 1 : kItems], v_entry;
     const auto find_key_pages = [&](uint32_t at) {
 #pragma unroll
         for (uint32_t i = 0; i < (WIDE ? 1 : kItems); ++i)
-            k_page[i] = at < last ? page_of(a.s, s, (at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) >> shift) : kNoPage;
+            k_entry[i] = attend_ask<WIDE>(a.s, s, (at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) >> shift, at < last);
     };
     const auto find_value_pages = [&](uint32_t at) {
         const uint32_t v0 = at * kAttendStep + (WIDE ? 0 : v_part * 16);
-        v_page = at < last && (WIDE || (v0 < range.high && v0 + 16 > range.low)) ? page_of(a.s, s, v0 >> shift) : kNoPage;
+        if constexpr (WIDE)
+            v_entry = k_entry[0];
+        else
+            v_entry = attend_ask<false>(a.s, s, v0 >> shift, at < last && v0 < range.high && v0 + 16 > range.low);
     };
     uint4 k_item[kItems], v_item[kItems];
     float k_scale[WIDE ? 1 : kItems], v_scale;
@@ -637,18 +667,19 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
             const uint32_t p = WIDE ? 0 : i;
-            k_there[p] = k_page[p] != kNoPage;
-            const uint64_t page = static_cast<uint64_t>(k_there[p] ? k_page[p] : 0) * a.c.heads + head;  // (read, and not used)
+            const uint32_t k_page = attend_told<WIDE>(a.s, k_entry[p]);
+            k_there[p] = k_page != kNoPage;
+            const uint64_t page = static_cast<uint64_t>(k_there[p] ? k_page : 0) * a.c.heads + head;  // (read, and not used)
             k_scale[p] = a.c.k_scales[page];
             const uint8_t *from = a.c.k + ((page << shift) + ((at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) & inside)) * DIM;
             k_item[i] = *reinterpret_cast<const uint4 *>(from + (WIDE ? (k_key + i * kKeysApart) * DIM : 0) + k_part * 16);
         }
     };
     const auto request_values = [&](uint32_t at) {
+        const uint32_t v_page = attend_told<WIDE>(a.s, v_entry);
         v_there = v_page != kNoPage;
         const uint64_t page = static_cast<uint64_t>(v_there ? v_page : 0) * a.c.heads + head;
         v_scale = a.c.v_scales[page];
-        v_scale = v_there ? v_scale : 1.0f;
         const uint8_t *from = a.c.v + (page * DIM << shift) + ((at * kAttendStep + (WIDE ? 0 : v_part * 16)) & inside);
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i)
@@ -680,12 +711,13 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
                 found |= attend_clean(v_item[i].z, attend_bytes(from, upto, 2)) | attend_clean(v_item[i].w, attend_bytes(from, upto, 3));
             }
         }
+        const float of_values = v_there ? v_scale : 1.0f;
 #pragma unroll
         for (uint32_t i = 0; i < kItems; ++i) {
             const uint32_t feature = v_feature + i * kFeaturesApart;
             uint8_t *line = value_space[turn] + feature * kAttendStep * 2;
-            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2) ^ (feature / 2 % 8)) * 16) = attend_widen(v_item[i].x, v_item[i].y, v_scale);
-            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2 + 1) ^ (feature / 2 % 8)) * 16) = attend_widen(v_item[i].z, v_item[i].w, v_scale);
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2) ^ (feature / 2 % 8)) * 16) = attend_widen(v_item[i].x, v_item[i].y, of_values);
+            *reinterpret_cast<attend_bf16x8_t *>(line + ((v_part * 2 + 1) ^ (feature / 2 % 8)) * 16) = attend_widen(v_item[i].z, v_item[i].w, of_values);
         }
     };
 
@@ -735,6 +767,9 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         put_keys(0);
         put_values(begin, 0);
     }
+#pragma unroll
+    for (uint32_t j = 0; j < DIM / 16; ++j)
+        asm volatile("" ::"v"(q[j]));  // (the queries are waited for here, not in every step)
     uint32_t step = begin;
     for (uint32_t turn = 0; step < last; ++step, turn ^= 1) {
         __syncthreads();
@@ -745,8 +780,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
             find_value_pages(step + 2);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (!WIDE)
-            __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_s_setprio(0);
         attend_f32x16_t now[2];
         products(now, turn);
         // (six operands on their way from LDS before the first product, one more behind each)
@@ -785,21 +819,23 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
                 o[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values, p, o[f], 0, 0, 0);
             }
         }
-        // (four operands before the exponentials; then the products, the remaining exponentials between them)
-        __builtin_amdgcn_sched_group_barrier(kSchedLds, 4, 1);
-        __builtin_amdgcn_sched_group_barrier(kSchedVector, 34, 1);
+        // Pages of less than a step, heads of 128: four operands before the exponentials; then the products, the remaining exponentials between them (4096
+        // tokens of 32 heads on 8 in pages of 16: 160 us, in the compiler's order 168).  Elsewhere its order is the better one (pages of 64: 4096 tokens 159 us,
+        // this one 161; 16384 tokens 2140 and 2290).
+        if constexpr (!WIDE && DIM > 64) {
+            __builtin_amdgcn_sched_group_barrier(kSchedLds, 4, 1);
+            __builtin_amdgcn_sched_group_barrier(kSchedVector, 34, 1);
 #pragma unroll
-        for (uint32_t g = 0; g < DIM / 8 - 4; ++g) {
-            __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 1);
-            __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 1);
-            __builtin_amdgcn_sched_group_barrier(kSchedVector, 8, 1);
+            for (uint32_t g = 0; g < DIM / 8 - 4; ++g) {
+                __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(kSchedLds, 1, 1);
+                __builtin_amdgcn_sched_group_barrier(kSchedVector, 8, 1);
+            }
+            __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 4, 1);
         }
-        __builtin_amdgcn_sched_group_barrier(kSchedMatrix, 4, 1);
         __builtin_amdgcn_sched_barrier(0);
-        // (short pages: widening and the next requests, with a page of their own each, go before the other workgroup's products: 4096 tokens in
-        // pages of 16 182 us, without it 198; in pages of 64 165 either way, 16384 tokens 1 % more)
-        if constexpr (!WIDE)
-            __builtin_amdgcn_s_setprio(1);
+        // (widening and the next requests go before the products of the other workgroup's wave on the SIMD: 159 us, without that 163)
+        __builtin_amdgcn_s_setprio(1);
         if (step + 1 < last) {
             put_keys(turn ^ 1);
             put_values(step + 1, turn ^ 1);

@@ -87,8 +87,16 @@ __device__ __forceinline__ Found find_sequence(const SequencesView &v, const Til
 #pragma unroll
         for (int apart = 32; apart; apart >>= 1)
             longest = max(longest, __shfl_xor(longest, apart));
-        f.longest = longest > 0 ? static_cast<uint32_t>(longest) : 0;
+        f.longest = __builtin_amdgcn_readfirstlane(longest > 0 ? static_cast<uint32_t>(longest) : 0);
     }
+    // (every lane has the same; what hangs on it is scalar once that is said)
+    f.s = __builtin_amdgcn_readfirstlane(f.s);
+    f.n.begin = __builtin_amdgcn_readfirstlane(f.n.begin);
+    f.n.count = __builtin_amdgcn_readfirstlane(f.n.count);
+    f.n.first = __builtin_amdgcn_readfirstlane(f.n.first);
+    f.n.length = __builtin_amdgcn_readfirstlane(f.n.length);
+    f.tile = static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(f.tile >> 32))) << 32 |
+             __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(f.tile));
     return f;
 }
 
