@@ -141,18 +141,22 @@ struct AttendEntry {
     uint32_t page;
     bool in;
 };
-// UNIFORM: number is the same for all lanes
-template <bool UNIFORM>
-__device__ __forceinline__ AttendEntry attend_ask(const SequencesView &v, uint32_t s, uint32_t number, bool wanted)
+// 0 that is a vector register: number + 0 for a vector load.  Scalar loads, the compiler's choice where all lanes ask for one number, are waited for together with
+// all that comes from LDS; but the first answer of all is there sooner by one.
+__device__ __forceinline__ uint32_t attend_zero()
 {
-    uint32_t zero = 0;
-    if constexpr (UNIFORM)
-        asm volatile("v_mov_b32 %0, 0" : "=v"(zero));  // (a vector load: scalar ones are waited for together with all that comes from LDS)
+    uint32_t zero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(zero));
+    return zero;
+}
+__device__ __forceinline__ AttendEntry attend_ask(const SequencesView &v, uint32_t s, uint32_t number, bool wanted, uint32_t zero = 0)
+{
     AttendEntry e;
     e.in = wanted && number < v.table_width;
     e.page = static_cast<uint32_t>((v.table + static_cast<uint64_t>(s) * v.table_width + (e.in ? number : 0))[zero]);
     return e;
 }
+// UNIFORM: the number is the same for all lanes
 template <bool UNIFORM>
 __device__ __forceinline__ uint32_t attend_told(const SequencesView &v, const AttendEntry &e)
 {
@@ -269,14 +273,14 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     // used up, its values behind this step's second product.
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     AttendEntry k_entry, v_entry;
-    const auto find_pages = [&](uint32_t at) {
+    const auto find_pages = [&](uint32_t at, uint32_t zero) {
         if constexpr (WIDE) {
-            k_entry = v_entry = attend_ask<true>(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift), at < last);
+            k_entry = v_entry = attend_ask(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift), at < last, zero);
             return;
         }
         const uint32_t k_group = at * kAttendStep + i / 4 * 16, v_group = at * kAttendStep + g * 16;
-        k_entry = attend_ask<false>(a.s, s, k_group >> shift, at < last && k_group < range.high && k_group + 16 > range.low);
-        v_entry = attend_ask<false>(a.s, s, v_group >> shift, at < last && v_group < range.high && v_group + 16 > range.low);
+        k_entry = attend_ask(a.s, s, k_group >> shift, at < last && k_group < range.high && k_group + 16 > range.low);
+        v_entry = attend_ask(a.s, s, v_group >> shift, at < last && v_group < range.high && v_group + 16 > range.low);
     };
     uint4 k[4][kWide], v[kFeatures];
     float k_scale, v_scale;
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     const auto request_values = [&](uint32_t at, uint32_t next) {
         const uint32_t v_page = attend_told<WIDE>(a.s, v_entry);
         held = v_page != kNoPage;
-        find_pages(next);
+        find_pages(next, attend_zero());
         const uint64_t page = static_cast<uint64_t>(held ? v_page : 0) * a.c.heads + head;
         const uint8_t *from = WIDE ? a.c.v + (page * DIM << shift) + (at * kAttendStep & inside) + (i << shift) + g * 16
                                    : a.c.v + ((page * DIM + i) << shift) + ((at * kAttendStep + g * 16) & inside);
@@ -310,7 +314,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
     step += wave;
     const uint32_t begin = step;
     if (step < last) {
-        find_pages(step);
+        find_pages(step, 0);
         request_keys(step);
         request_values(step, step + WAVES);
     }
@@ -454,10 +458,10 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     const uint32_t k_row = c / 4 % 2 * 16 + c / 8 * 4 + c % 4;
     AttendEntry k_entry[2], v_entry[2];
-    const auto find_pages = [&](uint32_t at) {
-        const auto entry_at = [&](uint32_t group) { return attend_ask<false>(a.s, s, group >> shift, at < last && group < range.high && group + 16 > range.low); };
+    const auto find_pages = [&](uint32_t at, uint32_t zero) {
+        const auto entry_at = [&](uint32_t group) { return attend_ask(a.s, s, group >> shift, at < last && group < range.high && group + 16 > range.low); };
         if constexpr (WIDE) {
-            k_entry[0] = k_entry[1] = v_entry[0] = v_entry[1] = attend_ask<true>(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift), at < last);
+            k_entry[0] = k_entry[1] = v_entry[0] = v_entry[1] = attend_ask(a.s, s, __builtin_amdgcn_readfirstlane(at * kAttendStep >> shift), at < last, zero);
             return;
         }
 #pragma unroll
@@ -487,7 +491,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     // (and the entries of the step `next`, before the values: whoever waits for them does not wait for these)
     const auto request_values = [&](uint32_t at, uint32_t next) {
         const uint32_t v_page[2] = {attend_told<WIDE>(a.s, v_entry[0]), attend_told<WIDE>(a.s, v_entry[1])};
-        find_pages(next);
+        find_pages(next, attend_zero());
 #pragma unroll
         for (uint32_t x = 0; x < 2; ++x) {
             held[x] = v_page[x] != kNoPage;
@@ -503,7 +507,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     step += wave;
     const uint32_t begin = step;
     if (step < last) {
-        find_pages(step);
+        find_pages(step, 0);
         request_keys(step);
         request_values(step, step + WAVES);
     }
@@ -648,17 +652,17 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
     const uint32_t shift = a.s.page_shift, inside = (1u << shift) - 1;
     const uint32_t k_key = threadIdx.x / (DIM / 16), k_part = threadIdx.x % (DIM / 16), v_feature = threadIdx.x / 4, v_part = threadIdx.x % 4;
     AttendEntry k_entry[WIDE ? 1 : kItems], v_entry;
-    const auto find_key_pages = [&](uint32_t at) {
+    const auto find_key_pages = [&](uint32_t at, uint32_t zero) {
 #pragma unroll
         for (uint32_t i = 0; i < (WIDE ? 1 : kItems); ++i)
-            k_entry[i] = attend_ask<WIDE>(a.s, s, (at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) >> shift, at < last);
+            k_entry[i] = attend_ask(a.s, s, (at * kAttendStep + (WIDE ? 0 : k_key + i * kKeysApart)) >> shift, at < last, zero);
     };
     const auto find_value_pages = [&](uint32_t at) {
         const uint32_t v0 = at * kAttendStep + (WIDE ? 0 : v_part * 16);
         if constexpr (WIDE)
             v_entry = k_entry[0];
         else
-            v_entry = attend_ask<false>(a.s, s, v0 >> shift, at < last && v0 < range.high && v0 + 16 > range.low);
+            v_entry = attend_ask(a.s, s, v0 >> shift, at < last && v0 < range.high && v0 + 16 > range.low);
     };
     uint4 k_item[kItems], v_item[kItems];
     float k_scale[WIDE ? 1 : kItems], v_scale;
@@ -758,11 +762,11 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         most = attend_max_of_halves(most) * a.scale;
     };
     if (begin < last) {
-        find_key_pages(begin);
+        find_key_pages(begin, 0);
         find_value_pages(begin);
         request_keys(begin);
         request_values(begin);
-        find_key_pages(begin + 1);
+        find_key_pages(begin + 1, attend_zero());
         find_value_pages(begin + 1);
         put_keys(0);
         put_values(begin, 0);
@@ -776,7 +780,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         if (step + 1 < last) {
             request_keys(step + 1);
             request_values(step + 1);
-            find_key_pages(step + 2);
+            find_key_pages(step + 2, attend_zero());
             find_value_pages(step + 2);
         }
         __builtin_amdgcn_sched_barrier(0);
