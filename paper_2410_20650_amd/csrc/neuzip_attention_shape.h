@@ -28,10 +28,19 @@ struct AttendShape {
 };
 
 // Whether tiles of 128 rows, `tiles` of them with all heads, are taken rather than tiles of 32: a step costs less there and takes longer, so there
-// has to be enough work to fill the CUs.  us, tiles of 32 / 128: head_dim 128, 8 heads, prompts of 1024 tokens (256 tiles of up to 16 steps) 33 / 40, 2 of
-// 1024 46 / 42, 8 of 512 65 / 46, 512 tokens behind 7680 (128 tiles of 128 steps) 118 / 95, 16 parts of 64 behind 2000 99 / 105; head_dim 64, 2048
-// tokens (512 tiles) 44 / 54, 8 of 512 (822) 38 / 28, 4096 (1024) 129 / 107, 16 parts of 64 (402) 54 / 75.
-inline bool attend_is_large(uint32_t head_dim, uint64_t tiles, uint64_t steps) { return head_dim == 128 ? tiles * steps >= 4608 : tiles >= 700; }
+// has to be enough work for all CUs, either many tiles or, with heads of 128, few that look back far (their steps are split).  us, tiles of 32 / 128,
+// 32 query heads on 8:
+//   head_dim 128: prompts of 512 tokens (128 tiles of up to 8 steps) 12 / 18, 1024 (256 of 16) 28 / 31, 1280 (320) 38 / 39, 2048 (512) 68 / 60, 4 of 384
+//     (384 of 6) 31 / 21, 16 of 128 (512 of 2) 34 / 16;  256 tokens behind 7936 (64 of 128) 59 / 54, 512 behind 7680 (128 of 128) 95 / 88, but 128 behind
+//     8064 (32 of 128) 38 / 41 and 512 behind 3584 (128 of 64) 51 / 55
+//   head_dim 64: 1024 tokens (256 of 16) 17 / 23, 2048 (512 of 32) 38 / 43, 4096 (1024) 110 / 92;  4 of 384 (384 of 6) 17 / 15, 2 of 768 (384 of 12) 21 / 20,
+//     2 of 1024 (512 of 16) 28 / 29;  512 behind 7680 (128 of 128) 55 / 61
+inline bool attend_is_large(uint32_t head_dim, uint64_t tiles, uint64_t steps)
+{
+    if (head_dim == 128)
+        return tiles >= 320 || (steps >= 100 && tiles * steps >= 8192);
+    return tiles >= (steps <= 12 ? 384 : 700);
+}
 
 // heads: of the cache; count: sequences; longest: no sequence has more tokens
 inline AttendShape attend_shape(uint32_t heads, uint32_t head_dim, uint32_t count, uint32_t q_heads, uint32_t rows, uint32_t window, uint64_t longest)

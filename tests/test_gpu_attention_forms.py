@@ -20,12 +20,13 @@ CASES = {
     "some": (3, 5, 64, 16, 0, [(130, 700), (77, 77), (0, 40), (300, 301)]),
     "some, window": (2, 4, 128, 64, 100, [(230, 1700), (77, 77)]),
     "some, split": (2, 8, 128, 16, 0, [(33, 3333), (20, 2050)]),
-    "many": (8, 4, 128, 64, 0, [(700, 1100), (200, 200), (330, 1000)]),
-    "many, short pages": (8, 4, 128, 16, 0, [(700, 1100), (200, 200), (330, 1000)]),
+    "many": (8, 4, 128, 64, 0, [(800, 1100), (200, 200), (330, 1000)]),
+    "many, short pages": (8, 4, 128, 16, 0, [(800, 1100), (200, 200), (330, 1000)]),
     "many, small heads": (8, 5, 64, 32, 0, [(1600, 1600), (700, 900), (40, 41)]),
     "many, small heads, wide pages": (8, 5, 64, 128, 300, [(1600, 1600), (700, 900), (40, 41)]),
-    "many, split": (4, 3, 128, 128, 0, [(900, 5100), (1, 3000)]),
-    "many, split, short pages": (4, 3, 128, 32, 0, [(500, 5100), (0, 3000), (300, 4000)]),
+    "many, split": (4, 3, 128, 128, 0, [(900, 9100), (1, 3000)]),
+    "many, split, short pages": (4, 3, 128, 32, 0, [(600, 9100), (0, 3000), (300, 4000)]),
+    "many, small heads, short prompts": (8, 4, 64, 32, 0, [(400, 410), (380, 380), (500, 700), (600, 600)]),
     "many, window": (8, 4, 128, 64, 777, [(1000, 2300), (600, 600)]),
 }
 
