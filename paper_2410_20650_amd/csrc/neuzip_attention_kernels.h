@@ -10,7 +10,8 @@
 //
 // attend_few_kernel: a workgroup has up to 16 rows, its waves a step of 64 keys each in turn, keys and values from memory straight into registers; the
 // waves' sums are joined in LDS.  Work is split over the keys too where there are few rows, and joined by attend_join_kernel.
-// What bounds it: the bytes of the cache.
+// What bounds it: the bytes of the cache.  Measured, 32 query heads on 8 of 128: 32 sequences of 8192 tokens 93 us a call (5.8 TB/s), 48 of 2178 to 8192 108 (4.8: the
+// longest ones' workgroups end last), one of 32768 tokens 14.3 us and 4.6 for the join of its 32 splits.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -420,7 +421,9 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
 }
 
 // ---- some rows: the same with 32 rows to a workgroup, in matrix instructions of 32 x 32.  Here the lane (row c = l % 32, half h = l / 32) has of
-// every 32 keys the ones 16 h .. 16 h + 15; row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4.
+// every 32 keys the ones 16 h .. 16 h + 15; row c of 32 of the keys' operand is key 16 * (c / 4 % 2) + 4 * (c / 8) + c % 4.  What bounds it: the way from a page's number
+// to its bytes, a step or two after another for each wave.  Measured: 512 tokens, 32 query heads on 8 of 128, 11.6 us; 1405 of five sequences of 722 to 2011 tokens,
+// 15 heads on 3 of 64, a window of 256, 12.1.
 
 template <uint32_t DIM, bool WIDE>
 __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const AttendArgs a)
@@ -607,8 +610,10 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 // a feature, 64 keys in 8 pieces, in places p ^ feature / 2 % 8: the sixteen lanes that read together, 0 to 3, 12 to 15, 20 to 27 or the others, find different banks.
 // What bounds it: a step of a wave takes the matrix cores 1024 cycles (head_dim 128), the vector unit about 1450 (exponentials 512, the rest of the softmax
 // 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD and half of it overlaps.  A prompt of 4096 tokens, 32
-// query heads on 8, takes 164 us, 835 TFLOP/s.  A wave with 64 rows halves what LDS reads, but fills 400 registers and is alone on its SIMD: 350 us; with the
-// next step's products beside this step's exponentials in the program 169 us: 256 registers leave none for operands on their way.
+// query heads on 8, takes 159 us, 865 TFLOP/s (matrix cores busy 0.35 of the time, the vector unit 0.42), one of 16384 2.17 ms, 1010 TFLOP/s.  Without widening
+// into LDS it would take 126, without requests 149, without exponentials 146.  Tried: a wave with 64 rows halves what LDS reads, but fills 400 registers and is alone
+// on its SIMD, 350 us; the next step's products beside this step's exponentials in the program, 169 us, as 256 registers leave none for operands on their
+// way; the rows' sums by dot products or in the matrix cores, 178 and 186.
 constexpr int kSchedVector = 0x2, kSchedMatrix = 0x8, kSchedLds = 0x100;  // kinds of instructions (sched_group_barrier)
 
 template <uint32_t DIM, bool WIDE>

@@ -11,7 +11,8 @@ namespace nz {
 constexpr uint32_t kAttendFewRows = 16, kAttendSomeRows = 32, kAttendManyRows = 128;  // of a workgroup: a sequence's newest tokens times the query heads of a head
 constexpr uint32_t kAttendStep = 64;        // keys
 constexpr uint32_t kAttendCus = 256;
-constexpr uint32_t kAttendWaves = 2048;     // that a launch is split into, where its keys allow it: two to a SIMD
+// That a launch is split into, where its keys allow it: two to a SIMD.  (3072: 64 sequences of 4096 tokens 99 us, with 2048 93; 1 of 32768 18.1 and 18.5.)
+constexpr uint32_t kAttendWaves = 2048;
 constexpr uint32_t kAttendWaveSteps = 2;    // of each wave of a split at least, few and some rows
 constexpr uint32_t kAttendManySteps = 16;   // of a split at least, many rows
 constexpr uint32_t kAttendMostSplits = 128;
@@ -63,6 +64,7 @@ inline AttendShape attend_shape(uint32_t heads, uint32_t head_dim, uint32_t coun
     // workgroups that have something to do, about
     const uint64_t full = (all + tile - 1) / tile;
     const uint64_t wgs = (full > count ? full : count) * heads;
+    // (us, 8 waves / 4: 32 sequences of 8192 tokens, 256 workgroups, 94 / 99; 48 of 5232 99 / 96, 256 of 1024 108 / 96)
     shape.waves = tile == kAttendFewRows && wgs <= kAttendCus ? 8 : 4;
     shape.least_steps = tile == kAttendManyRows ? kAttendManySteps : kAttendWaveSteps * shape.waves;
     const uint64_t wanted = (kAttendWaves + wgs * shape.waves - 1) / (wgs * shape.waves), most = keys / (kAttendStep * shape.least_steps);

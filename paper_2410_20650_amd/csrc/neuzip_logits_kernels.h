@@ -4,6 +4,8 @@
 // occurs in the row's history, and finds the last bias entry of each; both with integer atomics, whose order does not show.  Every workgroup of a
 // row reads the whole history (8 bytes a token, from the second one on out of a cache), which is why a slice is not shorter than it has to be for
 // all CUs to have one.  What bounds it: reading and writing the logits once; for one row, the launch and the history's way through the caches.
+// Measured, 128256 tokens: 48 rows with up to 4000 tokens of history 15.3 us (57 MB, 3.7 TB/s: a third of the workgroups start when the others have ended, and
+// first read their history), one row with 1000 3.4 us.
 #pragma once
 
 #include <hip/hip_runtime.h>

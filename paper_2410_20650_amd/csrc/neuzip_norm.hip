@@ -28,6 +28,7 @@ void launch_norm_as(const NormArgs &a, hipStream_t stream)
     hipLaunchKernelGGL((norm_kernel<THREADS, PIECES, X, STREAM, T>), dim3((a.tokens + rows - 1) / rows), dim3(threads), 0, stream, a);
 }
 
+// us, a wave / 256 lanes to a row: 4096 rows of 512 4.4 / 5.5, 32768 of them 26.6 / 34.5; 333 rows of 1024 2.8 / 2.5 and 4096 of them 7.1 / 7.9.
 template <class X, bool STREAM, class T>
 void launch_norm(const NormArgs &a, hipStream_t stream)
 {

@@ -67,7 +67,7 @@ def case(rows, vocab, seed, history, bias):
 
 
 @pytest.mark.parametrize("history, bias", [(0, 0), (1, 1), (40, 5), (3000, 300)])
-@pytest.mark.parametrize("rows, vocab", [(1, 1), (2, 31), (5, 1000), (3, 1024), (7, 4097), (1, 128256), (6, 50257), (70, 2049)])
+@pytest.mark.parametrize("rows, vocab", [(1, 1), (2, 31), (5, 1000), (3, 1024), (7, 4097), (1, 128256), (6, 50257), (70, 2049), (22, 50257), (9, 128256)])
 def test_everything(nz, rows, vocab, history, bias):
     logits, histories, (repetition, frequency, presence), biases, masks, ids = case(rows, vocab, 3, history, bias)
     tokens, starts = ragged(histories, torch.int64)
