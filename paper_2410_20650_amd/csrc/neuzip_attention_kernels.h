@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 // a feature, 64 keys in 8 pieces, in places p ^ feature / 2 % 8: the sixteen lanes that read together, 0 to 3, 12 to 15, 20 to 27 or the others, find different banks.
 // What bounds it: a step of a wave takes the matrix cores 1024 cycles (head_dim 128), the vector unit about 1450 (exponentials 512, the rest of the softmax
 // 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD and half of it overlaps.  A prompt of 4096 tokens, 32
-// query heads on 8, takes 159 us, 865 TFLOP/s (matrix cores busy 0.35 of the time, the vector unit 0.42), one of 16384 2.17 ms, 1010 TFLOP/s.  Without widening
+// query heads on 8, takes 159 us, 865 TFLOP/s (matrix cores busy a third of the time, the vector unit 0.4 of it), one of 16384 2.17 ms, 1010 TFLOP/s.  Without widening
 // into LDS it would take 126, without requests 149, without exponentials 146.  Tried: a wave with 64 rows halves what LDS reads, but fills 400 registers and is alone
 // on its SIMD, 350 us; the next step's products beside this step's exponentials in the program, 169 us, as 256 registers leave none for operands on their
 // way; the rows' sums by dot products or in the matrix cores, 178 and 186.

@@ -11,7 +11,7 @@ namespace nz {
 constexpr uint32_t kAttendFewRows = 16, kAttendSomeRows = 32, kAttendManyRows = 128;  // of a workgroup: a sequence's newest tokens times the query heads of a head
 constexpr uint32_t kAttendStep = 64;        // keys
 constexpr uint32_t kAttendCus = 256;
-// That a launch is split into, where its keys allow it: two to a SIMD.  (3072: 64 sequences of 4096 tokens 99 us, with 2048 93; 1 of 32768 18.1 and 18.5.)
+// That a launch is split into, where its keys allow it: two to a SIMD.  (4096: 64 sequences of 4096 tokens 99 us, with 2048 93; 48 of 2178 to 8192 113 and 108.)
 constexpr uint32_t kAttendWaves = 2048;
 constexpr uint32_t kAttendWaveSteps = 2;    // of each wave of a split at least, few and some rows
 constexpr uint32_t kAttendManySteps = 16;   // of a split at least, many rows

@@ -8,8 +8,8 @@
 // THREADS lanes share a row: a wave where the rows are short or many, so that its sums need neither LDS nor a barrier; else a workgroup.
 // The backward pass keeps w and the lane's part of dw in registers over all rows that a workgroup takes; the parts of a workgroup's rows
 // are added in LDS, those of the workgroups by a launch of its own, in order, so that dw is the same every time.
-// Measured, float32 results onto a bf16 stream of width 4096: 4096 tokens 24.9 us (168 MB, 6.7 TB/s), 2048 tokens 13.0 us, their backward pass 13.9 (67 MB and
-// 4 MB of parts, 5.1 TB/s) and 4.7 for the parts; one token 2.7 us, a launch.
+// Measured, float32 results onto a bf16 stream of width 4096: 4096 tokens 27.4 us from memory (168 MB, 6.1 TB/s), 2048 tokens 15.6, their backward pass 16.0 (67 MB and
+// 4 MB of parts, 4.5 TB/s) and 4.0 for the parts; one token 2.5 us, a launch.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kNormBackThreads) norm_back_kernel(const NormB
 }
 
 // dw: the sum of `count` rows of `width` floats, kNormJoinColumns columns to a workgroup, 64 runs of rows side by side.  (Its time is one way to
-// memory and back: 256 rows of 4096 in 4.7 us, 84 of 1160 in 2.7.)
+// memory and back: 256 rows of 4096 in 4.0 us, 84 of 1160 in 2.8.)
 inline __global__ void __launch_bounds__(256) norm_join_kernel(const float *parts, float *grad_weight, uint32_t count, uint32_t width)
 {
     __shared__ float4 sums[4][kNormJoinColumns / 4];
