@@ -187,6 +187,8 @@ class CompressedAttention:
     def forward(self, x: torch.Tensor, cache: nz.KeyValueCache, sequences: nz.Sequences, space: torch.Tensor, longest: int = 0) -> torch.Tensor:
         """x: rows x in_features, bf16, the newest tokens of the sequences, whose lengths count them already.  They are put into the cache and look back at
         it.  Returns float32 rows x out_features."""
+        if x.shape[0] == 0:
+            return torch.empty((0, self.out.out_features), dtype=torch.float32, device=x.device)
         parts = (self.queries, self.keys, self.values)
         if x.shape[0] <= 64 and self.queries.in_features % 128 == 0:     # (one launch for the three)
             q, k, v = nz.neuzip_linear_batch([p.blob for p in parts], [p.out_features for p in parts], self.queries.in_features, x.contiguous())
@@ -194,7 +196,7 @@ class CompressedAttention:
             q, k, v = (p.forward(x, space) for p in parts)
         turned = nz.neuzip_cache_append(cache, sequences, k, v, q, self.rotary)
         seen = nz.neuzip_cache_attention(cache, sequences, turned, window=self.window, longest=longest)
-        return self.out.forward(seen.view(x.shape[0], -1), space)
+        return self.out.forward(seen.view(x.shape[0], self.out.in_features), space)
 
 
 def training_step(layers, x: torch.Tensor, target: torch.Tensor, lr: float, space: torch.Tensor,

@@ -113,6 +113,8 @@ class SmallDecoder:
         has already is penalised by.  bias: (tokens, values) for every sequence.  allowed: a mask of ceil(rows / 32) words (int32) that all obey."""
         count, device = len(prompts), self.device
         lengths = [p.numel() for p in prompts]
+        if not lengths or min(lengths) == 0:
+            raise ValueError("an answer needs a prompt of at least one token")
         pages = (max(lengths) + steps + page_tokens - 1) // page_tokens
         if pages * page_tokens > self.positions:
             raise ValueError("prompts and answers need more positions than there are angles for")

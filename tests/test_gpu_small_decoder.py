@@ -140,3 +140,15 @@ def test_layers_refuse_what_they_cannot_hold():
     for i, bad in ((0, (192, 256)), (1, (100, 256)), (2, (64, 256)), (3, (256, 128))):
         with pytest.raises(ValueError):
             CompressedAttention(*[inputs.gaussian_bf16(bad, 990, device=DEV) if j == i else t for j, t in enumerate(w)], 64)
+
+
+def test_no_rows_and_no_prompt(nz):
+    from paper_2410_20650_amd.small_model import SmallDecoder
+    decoder = SmallDecoder(rows=100, layers=1)
+    attention = decoder.layers[0][1]
+    nobody = nz.Sequences(ints([0, 0]), ints([0]), ints([[0]]))
+    none = torch.empty((0, 256), dtype=torch.bfloat16, device=DEV)
+    assert attention.forward(none, attention.new_cache(1, 64, DEV), nobody, decoder.space).shape == (0, 256)
+    for prompts in ([], [torch.arange(3, device=DEV), torch.arange(0, device=DEV)]):
+        with pytest.raises(ValueError):
+            decoder.answer(prompts, 2)
