@@ -214,6 +214,13 @@ def test_long_ones(nz, counts, lengths, q_heads, dim, page):
     check_attention(nz, cache, plain, table, counts, lengths, q_heads, seed=42, window=1000)
 
 
+@pytest.mark.parametrize("window", [3000, 4097])
+@pytest.mark.parametrize("counts, lengths, q_heads", [([1], [9001], 8), ([3], [7333], 4), ([40], [6500], 8), ([1, 2], [8000, 3111], 2)])
+def test_windows_that_are_split(nz, counts, lengths, q_heads, window):
+    cache, plain, table = filled(nz, lengths, 2, 64, 64, seed=43)
+    check_attention(nz, cache, plain, table, counts, lengths, q_heads, seed=44, window=window)
+
+
 @pytest.mark.parametrize("count", [63, 64, 65, 200])
 @pytest.mark.parametrize("group", [1, 20])
 def test_many_sequences(nz, count, group):
