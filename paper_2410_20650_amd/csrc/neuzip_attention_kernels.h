@@ -604,23 +604,23 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
     attend_leave<DIM, WAVES, kAttendSomeRows>(a, n, head, split, row0, row_end, sums, stats);
 }
 
-// ---- many rows: a wave has 32 rows, a workgroup 128.  A step's keys and values are widened once, by all four waves, into LDS, from where every wave reads
+// ---- many rows: a wave has 32 rows, a workgroup 128 or 256.  A step's keys and values are widened once, by all waves, into LDS, from where every wave reads
 // them as operands; the next step's bytes are on their way meanwhile, and the pages of the one behind it.  Lanes hold keys as above.
 // In LDS: row c of 32 of the keys' operand, its pieces of 16 bytes (8 features) in places p ^ c % 16 (rows of 128 bytes: p ^ c / 2 % 8); the values' row is
 // a feature, 64 keys in 8 pieces, in places p ^ feature / 2 % 8: the sixteen lanes that read together, 0 to 3, 12 to 15, 20 to 27 or the others, find different banks.
 // What bounds it: a step of a wave takes the matrix cores 1024 cycles (head_dim 128), the vector unit about 1450 (exponentials 512, the rest of the softmax
 // 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD and half of it overlaps.  A prompt of 4096 tokens, 32
-// query heads on 8, takes 159 us, 865 TFLOP/s (matrix cores busy a third of the time, the vector unit 0.4 of it), one of 16384 2.17 ms, 1010 TFLOP/s.  Without widening
-// into LDS it would take 126, without requests 149, without exponentials 146.  Tried: a wave with 64 rows halves what LDS reads, but fills 400 registers and is alone
-// on its SIMD, 350 us; the next step's products beside this step's exponentials in the program, 169 us, as 256 registers leave none for operands on their
-// way; the rows' sums by dot products or in the matrix cores, 178 and 186.
+// query heads on 8, takes 151 us with 256 rows to a workgroup (911 TFLOP/s), 159 with 128 (matrix cores busy a third of the time, the vector unit 0.4 of it); one of 16384
+// 2.13 ms, 1030 TFLOP/s.  With 128 rows it would take 126 without widening into LDS, 149 without requests, 146 without exponentials.  Tried: a wave with 64 rows halves
+// what LDS reads, but fills 400 registers and is alone on its SIMD, 350 us; the next step's products beside this step's exponentials in the program, 169 us, as
+// 256 registers leave none for operands on their way; the rows' sums by dot products or in the matrix cores, 178 and 186.
 constexpr int kSchedVector = 0x2, kSchedMatrix = 0x8, kSchedLds = 0x100;  // kinds of instructions (sched_group_barrier)
 
-template <uint32_t DIM, bool WIDE>
-__global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const AttendArgs a)
+template <uint32_t DIM, bool WIDE, uint32_t WAVES>
+__global__ void __launch_bounds__(WAVES * 64, 2) attend_many_kernel(const AttendArgs a)
 {
     constexpr uint32_t kPieces = DIM / 8, kBytes = kAttendStep * DIM * 2;
-    constexpr uint32_t kItems = kAttendStep * DIM / 16 / kAttendThreads;  // 16 bytes of the cache, of keys and of values, to a thread
+    constexpr uint32_t kRows = WAVES * 32, kItems = kAttendStep * DIM / 16 / (WAVES * 64);  // 16 bytes of the cache, of keys and of values, to a thread
     constexpr uint32_t kKeysApart = kAttendStep / kItems, kFeaturesApart = DIM / kItems;
     __shared__ __align__(16) uint8_t key_space[2][kBytes];
     __shared__ __align__(16) uint8_t value_space[2][kBytes];
@@ -631,11 +631,11 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_many_kernel(const At
         return;
     const uint32_t s = at.s;
     const NewTokens n = at.n;
-    const uint64_t row0_wide = at.tile * kAttendManyRows;
+    const uint64_t row0_wide = at.tile * kRows;
     const uint32_t rows = n.count * a.group;
     if (row0_wide >= rows)
         return;
-    const uint32_t row0 = static_cast<uint32_t>(row0_wide), row_end = rows - row0 < kAttendManyRows ? rows : row0 + kAttendManyRows;
+    const uint32_t row0 = static_cast<uint32_t>(row0_wide), row_end = rows - row0 < kRows ? rows : row0 + kRows;
     const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64, c = lane % 32, h = lane / 32;
     const AttendRange range = attend_range(n, row0 / a.group, (row_end - 1) / a.group, a.window);
     uint32_t begin, last;

@@ -63,7 +63,7 @@ void launch_append(const AppendArgs &a, uint32_t wgs, hipStream_t stream)
 inline AttendShape shape_of(const neuzip_cache *c, const neuzip_sequences *s, uint32_t q_heads, uint32_t rows, uint32_t window, uint64_t longest)
 {
     const uint64_t room = static_cast<uint64_t>(s->table_width) << page_shift(c);
-    return attend_shape(c->heads, c->head_dim, s->count, q_heads, rows, window, longest && longest < room ? longest : room);
+    return attend_shape(c->heads, c->head_dim, c->page_tokens, s->count, q_heads, rows, window, longest && longest < room ? longest : room);
 }
 
 inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_heads > 0 && q_heads % c->heads == 0; }
@@ -71,8 +71,11 @@ inline bool valid_heads(const neuzip_cache *c, uint32_t q_heads) { return q_head
 template <uint32_t DIM, bool WIDE>
 void launch_attend_as(const AttendArgs &a, const AttendShape &shape, uint32_t wgs, hipStream_t stream)
 {
-    if (shape.rows == kAttendManyRows)
-        hipLaunchKernelGGL((attend_many_kernel<DIM, WIDE>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
+    if (shape.rows == kAttendHugeRows) {
+        if constexpr (WIDE && DIM == 128)  // (the rule's only case)
+            hipLaunchKernelGGL((attend_many_kernel<DIM, WIDE, 8>), dim3(wgs), dim3(512), 0, stream, a);
+    } else if (shape.rows == kAttendManyRows)
+        hipLaunchKernelGGL((attend_many_kernel<DIM, WIDE, 4>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
     else if (shape.rows == kAttendSomeRows)
         hipLaunchKernelGGL((attend_some_kernel<DIM, WIDE>), dim3(wgs), dim3(kAttendThreads), 0, stream, a);
     else if (shape.waves == 8)

@@ -31,7 +31,7 @@ def taken(ask):
     found = {}
     for name, (heads, group, dim, page, window, plan) in forms_of.CASES.items():
         rows, longest = sum(n for n, _ in plan) + 5, (max((n + page - 1) // page for _, n in plan) + 1) * page
-        ((tile, waves, splits),) = ask([(heads, dim, len(plan), heads * group, rows, window, longest)])
+        ((tile, waves, splits),) = ask([(heads, dim, page, len(plan), heads * group, rows, window, longest)])
         found.setdefault((dim, tile, waves, splits > 1, page >= 64 if tile == 128 else None), []).append(name)
     return found
 
@@ -42,15 +42,17 @@ def test_every_form_is_taken(ask):
     for dim in (64, 128):
         for form in ((16, 8, None), (16, 4, None), (32, 4, None), (128, 4, False), (128, 4, True)):
             assert (dim, *form) in kernels, (dim, form, found)
-    for tile, waves in ((16, 8), (16, 4), (32, 4), (128, 4)):
+    assert (128, 256, 8, None) in kernels
+    for tile, waves in ((16, 8), (16, 4), (32, 4), (128, 4), (256, 8)):
         for split in (False, True):
             assert any(f[1:4] == (tile, waves, split) for f in found), (tile, waves, split)
 
 
 def test_the_rule(ask):
     """Any call has a form, and its splits are no more than there are keys for."""
-    calls = [(h, d, s, h * g, r, w, n) for h in (1, 8) for d in (64, 128) for s in (1, 48) for g in (1, 4, 17) for r in (1, 16, 500, 9000) for w in (0, 1, 300)
+    calls = [(h, d, p, s, h * g, r, w, n) for h in (1, 8) for d in (64, 128) for p in (16, 64) for s in (1, 48) for g in (1, 4, 17) for r in (1, 16, 500, 9000) for w in (0, 1, 300)
              for n in (16, 1000, 100000)]
     for call, (tile, waves, splits) in zip(calls, ask(calls)):
-        assert (tile, waves) in ((16, 4), (16, 8), (32, 4), (128, 4)) and 1 <= splits <= 128
-        assert splits == 1 or splits * 64 * 8 <= call[6]
+        assert (tile, waves) in ((16, 4), (16, 8), (32, 4), (128, 4), (256, 8)) and 1 <= splits <= 128
+        assert splits == 1 or splits * 64 * 8 <= call[7]
+        assert tile < 256 or (call[1] == 128 and call[2] >= 64)     # (the only ones that there is a kernel for)

@@ -24,8 +24,11 @@ CASES = {
     "many, short pages": (8, 4, 128, 16, 0, [(800, 1100), (200, 200), (330, 1000)]),
     "many, small heads": (8, 5, 64, 32, 0, [(1600, 1600), (700, 900), (40, 41)]),
     "many, small heads, wide pages": (8, 5, 64, 128, 300, [(1600, 1600), (700, 900), (40, 41)]),
-    "many, split": (4, 3, 128, 128, 0, [(900, 9100), (1, 3000)]),
+    "many, split": (4, 8, 128, 128, 0, [(1300, 2500), (100, 900)]),
     "many, split, short pages": (4, 3, 128, 32, 0, [(600, 9100), (0, 3000), (300, 4000)]),
+    "most": (8, 4, 128, 64, 0, [(3300, 3300), (900, 900)]),
+    "most, split": (4, 4, 128, 128, 0, [(500, 9100), (0, 70), (300, 4000)]),
+    "most, window": (8, 4, 128, 64, 3111, [(3500, 4200), (1, 1), (700, 900)]),
     "many, small heads, short prompts": (8, 4, 64, 32, 0, [(400, 410), (380, 380), (500, 700), (600, 600)]),
     "many, window": (8, 4, 128, 64, 777, [(1000, 2300), (600, 600)]),
 }
