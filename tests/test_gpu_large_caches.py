@@ -28,8 +28,8 @@ def normal(*shape, seed, dtype=BF):
 
 
 def test_pages_behind_32_bits(nz):
-    """Every form of the attention's kernels (one token, 130, 1100 of a sequence) on either content."""
-    heads, group, page, dim, pages, length = 8, 4, 64, 128, 70000, 1100
+    """Every form of the attention's kernels (one token, 130, 1400, 4200 of a sequence) on either content."""
+    heads, group, page, dim, pages, length = 8, 4, 64, 128, 70000, 4200
     assert pages * heads * page * dim > MANY and (pages - 100) * heads * page * dim > MANY
     cache = nz.KeyValueCache.empty(pages, heads, dim, page)
     need = (length + page - 1) // page
@@ -38,9 +38,9 @@ def test_pages_behind_32_bits(nz):
     q = normal(length, heads * group, dim, seed=3)
     outs = {}
     for name, place in places.items():
-        for begin, end in ((0, 700), (700, length)):    # (the page between them twice)
+        for begin, end in ((0, 2900), (2900, length)):    # (the page between them twice)
             nz.neuzip_cache_append(cache, nz.Sequences(ints([0, end - begin]), ints([end]), ints([place])), k[begin:end], v[begin:end])
-        outs[name] = [nz.neuzip_cache_attention(cache, nz.Sequences(ints([0, n]), ints([length]), ints([place])), q[length - n:]) for n in (1, 130, length)]
+        outs[name] = [nz.neuzip_cache_attention(cache, nz.Sequences(ints([0, n]), ints([length]), ints([place])), q[length - n:]) for n in (1, 130, 1400, length)]
     first, last = (torch.tensor(places[name], device=DEV) for name in ("first", "last"))
     filled = torch.arange(need * page, device=DEV) < length
     for held in (cache.k.view(torch.uint8).transpose(2, 3), cache.v.view(torch.uint8)):
