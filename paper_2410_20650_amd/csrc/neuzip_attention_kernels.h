@@ -613,7 +613,8 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 // query heads on 8, takes 151 us with 256 rows to a workgroup (911 TFLOP/s), 159 with 128 (matrix cores busy a third of the time, the vector unit 0.4 of it); one of 16384
 // 2.13 ms, 1030 TFLOP/s.  With 128 rows it would take 126 without widening into LDS, 149 without requests, 146 without exponentials.  Tried: a wave with 64 rows halves
 // what LDS reads, but fills 400 registers and is alone on its SIMD, 350 us; the next step's products beside this step's exponentials in the program, 169 us, as
-// 256 registers leave none for operands on their way; the rows' sums by dot products or in the matrix cores, 178 and 186.
+// 256 registers leave none for operands on their way; the rows' sums by dot products or in the matrix cores, 178 and 186;
+// the workgroup's halves a phase apart, one at products while the other is at weights, with a barrier to each phase, 151 to 162 against 148 on the same card.
 constexpr int kSchedVector = 0x2, kSchedMatrix = 0x8, kSchedLds = 0x100;  // kinds of instructions (sched_group_barrier)
 
 template <uint32_t DIM, bool WIDE, uint32_t WAVES>
