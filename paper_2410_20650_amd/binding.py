@@ -839,9 +839,22 @@ def neuzip_norm_backward(total: torch.Tensor, weight: torch.Tensor, grad_y: torc
     return grad_x, grad_weight
 
 
-class KeyValueCache:
+class _Fixed:
+    """What is set once, stays: the library is given the addresses that the tensors had then."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__:
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be replaced: make another {type(self).__name__}")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{type(self).__name__}.{name} cannot be removed")
+
+
+class KeyValueCache(_Fixed):
     """The keys and values of tokens so far, in 8 bits (neuzip_cache).  k: pages x heads x page_tokens x head_dim, v: pages x heads x head_dim x
-    page_tokens (torch.float8_e4m3fn), k_scales, v_scales: pages x heads (float32, powers of two)."""
+    page_tokens (torch.float8_e4m3fn), k_scales, v_scales: pages x heads (float32, powers of two).  The tensors stay the cache's; what they hold may
+    change."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor):
         if k.dim() != 4:
@@ -870,9 +883,10 @@ class KeyValueCache:
                    *(torch.empty((pages, heads), dtype=torch.float32, device=device) for _ in range(2)))
 
 
-class Sequences:
+class Sequences(_Fixed):
     """The ragged sequences of a call (neuzip_sequences), int32: starts (sequences + 1: whose rows are whose), lengths (tokens of each, with the rows'),
-    table (sequences x pages of each, in order).  The tensors may change between calls; they are read when a call's work runs."""
+    table (sequences x pages of each, in order).  What the tensors hold may change between calls, and is read when a call's work runs; they
+    themselves cannot be replaced."""
 
     def __init__(self, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
         if table.dim() != 2:
