@@ -743,6 +743,13 @@ def _here(t, dtype, shape, what, device):
     return t
 
 
+def _word(n, what):
+    """n, which the library takes in 32 bits.  (ctypes cuts off what is beyond them, and a part of the work would be done.)"""
+    if n >> 32:
+        raise ValueError(f"{n} {what}: more than the library counts")
+    return n
+
+
 def _scratch_here(size, scratch, t, device, stream):
     if size == 0 and scratch is None:
         return None
@@ -891,7 +898,7 @@ class Sequences(_Fixed):
     def __init__(self, starts: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor):
         if table.dim() != 2:
             raise ValueError("table must be sequences x pages")
-        count, width = table.shape
+        count, width = _word(table.shape[0], "sequences"), _word(table.shape[1], "pages of a sequence")
         _expect(table, torch.int32, (count, width), "table")
         _expect(starts, torch.int32, (count + 1,), "starts")
         _expect(lengths, torch.int32, (count,), "lengths")
@@ -1011,13 +1018,14 @@ def neuzip_logits(logits: torch.Tensor, history: torch.Tensor = None, history_st
     if logits.dim() != 2:
         raise ValueError("logits must be rows x vocab")
     rows, vocab = logits.shape
+    _word(rows, "rows")
     if (history is None) != (history_starts is None) or not (bias is None) == (bias_values is None) == (bias_starts is None):
         raise ValueError("tokens come with their starts, biases with their values")
     if (masks is None) != (mask_ids is None):
         raise ValueError("masks and mask_ids come together")
     history_tokens = history.numel() if history is not None else 0
     entries = bias.numel() if bias is not None else 0
-    count = masks.shape[0] if masks is not None and masks.dim() else 0
+    count = _word(masks.shape[0], "masks") if masks is not None and masks.dim() else 0
     if out is None:
         out = _empty_like(logits, torch.float32, stream)
     f32, i32, i64, one, behind = torch.float32, torch.int32, torch.int64, (rows,), (rows + 1,)
