@@ -21,11 +21,25 @@ inline bool valid_type(int t) { return t == NEUZIP_F32 || t == NEUZIP_BF16; }
 inline bool valid_width(uint64_t w) { return w > 0 && w % 8 == 0 && w <= kNormWidest; }
 inline bool valid_eps(float eps) { return eps >= 0.0f; }  // (no NaN)
 
+// A launch has fewer than 2^32 threads: with 1024 to a row, 2^22 tokens and more are several.
 template <int THREADS, int PIECES, class X, bool STREAM, class T>
 void launch_norm_as(const NormArgs &a, hipStream_t stream)
 {
     constexpr uint32_t threads = THREADS > static_cast<int>(kNormThreads) ? THREADS : kNormThreads, rows = threads / THREADS;
-    hipLaunchKernelGGL((norm_kernel<THREADS, PIECES, X, STREAM, T>), dim3((a.tokens + rows - 1) / rows), dim3(threads), 0, stream, a);
+    constexpr uint32_t most = ((1ull << 32) / threads - 1) * rows;
+    static_assert(too_many_wgs(most / rows + 1, threads) && !too_many_wgs(most / rows, threads) && (threads > kNormThreads || most >= kNormMostTokens - 1));
+    for (uint32_t first = 0; first < a.tokens; first += most) {
+        const uint64_t at = static_cast<uint64_t>(first) * a.width;
+        NormArgs part = a;
+        part.x = static_cast<const X *>(a.x) + at;
+        part.y = a.y + at;
+        if constexpr (STREAM) {
+            part.residual = static_cast<const T *>(a.residual) + at;
+            part.total = static_cast<T *>(a.total) + at;
+        }
+        part.tokens = a.tokens - first < most ? a.tokens - first : most;
+        hipLaunchKernelGGL((norm_kernel<THREADS, PIECES, X, STREAM, T>), dim3((part.tokens + rows - 1) / rows), dim3(threads), 0, stream, part);
+    }
 }
 
 // us, a wave / 256 lanes to a row: 4096 rows of 512 4.4 / 5.5, 32768 of them 26.6 / 34.5; 333 rows of 1024 2.8 / 2.5 and 4096 of them 7.1 / 7.9.
@@ -105,8 +119,7 @@ int neuzip_norm(const void *d_x, int x_type, const void *d_residual, void *d_tot
     for (const void *p : pointers)
         if (misaligned(p))
             return NEUZIP_EINVAL;
-    // (a workgroup of 256 lanes to a row: fewer than 2^32 threads)
-    if (tokens >= kNormMostTokens || too_many_wgs(tokens, width > 8192 ? 1024 : kNormThreads))
+    if (tokens >= kNormMostTokens)
         return NEUZIP_EUNSUPPORTED;
     NormArgs a;
     a.x = d_x;
