@@ -545,6 +545,7 @@ int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *seque
  *
  *   d_q, q_row  rows x q_heads x head_dim bf16 words, q_row elements from one row to the next (a multiple of 8).  q_heads is a multiple of the cache's heads;
  *               query head h reads the cache's head h / (q_heads / heads).
+ *   scale       above 0 and, times log2(e), within binary32: below 2.35e38 (else EINVAL).
  *   window      0: none.
  *   longest     no sequence has more tokens; 0: table_width * page_tokens.  (It decides how the work is split, so it may be too high, not too low:
  *               results are the same but for the order of sums.)

@@ -17,6 +17,7 @@ using namespace nz;
 namespace {
 
 constexpr uint64_t kAttendMostRows = 1ull << 27;  // rows times query heads
+constexpr float kLog2e = 1.4426950408889634f;
 
 inline bool off(const void *p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) & (size - 1); }
 
@@ -174,7 +175,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
                            uint32_t rows, float scale, uint32_t window, uint64_t longest, void *d_out, void *d_scratch,
                            uint64_t scratch_bytes, void *hip_stream)
 {
-    if (!valid_cache(cache) || !valid_sequences(cache, sequences) || !valid_heads(cache, q_heads) || !(scale > 0.0f) || !std::isfinite(scale))
+    if (!valid_cache(cache) || !valid_sequences(cache, sequences) || !valid_heads(cache, q_heads) || !(scale > 0.0f) || !std::isfinite(scale * kLog2e))
         return NEUZIP_EINVAL;
     if (rows == 0 || sequences->count == 0)
         return NEUZIP_OK;
@@ -204,7 +205,7 @@ int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *se
     a.numbers = shape.numbers;
     a.most_keys = shape.keys;
     a.least_steps = shape.least_steps;
-    a.scale = scale * 1.4426950408889634f;
+    a.scale = scale * kLog2e;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const uint32_t grid = static_cast<uint32_t>(wgs);
     return cache->head_dim == 64 ? launch_attend<64>(a, shape, grid, stream) : launch_attend<128>(a, shape, grid, stream);
