@@ -23,7 +23,9 @@
 namespace nz {
 
 constexpr uint32_t kAttendThreads = 256;
-constexpr float kAttendSlack = 6.0f;      // a row's weights may exceed 1 by so much (a factor of 64) before its sums are scaled down to a new maximum
+// A row's weights may exceed 1 by so much (a factor of 64) before its sums are scaled down to a new maximum.  Each row goes by its own keys: were it scaled whenever
+// another one of its wave is, its last bits would hang on keys that it does not see.
+constexpr float kAttendSlack = 6.0f;
 
 struct AttendArgs {
     SequencesView s;
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(WAVES * 64, 3) attend_few_kernel(const AttendA
         most = fmaxf(most, __shfl_xor(most, 32));
         most *= a.scale;
         if (__any(most > top + kAttendSlack)) {
-            const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+            const float higher = most > top + kAttendSlack ? most : top, less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
             top = higher;
             total *= less;
 #pragma unroll
@@ -552,7 +554,7 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
                 most = fmaxf(most, score[x][e]);
         most = attend_max_of_halves(most) * a.scale;
         if (__any(most > top + kAttendSlack)) {
-            const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+            const float higher = most > top + kAttendSlack ? most : top, less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
             top = higher;
             total *= less;
 #pragma unroll
@@ -804,7 +806,7 @@ __global__ void __launch_bounds__(WAVES * 64, 2) attend_many_kernel(const Attend
         __builtin_amdgcn_sched_barrier(0);
         look(now, step, turn);
         if (__any(most > top + kAttendSlack)) {
-            const float higher = fmaxf(top, most), less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
+            const float higher = most > top + kAttendSlack ? most : top, less = higher == -__builtin_inff() ? 1.0f : attend_exp2(top - higher);
             top = higher;
             total *= less;
 #pragma unroll
