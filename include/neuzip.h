@@ -532,6 +532,7 @@ typedef struct {
  *   rows        of the tensors.
  * A page that is appended to belongs to one sequence, once in its table, and to no other call at that time.  A left-out sequence's rows of q_out
  * are zeros.  All pointers to values are aligned to 16 bytes.
+ * heads from 2^16 on, and calls of (rows / page_tokens + 2 * count) * 2 * heads (and rows, with queries) from 2^24 on -> EUNSUPPORTED.
  * Never allocates, never synchronises; results do not change from run to run.
  */
 int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *sequences, int type, const void *d_k, uint64_t k_row,
@@ -554,7 +555,8 @@ int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *seque
  *               work has run (NULL where that is 0).
  * Keys and values are taken as the cache holds them; scores, maxima, sums and the output's sums are binary32, the weights of the softmax are
  * rounded to bf16 for the matrix cores (each by at most 2^-8 of itself; their sum is that of the unrounded ones), out is rounded once.  A key that a token does not see has no influence, whatever
- * it holds.  rows * q_heads up to 2^27 - 1 (else EUNSUPPORTED).  Never allocates, never synchronises; results do not change from run to run.
+ * it holds.  rows * q_heads up to 2^27 - 1, and fewer than 2^23 workgroups, of which single
+ * tokens take one for each sequence, head and 16 query heads of it (else EUNSUPPORTED).  Never allocates, never synchronises; results do not change from run to run.
  */
 int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *sequences, const void *d_q, uint64_t q_row, uint32_t q_heads,
                            uint32_t rows, float scale, uint32_t window, uint64_t longest, void *d_out, void *d_scratch,
