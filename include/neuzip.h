@@ -567,8 +567,8 @@ uint64_t neuzip_cache_attention_scratch_bytes(const neuzip_cache *cache, const n
 /*
  * neuzip_logits -- what is done to the output projection's result before a token is taken from it, row by row.  With c = how often a token
  * occurs in the row's history, for each of them in this order:
- *     c > 0:  x <- x > 0 ? x / repetition : x * repetition;   x <- x - frequency * c;   c > 0:  x <- x - presence;
- *     x <- x + its bias;   not allowed by the row's mask:  x <- -infinity
+ *     where c > 0:  x <- x > 0 ? x / repetition : x * repetition,  x <- x - frequency * c,  x <- x - presence;
+ *     where it has one:  x <- x + its bias;   not allowed by the row's mask:  x <- -infinity
  *
  *   d_logits, d_out   rows x vocab floats, row-major; d_out may be d_logits.
  *   history     d_tokens[d_starts[r]] .. d_tokens[d_starts[r + 1] - 1] is row r's, 64-bit integers (a number outside 0 .. vocab - 1 counts for
