@@ -554,9 +554,12 @@ int neuzip_cache_append(const neuzip_cache *cache, const neuzip_sequences *seque
  *   d_scratch   device buffer of scratch_bytes bytes, at least neuzip_cache_attention_scratch_bytes(), 16-byte aligned, in use until the call's
  *               work has run (NULL where that is 0).
  * Keys and values are taken as the cache holds them; scores, maxima, sums and the output's sums are binary32, the weights of the softmax are
- * rounded to bf16 for the matrix cores (each by at most 2^-8 of itself; their sum is that of the unrounded ones), out is rounded once.  A key that a token does not see has no influence, whatever
- * it holds.  rows * q_heads up to 2^27 - 1, and fewer than 2^23 workgroups, of which single
- * tokens take one for each sequence, head and 16 query heads of it (else EUNSUPPORTED).  Never allocates, never synchronises; results do not change from run to run.
+ * rounded to bf16 for the matrix cores (each by at most 2^-8 of itself; their sum is that of the unrounded ones), out is rounded once.  A key that a
+ * token does not see has no influence, whatever it holds.
+ * All sequences of a call are cut into tiles of one height, and their keys into as many parts, by rows, count, window and longest: a prompt beside many single tokens, or
+ * one text far longer than the others, is right in one call and faster in calls of their own.
+ * rows * q_heads up to 2^27 - 1, and fewer than 2^23 workgroups, of which single tokens take one for each sequence, head and 16 query heads of it (else
+ * EUNSUPPORTED).  Never allocates, never synchronises; results do not change from run to run.
  */
 int neuzip_cache_attention(const neuzip_cache *cache, const neuzip_sequences *sequences, const void *d_q, uint64_t q_row, uint32_t q_heads,
                            uint32_t rows, float scale, uint32_t window, uint64_t longest, void *d_out, void *d_scratch,

@@ -6,7 +6,9 @@
 // the weights P^T are then, once rounded to bf16, the second product's operand where they are, without a way through LDS.  For that the keys
 // are taken in an order of their own (the sum over them has none): lane group g of four has keys 16 g .. 16 g + 15 of the 64 of a step,
 // which in a page of the values are 16 consecutive bytes.  Bytes become bf16, times their page's scale, by one instruction for two (exact: e4m3 has 4
-// significant bits and scales are powers of two).
+// significant bits and scales are powers of two).  The weights are rounded because the matrix cores multiply bf16 by bf16; their sum is that of the unrounded ones, in
+// binary32.  Against 64 bits the results are off by 0.0020 to 0.0023 of themselves (root mean square), where weights in binary32 have 0.0016 to 0.0017, what the
+// rounding of the result takes alone.
 //
 // attend_few_kernel: a workgroup has up to 16 rows, its waves a step of 64 keys each in turn, keys and values from memory straight into registers; the
 // waves' sums are joined in LDS.  Work is split over the keys too where there are few rows, and joined by attend_join_kernel.
@@ -611,9 +613,11 @@ __global__ void __launch_bounds__(kAttendThreads, 2) attend_some_kernel(const At
 // In LDS: row c of 32 of the keys' operand, its pieces of 16 bytes (8 features) in places p ^ c % 16 (rows of 128 bytes: p ^ c / 2 % 8); the values' row is
 // a feature, 64 keys in 8 pieces, in places p ^ feature / 2 % 8: the sixteen lanes that read together, 0 to 3, 12 to 15, 20 to 27 or the others, find different banks.
 // What bounds it: a step of a wave takes the matrix cores 1024 cycles (head_dim 128), the vector unit about 1450 (exponentials 512, the rest of the softmax
-// 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD and half of it overlaps.  A prompt of 4096 tokens, 32
-// query heads on 8, takes 151 us with 256 rows to a workgroup (911 TFLOP/s), 159 with 128 (matrix cores busy a third of the time, the vector unit 0.4 of it); one of 16384
-// 2.13 ms, 1030 TFLOP/s.  With 128 rows it would take 126 without widening into LDS, 149 without requests, 146 without exponentials.  Tried: a wave with 64 rows halves
+// 400, requests, widening and LDS addresses), LDS 320, for eight waves 2560; two waves share a SIMD.  A prompt of 4096 tokens, 32
+// query heads on 8, takes 148 us with 256 rows to a workgroup (929 TFLOP/s), 159 with 128; one of 16384 2.08 ms, 1057 TFLOP/s.  Neither unit is full: of 4096 tokens the matrix
+// cores are busy 0.36 of the launch and the vector unit issues 0.40 of it (16384: 0.44 and 0.46), with 1.74 (1.92) waves to a SIMD, which spend 0.32 of their time waiting, for
+// LDS, for requests, and for each other at the barrier of a step, which keeps a workgroup's waves in one phase; 0.30 waiting for their turn at a unit that another one has.
+// With 128 rows it would take 126 without widening into LDS, 149 without requests, 146 without exponentials.  Tried: a wave with 64 rows halves
 // what LDS reads, but fills 400 registers and is alone on its SIMD, 350 us; the next step's products beside this step's exponentials in the program, 169 us, as
 // 256 registers leave none for operands on their way; the rows' sums by dot products or in the matrix cores, 178 and 186;
 // the workgroup's halves a phase apart, one at products while the other is at weights, with a barrier to each phase, 151 to 162 against 148 on the same card.

@@ -48,6 +48,9 @@ inline bool attend_is_large(uint32_t head_dim, uint64_t tiles, uint64_t steps)
 // new tokens, `tokens` of a sequence, that look back far).  us, tiles of 128 / 256 rows, 32 query heads on 8, pages of 64: prompts of 4096 tokens 163 / 151, 8192
 // 581 / 555, 2 of 4096 310 / 302, but 3000 91 / 98, 4 of 2048 172 / 173, 64 of 512 272 / 309;  1024 tokens behind 7168 160 / 147, 4 of 512 behind 3584 148 / 138,
 // 512 behind 32256 299 / 275, but 2048 behind 2048 123 / 132.  In pages of 16 the prompt of 4096 takes 155 / 159.
+// Several prompts: 2 of 3100 182 / 186, 2 of 3300 207 / 203, 3 of 3100 267 / 271, 3 of 4096 440 / 440, 6 of 4096 893 / 882, 3 of 6000 929 / 907, 3 of 8192 1665 / 1627; one of
+// 6000 311 / 320; 4 of 1024 behind 3000 255 / 246, 8 of 300 behind 3000 195 / 200.
+// (Heads of 64 have no such tiles: a step's keys are 256 pieces of 16 bytes, half as many as the threads that would ask for them.)
 inline bool attend_is_largest(uint32_t head_dim, uint32_t page_tokens, uint64_t tiles, uint64_t steps, uint64_t tokens)
 {
     return head_dim == 128 && page_tokens >= kAttendStep && steps >= 48 && (tiles >= 1024 || steps * kAttendStep >= 4 * tokens);

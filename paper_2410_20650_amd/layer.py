@@ -186,7 +186,9 @@ class CompressedAttention:
 
     def forward(self, x: torch.Tensor, cache: nz.KeyValueCache, sequences: nz.Sequences, space: torch.Tensor, longest: int = 0) -> torch.Tensor:
         """x: rows x in_features, bf16, the newest tokens of the sequences, whose lengths count them already.  They are put into the cache and look back at
-        it.  Returns float32 rows x out_features."""
+        it.  Returns float32 rows x out_features.  longest: no sequence has more tokens; without it the attention's form is chosen for sequences that
+        fill their rows of the table, which costs time and scratch memory where a table has much more room than they have tokens (the attention of a prompt of 512
+        tokens, 32 heads on 8 of 128, in a table for 131072: 37 us and 34 MB for 12 us and none; of 2048: 69 us for 59)."""
         if x.shape[0] == 0:
             return torch.empty((0, self.out.out_features), dtype=torch.float32, device=x.device)
         parts = (self.queries, self.keys, self.values)
