@@ -486,6 +486,8 @@ uint64_t neuzip_norm_backward_scratch_bytes(uint64_t tokens, uint64_t width);
  *   d_k         pages x heads x page_tokens x head_dim bytes in e4m3 (4 bits of exponent, 3 of mantissa, largest 448, no infinity).
  *   d_v         pages x heads x head_dim x page_tokens bytes, likewise.
  *   d_k_scales, d_v_scales   pages x heads floats, powers of two: a byte stands for its value times its page's and head's scale.
+ *               From 2^-100, the least that neuzip_cache_append sets, to 2^119, so that 448 times it is a bf16 number, which the attention takes bytes as.
+ *               (neuzip_cache_append sets 2^120 for a page and head with numbers beyond 1.75 * 2^127, of which bytes of 256 and more are infinite then.)
  *   heads, head_dim, page_tokens   head_dim 64 or 128, page_tokens 16, 32, 64 or 128 (else EINVAL).
  * d_k and d_v are aligned to 16 bytes.  A new cache needs no filling: what no token was put to is not read for its value.
  */
